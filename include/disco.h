@@ -49,7 +49,7 @@
  * channel; the depthwise calls filter each channel by its own W[c][K]
  * (the depthwise half of the paper's depthwise-separable layers, Sec. 4.2).
  *
- * Conventions for every call:
+ * Conventions for every call (the token and gradient calls at the end add to them):
  *   - every call returns a disco_status_t; on failure nothing is enqueued on
  *     the stream and no output is written; disco_last_error() then holds a
  *     human-readable reason (thread-local, valid until the next call on the
@@ -363,6 +363,120 @@ disco_status_t disco_psi_entries(int nlat_in, int nlon_in, int nlat_out, int nlo
                                  int64_t capacity, int32_t* out_ring, int32_t* phase,
                                  int32_t* in_ring, int32_t* offset, float* values,
                                  int64_t* count, int32_t* phases, int32_t* stride);
+
+/* ---- Attention between grids, and the clipping of gradients -------------
+ *
+ * A network of the layers above reads the states of one grid (an encoder's)
+ * from another grid, from a few latent tokens or from one place, by attention,
+ * and trains all of its weights together.  The calls below do that on token
+ * tensors [batch][tokens][heads][dim], given with their strides, so that the
+ * parts of a joint projection are read, and gradients written, where they lie.
+ * They need no plan: a call runs on the device that holds its first tensor,
+ * which holds all of them.  Types as above (fp32, or bf16 storage with fp32
+ * sums), one type for the tensors of a call; tables, biases and statistics
+ * are fp32.  Scratch memory: `workspace` of at least the bytes that the
+ * ..._workspace call names (256-byte aligned, on the same device, the caller's
+ * until the work is complete), or NULL for the stream-ordered pool. */
+typedef struct {
+    void* data;           /* device pointer (may be NULL only when the tensor is empty) */
+    int32_t dtype;        /* disco_dtype_t */
+    int32_t dim;          /* entries of a head, 1..128, contiguous */
+    int32_t heads;
+    int32_t reserved;     /* 0 */
+    int64_t batch, tokens;
+    int64_t stride_batch, stride_token, stride_head; /* in elements, >= 0; of an output no two rows overlap */
+} disco_heads_t;
+
+enum { DISCO_ROTARY_HALF = 0, DISCO_ROTARY_INTERLEAVED = 1 };
+
+/* Rotation of a head's first rotary_dim entries to the token's position: pair
+ * i < rotary_dim / 2 is (i, i + rotary_dim / 2) in the half layout and (2i, 2i + 1)
+ * in the interleaved one, and turns by the angle whose cosine and sine stand
+ * in row `position` of the tables [rows][rotary_dim / 2]: whatever a network
+ * takes for its angles (line positions stretched for long contexts,
+ * longitudes and colatitudes of a grid) goes into the tables.  A token whose
+ * position is no row of the tables comes out as NaN. */
+typedef struct {
+    int32_t rotary_dim;           /* even, 0..dim */
+    int32_t layout;               /* DISCO_ROTARY_HALF or DISCO_ROTARY_INTERLEAVED */
+    const float* cosines;
+    const float* sines;
+    int64_t rows;
+    const int32_t* positions;     /* [batch][tokens], or NULL: token s stands on row first_position + s */
+    int64_t position_stride_batch; /* elements between batch items of positions; 0: the same for all */
+    int64_t first_position;       /* used without positions only */
+} disco_rotation_t;
+
+/* Norm of every head with the rotation in the same pass:
+ *   y = rotate(w * x / sqrt(mean(x^2) + eps)) for each row (batch, token, head),
+ * the mean over the head's dim entries.  norm = 0: rotation alone (weight
+ * NULL).  weight: NULL (ones), [dim] for all heads, or [heads, dim]; x's type.
+ * rotation: NULL for the norm alone.  y has x's sizes and may be x itself (same
+ * data and strides), otherwise must not overlap it.  Errors: INVALID_ARGUMENT,
+ * SHAPE, DTYPE, DEVICE. */
+disco_status_t disco_norm_rotate(const disco_heads_t* x, int32_t norm, const disco_tensor_t* weight,
+                                 double eps, const disco_rotation_t* rotation, disco_heads_t* y,
+                                 hipStream_t stream);
+
+/* Gradients of disco_norm_rotate for dy: dx (x's sizes; may be dy itself) and
+ * dweight (weight's shape and type; a given weight with a norm only), either may be NULL.
+ * x is the forward input (may be NULL without norm).  dweight is summed in a
+ * fixed order. */
+disco_status_t disco_norm_rotate_backward(const disco_heads_t* x, int32_t norm, const disco_tensor_t* weight,
+                                          double eps, const disco_rotation_t* rotation,
+                                          const disco_heads_t* dy, disco_heads_t* dx, disco_tensor_t* dweight,
+                                          void* workspace, size_t workspace_bytes, hipStream_t stream);
+disco_status_t disco_norm_rotate_workspace(const disco_heads_t* x, const disco_tensor_t* weight, size_t* bytes);
+
+typedef struct {
+    double scale;                /* of the scores; 0 selects 1 / sqrt(dim) */
+    const float* key_bias;       /* NULL, or [batch][keys]: added to the scores of a key, e.g. the logarithm
+                                    of its quadrature weight; -inf takes the key out */
+    int64_t bias_stride_batch;   /* elements between batch items of key_bias; 0: the same for all */
+    const int32_t* key_lengths;  /* NULL, or [batch]: keys at and beyond it are taken out (values
+                                    outside 0..keys are taken as the nearer of the two) */
+} disco_attention_t;
+
+/* Attention of q to the states k, v of another length:
+ *   out[b,i,h] = sum_j p_ij v[b,j,h'], p_i = softmax_j(scale q[b,i,h] . k[b,j,h'] + bias[b,j]),
+ * q, out [batch][queries][heads][dim]; k, v [batch][keys][kv_heads][dim], heads a
+ * multiple of kv_heads, h' = h / (heads / kv_heads).  A query that no key is
+ * left for gives zeros.  What k and v hold at keys taken out (infinities and
+ * NaN too) reaches no output.  A bias below -2^127 counts as -2^127; NaN and +inf give NaN.  stats:
+ * NULL, or [batch][heads][queries][2] floats for the backward call: the
+ * largest score of the row in units of log 2 (-inf: no key) and the sum of
+ * 2^(score - largest).  The split of a long axis of keys between workgroups
+ * depends on the sizes alone, and partial sums are joined in a fixed order.
+ * options NULL: defaults.  batch * heads <= 65535 * 8.  Errors:
+ * INVALID_ARGUMENT, SHAPE, DTYPE, OUT_OF_MEMORY, DEVICE. */
+disco_status_t disco_cross_attention(const disco_heads_t* q, const disco_heads_t* k, const disco_heads_t* v,
+                                     const disco_attention_t* options, disco_heads_t* out, float* stats,
+                                     void* workspace, size_t workspace_bytes, hipStream_t stream);
+
+/* Gradients of disco_cross_attention for dout, from its inputs and its out
+ * and stats: dq, dk, dv (sizes of q, k, v), all written.  The gradients of keys that are
+ * taken out are zero.  Sums run in a fixed order. */
+disco_status_t disco_cross_attention_backward(const disco_heads_t* q, const disco_heads_t* k,
+                                              const disco_heads_t* v, const disco_attention_t* options,
+                                              const disco_heads_t* out, const float* stats,
+                                              const disco_heads_t* dout, disco_heads_t* dq, disco_heads_t* dk,
+                                              disco_heads_t* dv, void* workspace, size_t workspace_bytes,
+                                              hipStream_t stream);
+/* Scratch bytes of the call (backward = 0) or of its gradients (backward = 1).  Host only. */
+disco_status_t disco_cross_attention_workspace(const disco_heads_t* q, const disco_heads_t* k, int32_t backward,
+                                               size_t* bytes);
+
+/* Global norm of many gradients and clipping by it:
+ *   norm = sqrt(sum over tensors and entries of g^2),
+ *   clipped = g * min(1, max_norm / (norm + eps)),
+ * grads[count] of any shapes (ndim 0..4), each fp32 or bf16; clipped[i] of grads[i]'s type and
+ * shape, the same memory (in place) or apart from all of them; clipped NULL: the norm alone.  norm: one
+ * device float.  The squares are summed in 64 bits in an order that depends on
+ * the sizes alone; nothing is read back to the host.  A norm that is not finite propagates as the formula has it. */
+disco_status_t disco_gradient_clip(int32_t count, const disco_tensor_t* grads, disco_tensor_t* clipped,
+                                   double max_norm, double eps, float* norm, void* workspace,
+                                   size_t workspace_bytes, hipStream_t stream);
+disco_status_t disco_gradient_clip_workspace(int32_t count, const disco_tensor_t* grads, size_t* bytes);
 
 /* Kernel timing for measurement tools.  While enabled (on != 0), every
  * kernel the library launches from this process is bracketed by HIP events

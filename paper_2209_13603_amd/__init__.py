@@ -6,4 +6,4 @@ thin ctypes binding; ``paper_2209_13603_amd.synth`` holds the seeded workload
 inputs.  The library is loaded on first use and a missing or unbuilt library
 raises immediately: there is no CPU fallback.
 """
-__all__ = ["disco", "synth"]
+__all__ = ["attention", "disco", "gradients", "synth"]

@@ -22,7 +22,8 @@ DEBUG_BOUNDS_LIB_PATH = os.path.join(BUILD_DIR, "libdisco_debug_bounds.so")
 
 SOURCES = ["disco_plan.cpp", "disco_pack.cpp", "disco_spectral_plan.cpp", "disco_abi.cpp", "disco_kernels.hip",
            "disco_fused.hip", "disco_spectral.hip", "disco_sweep.hip", "disco_stencil.hip", "disco_grad.hip",
-           "disco_noalloc.hip", "disco_mfma.hip"]
+           "disco_noalloc.hip", "disco_mfma.hip", "disco_heads_abi.cpp", "disco_rotate.hip", "disco_attend.hip",
+           "disco_attend_grad.hip", "disco_clip.hip"]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 ROCM = os.environ.get("ROCM_PATH", "/opt/rocm")
 # roctx ranges around plan creation and the ops (no-ops without a profiler).
@@ -48,7 +49,7 @@ def _run(cmd, verbose):
         print(out)
 
 
-def build(verbose: bool = False, jobs: int = 5, debug_bounds: bool = False) -> str:
+def build(verbose: bool = False, jobs: int = 8, debug_bounds: bool = False) -> str:
     """Compile the library for gfx950; with debug_bounds the build that
     checks the kernels' psi indices (DISCO_DEBUG_BOUNDS), written beside it."""
     os.makedirs(BUILD_DIR, exist_ok=True)

@@ -58,7 +58,10 @@ EXPORTS = ("disco_plan_create", "disco_plan_destroy", "disco_plan_query", "disco
            "disco_forward_depthwise_backward", "disco_transpose_depthwise_backward",
            "disco_psi_entries", "disco_forward_noalloc",
            "disco_kernel_timing_enable", "disco_kernel_timing_read", "disco_kernel_work",
-           "disco_status_string", "disco_last_error", "disco_debug_bounds_violations")
+           "disco_status_string", "disco_last_error", "disco_debug_bounds_violations",
+           "disco_norm_rotate", "disco_norm_rotate_backward", "disco_norm_rotate_workspace",
+           "disco_cross_attention", "disco_cross_attention_backward", "disco_cross_attention_workspace",
+           "disco_gradient_clip", "disco_gradient_clip_workspace")
 
 
 def debug_bounds_violations() -> int:
@@ -83,6 +86,27 @@ class Basis(ctypes.Structure):
 class Tensor(ctypes.Structure):
     _fields_ = [("data", ctypes.c_void_p), ("dtype", ctypes.c_int32), ("ndim", ctypes.c_int32),
                 ("shape", ctypes.c_int64 * 4)]
+
+
+class Heads(ctypes.Structure):
+    """disco_heads_t: a token tensor [batch, tokens, heads, dim] with its strides."""
+    _fields_ = [("data", ctypes.c_void_p), ("dtype", ctypes.c_int32), ("dim", ctypes.c_int32),
+                ("heads", ctypes.c_int32), ("reserved", ctypes.c_int32), ("batch", ctypes.c_int64),
+                ("tokens", ctypes.c_int64), ("stride_batch", ctypes.c_int64), ("stride_token", ctypes.c_int64),
+                ("stride_head", ctypes.c_int64)]
+
+
+class RotationArgs(ctypes.Structure):
+    """disco_rotation_t."""
+    _fields_ = [("rotary_dim", ctypes.c_int32), ("layout", ctypes.c_int32), ("cosines", ctypes.c_void_p),
+                ("sines", ctypes.c_void_p), ("rows", ctypes.c_int64), ("positions", ctypes.c_void_p),
+                ("position_stride_batch", ctypes.c_int64), ("first_position", ctypes.c_int64)]
+
+
+class AttentionArgs(ctypes.Structure):
+    """disco_attention_t."""
+    _fields_ = [("scale", ctypes.c_double), ("key_bias", ctypes.c_void_p), ("bias_stride_batch", ctypes.c_int64),
+                ("key_lengths", ctypes.c_void_p)]
 
 
 class PlanInfo(ctypes.Structure):
@@ -171,6 +195,22 @@ def library(path: str = None) -> ctypes.CDLL:
     lib.disco_status_string.restype = ctypes.c_char_p
     lib.disco_last_error.argtypes = []
     lib.disco_last_error.restype = ctypes.c_char_p
+    V, Z, I32, S = ctypes.c_void_p, ctypes.c_size_t, ctypes.c_int32, P(ctypes.c_size_t)
+    H, T, R, A = P(Heads), P(Tensor), P(RotationArgs), P(AttentionArgs)
+    token_calls = {
+        "disco_norm_rotate": [H, I32, T, ctypes.c_double, R, H, V],
+        "disco_norm_rotate_backward": [H, I32, T, ctypes.c_double, R, H, H, T, V, Z, V],
+        "disco_norm_rotate_workspace": [H, T, S],
+        "disco_cross_attention": [H, H, H, A, H, V, V, Z, V],
+        "disco_cross_attention_backward": [H, H, H, A, H, V, H, H, H, H, V, Z, V],
+        "disco_cross_attention_workspace": [H, H, I32, S],
+        # the tensor arrays of many gradients come as addresses
+        "disco_gradient_clip": [I32, V, V, ctypes.c_double, ctypes.c_double, V, V, Z, V],
+        "disco_gradient_clip_workspace": [I32, V, S],
+    }
+    for name, args in token_calls.items():
+        getattr(lib, name).argtypes = args
+        getattr(lib, name).restype = ctypes.c_int
     lib.disco_debug_bounds_violations.argtypes = []
     lib.disco_debug_bounds_violations.restype = ctypes.c_int32
     _lib = lib
