@@ -442,24 +442,29 @@ typedef struct {
  * q, out [batch][queries][heads][dim]; k, v [batch][keys][kv_heads][dim], heads a
  * multiple of kv_heads, h' = h / (heads / kv_heads).  A query that no key is
  * left for gives zeros.  What k and v hold at keys taken out (infinities and
- * NaN too) reaches no output.  A bias below -2^127 counts as -2^127; NaN and +inf give NaN.  stats:
- * NULL, or [batch][heads][queries][2] floats for the backward call: the
- * largest score of the row in units of log 2 (-inf: no key) and the sum of
- * 2^(score - largest).  The split of a long axis of keys between workgroups
- * depends on the sizes alone, and partial sums are joined in a fixed order.
+ * NaN too) reaches no output.  Finite biases below -2^100 |scale| count as that;
+ * NaN and +inf give NaN.  For the backward call:
+ *   stats  NULL, or [batch][heads][queries][2] floats: a reference near the
+ *          row's largest score in units of log 2 (-inf: no key) and the sum of
+ *          2^(score - reference);
+ *   low    NULL, or (bf16 only, optional) a tensor of out's sizes that takes
+ *          what rounding took from out, so that the gradients' row sums
+ *          dout . out do not carry out's rounding.
+ * The split of a long axis of keys between workgroups depends on the sizes
+ * alone, and partial sums are joined in a fixed order.
  * options NULL: defaults.  batch * heads <= 65535 * 8.  Errors:
  * INVALID_ARGUMENT, SHAPE, DTYPE, OUT_OF_MEMORY, DEVICE. */
 disco_status_t disco_cross_attention(const disco_heads_t* q, const disco_heads_t* k, const disco_heads_t* v,
                                      const disco_attention_t* options, disco_heads_t* out, float* stats,
-                                     void* workspace, size_t workspace_bytes, hipStream_t stream);
+                                     disco_heads_t* low, void* workspace, size_t workspace_bytes, hipStream_t stream);
 
-/* Gradients of disco_cross_attention for dout, from its inputs and its out
- * and stats: dq, dk, dv (sizes of q, k, v), all written.  The gradients of keys that are
+/* Gradients of disco_cross_attention for dout, from its inputs and its out,
+ * stats and low (NULL where it was not asked for): dq, dk, dv (sizes of q, k, v), all written.  The gradients of keys that are
  * taken out are zero.  Sums run in a fixed order. */
 disco_status_t disco_cross_attention_backward(const disco_heads_t* q, const disco_heads_t* k,
                                               const disco_heads_t* v, const disco_attention_t* options,
                                               const disco_heads_t* out, const float* stats,
-                                              const disco_heads_t* dout, disco_heads_t* dq, disco_heads_t* dk,
+                                              const disco_heads_t* low, const disco_heads_t* dout, disco_heads_t* dq, disco_heads_t* dk,
                                               disco_heads_t* dv, void* workspace, size_t workspace_bytes,
                                               hipStream_t stream);
 /* Scratch bytes of the call (backward = 0) or of its gradients (backward = 1).  Host only. */

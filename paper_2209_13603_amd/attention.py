@@ -17,10 +17,19 @@ from __future__ import annotations
 import contextlib
 import ctypes
 import math
+from typing import NamedTuple
 
 from .disco import (AttentionArgs, DISCO_BFLOAT16, DISCO_FLOAT32, Heads, RotationArgs, _check, _tensor, library)
 
 LAYOUTS = {"half": 0, "interleaved": 1}
+
+
+class Stats(NamedTuple):
+    """What ``cross_attention`` keeps for its gradients: rows fp32 [B, H, Sq, 2], a reference near each row's
+    largest score in units of log 2 and the sum of 2^(score - reference), so that the logarithm of the
+    softmax's sum is (rows[..., 0] + log2(rows[..., 1])) * log(2); low, in bf16 storage, what rounding took from out."""
+    rows: object
+    low: object
 
 
 def _dtype(t):
@@ -186,8 +195,7 @@ def cross_attention(q, k, v, key_bias=None, key_lengths=None, scale=None, return
 
     key_bias: None or fp32 [Sk] or [B, Sk] (the logarithm of a quadrature weight; -inf takes the key
     out).  key_lengths: None or int32 [B].  scale: 1 / sqrt(D) where None.  A query that no key is left for
-    gives zeros.  return_stats: (out, stats), stats fp32 [B, H, Sq, 2] for ``cross_attention_backward``;
-    the logarithm of the softmax's sum is (stats[..., 0] + log2(stats[..., 1])) * log(2).
+    gives zeros.  return_stats: (out, Stats) for ``cross_attention_backward``.
     """
     import torch
     call = _Call(q, stream)
@@ -196,14 +204,16 @@ def cross_attention(q, k, v, key_bias=None, key_lengths=None, scale=None, return
     if scale == 0.0:
         raise ValueError("scale must not be 0")
     _same_device(q, k, v, out)
-    stats = call.empty((q.shape[0], q.shape[2], q.shape[1], 2), torch.float32) if return_stats else None
+    rows = call.empty((q.shape[0], q.shape[2], q.shape[1], 2), torch.float32) if return_stats else None
+    low = call.empty(q.shape, q.dtype) if return_stats and q.dtype == torch.bfloat16 else None
+    hlow = _heads(low, "low") if low is not None else None
     hq, hk = _heads(q, "q"), _heads(k, "k")
     opt = _options(q, k, key_bias, key_lengths, scale)
     keep, ws, n = call.workspace("disco_cross_attention_workspace", hq, hk, 0)
     _check(library().disco_cross_attention(hq, hk, _heads(v, "v"), opt, _heads(out, "out"),
-                                           stats.data_ptr() if stats is not None and stats.numel() else None, ws, n,
-                                           call.handle))
-    return (out, stats) if return_stats else out
+                                           rows.data_ptr() if rows is not None and rows.numel() else None, _ref(hlow),
+                                           ws, n, call.handle))
+    return (out, Stats(rows, low)) if return_stats else out
 
 
 def cross_attention_backward(q, k, v, out, stats, dout, key_bias=None, key_lengths=None, scale=None, dq=None, dk=None,
@@ -218,16 +228,18 @@ def cross_attention_backward(q, k, v, out, stats, dout, key_bias=None, key_lengt
     dv = call.empty(v.shape, v.dtype) if dv is None else dv
     if scale == 0.0:
         raise ValueError("scale must not be 0")
-    _same_device(q, k, v, out, stats, dout, dq, dk, dv)
-    _flat(stats, "stats", torch.float32, ((q.shape[0], q.shape[2], q.shape[1], 2),))
-    if not stats.is_contiguous():
-        raise ValueError("stats must be contiguous")
+    rows, low = stats
+    _same_device(q, k, v, out, rows, low, dout, dq, dk, dv)
+    _flat(rows, "stats.rows", torch.float32, ((q.shape[0], q.shape[2], q.shape[1], 2),))
+    if not rows.is_contiguous():
+        raise ValueError("stats.rows must be contiguous")
+    hlow = _heads(low, "stats.low") if low is not None else None
     hq, hk = _heads(q, "q"), _heads(k, "k")
     opt = _options(q, k, key_bias, key_lengths, scale)
     keep, ws, n = call.workspace("disco_cross_attention_workspace", hq, hk, 1)
     _check(library().disco_cross_attention_backward(
-        hq, hk, _heads(v, "v"), opt, _heads(out, "out"), stats.data_ptr() if stats.numel() else None,
-        _heads(dout, "dout"), _heads(dq, "dq"), _heads(dk, "dk"), _heads(dv, "dv"), ws, n, call.handle))
+        hq, hk, _heads(v, "v"), opt, _heads(out, "out"), rows.data_ptr() if rows.numel() else None,
+        _ref(hlow), _heads(dout, "dout"), _heads(dq, "dq"), _heads(dk, "dk"), _heads(dv, "dv"), ws, n, call.handle))
     return dq, dk, dv
 
 

@@ -1,12 +1,51 @@
-// disco_attend.h -- device helpers shared by the cross-attention kernels.
+// disco_attend.h -- device parts shared by the cross-attention kernels.
+//
+// All products run on matrix-core tiles of 32 x 32 whose column is a lane's own
+// (lane % 32), so that the softmax of a row, which stands in the columns of the
+// transposed scores, needs one exchange between two lanes and no broadcast.
+//
+//   scores  S[32 rows of an LDS tile][32 columns] += tile x fragments, the
+//           fragments (one vector of `dim` entries a column) in registers;
+//   values  O[32 entries d][32 columns] += tile^T x P, P in the layout that the
+//           scores leave: lane n + 32 h holds in register i the column n of row
+//           8 (i / 4) + 4 h + i % 4.  The sum over rows may run in any order, so
+//           P goes back into the matrix cores as it lies and the tile is read in
+//           that order.
+//
+// bf16 takes v_mfma_f32_32x32x16_bf16 and the transposing LDS read; fp32 takes
+// v_mfma_f32_32x32x2_f32 (its operands are single values, so nothing needs to be
+// transposed) and is exact to fp32 rounding.
+//
+// LDS tile: chunks of 16 bytes, 16 rows x 4 chunks to a segment of 1 KB, at
+// (c % 4) * 256 + ((row % 16) ^ 4 (c % 4)) * 16.  Row reads (a lane a row, 16
+// bytes), transposed reads (4 rows x 16 entries) and the staging writes (4 lanes
+// a row) all spread over the banks, and every address is a lane's own offset plus a
+// constant.
 #pragma once
 #include <hip/hip_runtime.h>
+
+#include <type_traits>
 
 #include "disco_heads.h"
 
 namespace disco {
 
-constexpr float kLog2e = 1.4426950408889634f;
+typedef float f4 __attribute__((ext_vector_type(4)));
+typedef float f8 __attribute__((ext_vector_type(8)));
+typedef float f16 __attribute__((ext_vector_type(16)));
+typedef __bf16 bf8 __attribute__((ext_vector_type(8)));
+typedef __bf16 bf4 __attribute__((ext_vector_type(4)));
+typedef short s4 __attribute__((ext_vector_type(4)));
+typedef short s8 __attribute__((ext_vector_type(8)));
+typedef uint32_t u4 __attribute__((ext_vector_type(4)));
+typedef __attribute__((address_space(3))) char lds_t;
+
+constexpr int kWave = 64;
+constexpr int kAttendThreads = 256;
+constexpr int kAttendWaves = kAttendThreads / kWave;
+// Finite biases stay above -2^100 in units of the scale: a mask of the type's
+// lowest value takes no key out, and must not become -inf on the way.
+constexpr float kLowestBias = -0x1p+100f;
 
 // Keys of batch item b that its length leaves.
 __device__ __forceinline__ int64_t key_count(const AttendArgs& a, int b) {
@@ -15,14 +54,211 @@ __device__ __forceinline__ int64_t key_count(const AttendArgs& a, int b) {
     return n < 0 ? 0 : n > a.keys ? a.keys : n;
 }
 
-// The bias of a key in units of log 2: -inf takes the key out, finite values
-// stay finite (a mask of the type's lowest value must not become -inf).
-__device__ __forceinline__ float bias2_of(float bias) {
-    const float t = bias * kLog2e;
-    return bias < -0x1p+127f && bias != -INFINITY ? -0x1p+127f * kLog2e : t;
+// What a key's score starts from, in units of the scale (positive here): the
+// product is added onto it in the matrix cores.
+__device__ __forceinline__ float start_of(float bias, float inv_scale) {
+    const float t = bias * inv_scale;
+    return t < kLowestBias && bias != -INFINITY ? kLowestBias : t;
 }
-__device__ __forceinline__ float key_bias2(const AttendArgs& a, int b, int64_t j) {
-    return a.bias ? bias2_of(a.bias[b * a.bias_sb + j]) : 0.0f;
+
+// Workgroups go round the XCDs one by one: gives each XCD a run of consecutive
+// work items, which share keys, values or queries in its L2.  Grid: 8 * ceil(n / 8).
+__device__ __forceinline__ int64_t xcd_item(int64_t n) {
+    const int64_t per = (n + 7) / 8;
+    return (int64_t)(blockIdx.x % 8) * per + blockIdx.x / 8;
+}
+inline unsigned xcd_grid(int64_t n) { return (unsigned)((n + 7) / 8 * 8); }
+
+__device__ __forceinline__ float other_half(float v) { return __shfl_xor(v, 32); }
+
+template <typename T>
+struct Mat;
+template <>
+struct Mat<__bf16> {
+    typedef bf8 Frag;
+    static constexpr int CH = 8;  // entries of a chunk
+    static __device__ __forceinline__ f16 scores(Frag a, Frag b, f16 c) {
+        return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
+    }
+};
+template <>
+struct Mat<float> {
+    typedef f4 Frag;
+    static constexpr int CH = 4;
+    static __device__ __forceinline__ f16 scores(Frag a, Frag b, f16 c) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) c = __builtin_amdgcn_mfma_f32_32x32x2f32(a[j], b[j], c, 0, 0, 0);
+        return c;
+    }
+};
+
+template <typename T, int DP>
+struct TileOf {
+    static constexpr int CH = Mat<T>::CH, NC = DP / CH, SEGS = NC / 4, NS = NC / 2;
+    static constexpr int kStep16 = SEGS * 1024;  // bytes of 16 rows
+    static_assert(NC % 4 == 0, "whole segments");
+    typedef typename Mat<T>::Frag Frag;
+    struct Lane {
+        uint32_t even, odd;  // row reads: chunks 2s + h of row lane % 32, s even and odd
+        uint32_t t0, t1;     // transposed reads: the first and the second eight rows of 16
+    };
+    static __device__ __forceinline__ Lane lane_of(int lane) {
+        const int h = lane / 32, i = lane % 16;
+        Lane o;
+        const uint32_t r = (uint32_t)((lane % 32) / 16) * kStep16;
+        o.even = r + h * 256 + ((i ^ (4 * h)) * 16);
+        o.odd = r + (2 + h) * 256 + ((i ^ (8 + 4 * h)) * 16);
+        if (std::is_same<T, __bf16>::value) {
+            const int cm = 2 * ((lane / 16) % 2) + (i % 4) / 2, row = 4 * h + i / 4;
+            o.t0 = cm * 256 + ((row ^ (4 * cm)) * 16) + (i % 2) * 8;
+            o.t1 = cm * 256 + (((row + 8) ^ (4 * cm)) * 16) + (i % 2) * 8;
+        } else {
+            const int cm = (lane / 4) % 4;
+            const uint32_t base = ((lane % 32) / 16) * 1024 + cm * 256 + (lane % 4) * 4;
+            o.t0 = base + (((4 * h) ^ (4 * cm)) * 16);
+            o.t1 = base + (((8 + 4 * h) ^ (4 * cm)) * 16);
+        }
+        return o;
+    }
+    // Rows 32 k .. 32 k + 31 of the tile, fragment s of each lane's row.
+    static __device__ __forceinline__ Frag row(const lds_t* tile, const Lane& l, int k, int s) {
+        typedef __attribute__((address_space(3))) const Frag F;
+        return *(F*)(tile + (s % 2 ? l.odd : l.even) + (s / 2) * 1024 + k * 2 * kStep16);
+    }
+    static __device__ __forceinline__ f16 scores(const lds_t* tile, const Lane& l, int k, const Frag (&f)[NS], f16 c) {
+#pragma unroll
+        for (int s = 0; s < NS; ++s) c = Mat<T>::scores(row(tile, l, k, s), f[s], c);
+        return c;
+    }
+    // o[D / 32] += (rows 32 k .. 32 k + 31 of the tile)^T x p
+    static __device__ __forceinline__ void values(const lds_t* tile, const Lane& l, int k, const f16& p,
+                                                  f16 (&o)[DP / 32]) {
+        if constexpr (std::is_same<T, __bf16>::value) {
+            typedef __attribute__((address_space(3))) s4 V;
+#pragma unroll
+            for (int ks = 0; ks < 2; ++ks) {
+                f8 e;
+#pragma unroll
+                for (int j = 0; j < 8; ++j) e[j] = p[8 * ks + j];
+                const bf8 b = __builtin_convertvector(e, bf8);  // to nearest: half of the result's own rounding
+#pragma unroll
+                for (int d = 0; d < DP / 32; ++d) {
+                    const uint32_t at = d * 1024 + (2 * k + ks) * kStep16;
+                    const s4 v0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((V*)(tile + l.t0 + at));
+                    const s4 v1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((V*)(tile + l.t1 + at));
+                    const bf8 a = __builtin_bit_cast(bf8, __builtin_shufflevector(v0, v1, 0, 1, 2, 3, 4, 5, 6, 7));
+                    o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, o[d], 0, 0, 0);
+                }
+            }
+        } else {
+            typedef __attribute__((address_space(3))) const float V;
+#pragma unroll
+            for (int i = 0; i < 16; ++i)
+#pragma unroll
+                for (int d = 0; d < DP / 32; ++d) {
+                    const uint32_t at = 2 * d * 1024 + (2 * k + i / 8) * kStep16 + (i % 4) * 16;
+                    const float v = *(V*)(tile + ((i / 4) % 2 ? l.t1 : l.t0) + at);
+                    o[d] = __builtin_amdgcn_mfma_f32_32x32x2f32(v, p[i], o[d], 0, 0, 0);
+                }
+        }
+    }
+};
+
+// 16 bytes of a row from entry c on, zeros beyond D.
+template <typename T>
+__device__ __forceinline__ u4 load_chunk(const T* row, int c, int D, bool wide) {
+    constexpr int CH = Mat<T>::CH;
+    if (c >= D) return u4{0u, 0u, 0u, 0u};
+    if (wide) return *(const u4*)(row + c);
+    typename Mat<T>::Frag f;
+#pragma unroll
+    for (int j = 0; j < CH; ++j) f[j] = c + j < D ? row[c + j] : (T)0.0f;
+    return __builtin_bit_cast(u4, f);
+}
+
+// A tile of ROWS rows on its way from memory to LDS, spread over the
+// workgroup's waves: each wave takes segments (16 rows x 4 chunks, a row's 64
+// bytes by four lanes).
+template <typename T, int DP, int ROWS>
+struct Stage {
+    typedef TileOf<T, DP> Tile;
+    static constexpr int kSegs = ROWS / 16 * Tile::SEGS;
+    static constexpr int N = (kSegs + kAttendWaves - 1) / kAttendWaves;
+    static constexpr int kBytes = kSegs * 1024;
+    u4 v[N];
+    static __device__ __forceinline__ int seg(int wave, int u) { return wave * N + u; }
+    static __device__ __forceinline__ bool has(int wave, int u) { return kSegs % kAttendWaves == 0 || seg(wave, u) < kSegs; }
+    static __device__ __forceinline__ int row_of(int wave, int lane, int u) {
+        return seg(wave, u) / Tile::SEGS * 16 + lane / 4;
+    }
+    // Rows row0 .. of a matrix of `rows` > 0 rows; those beyond come as the last one.
+    __device__ __forceinline__ void load(const T* base, int64_t stride, int64_t row0, int64_t rows, int D, bool wide,
+                                         int wave, int lane) {
+#pragma unroll
+        for (int u = 0; u < N; ++u) {
+            if (!has(wave, u)) continue;
+            const int64_t left = rows - 1 - row0;
+            const int r = (int)min((int64_t)row_of(wave, lane, u), left);
+            const int c = (seg(wave, u) % Tile::SEGS * 4 + lane % 4) * Mat<T>::CH;
+            v[u] = load_chunk(base + (row0 + r) * stride, c, D, wide);
+        }
+    }
+    // keep(row of the tile): whether the row's values count; zeros otherwise, so
+    // that whatever memory holds there meets no product.
+    template <typename F>
+    __device__ __forceinline__ void store(lds_t* tile, int wave, int lane, F&& keep) const {
+        typedef __attribute__((address_space(3))) u4 V;
+#pragma unroll
+        for (int u = 0; u < N; ++u) {
+            if (!has(wave, u)) continue;
+            const u4 z = keep(u) ? v[u] : u4{0u, 0u, 0u, 0u};
+            *(V*)(tile + seg(wave, u) * 1024 + (lane % 4) * 256 + (((lane / 4) ^ (4 * (lane % 4))) * 16)) = z;
+        }
+    }
+};
+
+// A lane's column vector as fragments: entries 2 CH s + CH h + j.
+template <typename T, int DP>
+__device__ __forceinline__ void load_frags(const T* row, int D, bool wide, bool live, int lane,
+                                           typename Mat<T>::Frag (&f)[TileOf<T, DP>::NS]) {
+    constexpr int CH = Mat<T>::CH;
+#pragma unroll
+    for (int s = 0; s < TileOf<T, DP>::NS; ++s) {
+        const u4 z = {0u, 0u, 0u, 0u};
+        f[s] = __builtin_bit_cast(typename Mat<T>::Frag,
+                                  live ? load_chunk(row, 2 * CH * s + CH * (lane / 32), D, wide) : z);
+    }
+}
+
+// Writes four consecutive entries.
+__device__ __forceinline__ void store4(__bf16* p, f4 v) { *(bf4*)p = __builtin_convertvector(v, bf4); }
+__device__ __forceinline__ void store4(float* p, f4 v) { *(f4*)p = v; }
+
+// A lane's column of accumulators o (entry 32 d + 8 (i / 4) + 4 h + i % 4 in
+// register i), times f, to the row's D entries.
+template <typename T, int DP>
+__device__ __forceinline__ void store_column(T* row, const f16 (&o)[DP / 32], float f, int D, bool wide, int lane) {
+#pragma unroll
+    for (int d = 0; d < DP / 32; ++d)
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            const int c = 32 * d + 8 * q + 4 * (lane / 32);
+            const f4 v = {o[d][4 * q] * f, o[d][4 * q + 1] * f, o[d][4 * q + 2] * f, o[d][4 * q + 3] * f};
+            if (wide) {
+                if (c < D) store4(row + c, v);
+            } else {
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                    if (c + j < D) row[c + j] = (T)v[j];
+            }
+        }
+}
+
+// Host: whether rows of D entries can be read or written 16 (fp32 columns) or
+// 8 bytes at a time.
+inline bool wide_rows(const Heads& t, int dim, int entries, size_t elem) {
+    return dim % entries == 0 && (uintptr_t)t.p % (entries * elem) == 0 && t.sb % entries == 0 && t.st % entries == 0 &&
+           t.sh % entries == 0;
 }
 
 }  // namespace disco

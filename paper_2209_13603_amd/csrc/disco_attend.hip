@@ -1,7 +1,9 @@
 // disco_attend.hip -- cross attention, forward.
 //
-// Scores are held in units of log 2: t_ij = scale2 q_i.k_j + bias2_j, and
-// p_ij = 2^(t_ij - m_i) / l_i with the running row maximum m and sum l, fp32.
+// One pass over the keys with the running maximum m and sum l of each row's
+// softmax, in units of log 2: t_ij = scale2 (q_i . k_j + bias_j / scale),
+// p_ij = 2^(t_ij - m_i), o_i = sum_j p_ij v_j / l_i.  The heads that share keys
+// and values are rows of one tile (row = query * group + head of the group).
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -14,82 +16,279 @@ namespace disco {
 
 namespace {
 
-constexpr int kTile = 256;
+// How a call is cut: blocks of kRows rows of each (batch item, kv head), their
+// keys in `splits` parts.  Parts leave unnormed sums, joined by k_attend_join.
+constexpr int kRows = 32 * kAttendWaves;
+struct Cut {
+    int64_t rows, row_blocks, items;
+    int32_t splits;
+    float* part;   // [splits][all rows][dim]
+    float* stat;   // [splits][all rows][2]
+    uint8_t wide_q, wide_k, wide_v, wide_o, wide_low;
+};
 
+// Workgroups of a CU that the registers are sized for.
+template <typename T, int DP>
+constexpr int kWorkgroups = std::is_same<T, float>::value && DP > 96 ? 1 : 2;
 template <typename T>
-__device__ __forceinline__ float dot(const T* a, const T* b, int D) {
-    float s = 0.0f;
-    for (int d = 0; d < D; ++d) s = fmaf((float)a[d], (float)b[d], s);
-    return s;
-}
+constexpr int kKeys = std::is_same<T, __bf16>::value ? 64 : 32;  // keys of a tile
 
-__device__ __forceinline__ float block_max(float v, float* red) {
-    for (int m = 32; m > 0; m >>= 1) v = fmaxf(v, __shfl_xor(v, m));
-    __syncthreads();
-    if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = v;
-    __syncthreads();
-    return fmaxf(fmaxf(red[0], red[1]), fmaxf(red[2], red[3]));
-}
+// Each wave holds 32 rows; the workgroup's waves share the tiles of keys and
+// values, double-buffered in LDS, the next tile's loads in flight in registers.
+template <typename T, int DP>
+__global__ __launch_bounds__(kAttendThreads, (kWorkgroups<T, DP>)) void k_attend(AttendArgs a, Cut c) {
+    typedef TileOf<T, DP> Tile;
+    constexpr int KT = kKeys<T>, NK = KT / 32;
+    typedef Stage<T, DP, KT> St;
+    __shared__ __align__(16) char smem[2 * 2 * St::kBytes];
+    __shared__ float starts[2][KT];
+    lds_t* lds = (lds_t*)smem;
 
-// One workgroup a query row; grid: (queries, batch * heads).
-template <typename T>
-__global__ __launch_bounds__(kTile) void k_attend(AttendArgs a) {
-    __shared__ float p[kTile], red[4], acc[kTile];
-    const int64_t i = blockIdx.x;
-    const int b = blockIdx.y / a.heads, h = blockIdx.y % a.heads, hk = h / (a.heads / a.kv_heads);
-    const T* q = (const T*)a.q.p + b * a.q.sb + i * a.q.st + h * a.q.sh;
-    const T* k = (const T*)a.k.p + b * a.k.sb + hk * a.k.sh;
-    const T* v = (const T*)a.v.p + b * a.v.sb + hk * a.v.sh;
-    const int64_t n = key_count(a, b);
-    const int dp = a.dim <= 32 ? 32 : a.dim <= 64 ? 64 : 128, d = threadIdx.x % dp, slice = threadIdx.x / dp;
-    float m = -INFINITY, l = 0.0f, o = 0.0f;
-    for (int64_t j0 = 0; j0 < n; j0 += kTile) {
-        const int64_t j = j0 + threadIdx.x;
-        float t = -INFINITY;
-        if (j < n) {
-            const float bias2 = key_bias2(a, b, j);
-            if (bias2 != -INFINITY) t = fmaf(dot(q, k + j * a.k.st, a.dim), a.scale2, bias2);
+    const int64_t id = xcd_item(c.items);
+    if (id >= c.items) return;
+    const int split = (int)(id % c.splits);
+    const int64_t rb = id / c.splits % c.row_blocks;
+    const int bh = (int)(id / c.splits / c.row_blocks), b = bh / a.kv_heads, hk = bh % a.kv_heads;
+    const int wave = threadIdx.x / kWave, lane = threadIdx.x % kWave, G = a.heads / a.kv_heads;
+    const int64_t row = rb * kRows + wave * 32 + lane % 32;
+    const bool live = row < c.rows;
+    const int64_t i = live ? row / G : 0;
+    const int h = hk * G + (int)(live ? row % G : 0);
+    const T* kp = (const T*)a.k.p + b * a.k.sb + hk * a.k.sh;
+    const T* vp = (const T*)a.v.p + b * a.v.sb + hk * a.v.sh;
+    const int64_t n = key_count(a, b), tiles = (n + KT - 1) / KT;
+    const int64_t t0 = tiles * split / c.splits, t1 = tiles * (split + 1) / c.splits;
+
+    typename Tile::Frag qf[Tile::NS];
+    load_frags<T, DP>((const T*)a.q.p + b * a.q.sb + i * a.q.st + h * a.q.sh, a.dim, c.wide_q, live, lane, qf);
+    if (a.scale2 < 0.0f)
+#pragma unroll
+        for (int s = 0; s < Tile::NS; ++s) qf[s] = -qf[s];
+    const float scale2 = fabsf(a.scale2), inv_scale = 1.0f / fabsf(a.scale);
+    const typename Tile::Lane ln = Tile::lane_of(lane);
+
+    f16 o[DP / 32];
+#pragma unroll
+    for (int d = 0; d < DP / 32; ++d)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) o[d][r] = 0.0f;
+    float m = -INFINITY, l = 0.0f;
+
+    St sk, sv;
+    float start[St::N], start1 = 0.0f;  // of the staged rows, and of key threadIdx.x of the tile
+    auto load = [&](int64_t t) {
+        sk.load(kp, a.k.st, t * KT, n, a.dim, c.wide_k, wave, lane);
+        sv.load(vp, a.v.st, t * KT, n, a.dim, c.wide_v, wave, lane);
+        auto start_at = [&](int64_t j) {
+            return j >= n ? -INFINITY : a.bias ? start_of(a.bias[b * a.bias_sb + j], inv_scale) : 0.0f;
+        };
+#pragma unroll
+        for (int u = 0; u < St::N; ++u) start[u] = start_at(t * KT + St::row_of(wave, lane, u));
+        if (threadIdx.x < KT) start1 = start_at(t * KT + threadIdx.x);
+    };
+    auto store = [&](int buf) {
+        auto keep = [&](int u) { return start[u] != -INFINITY; };
+        sk.store(lds + buf * 2 * St::kBytes, wave, lane, keep);
+        sv.store(lds + (buf * 2 + 1) * St::kBytes, wave, lane, keep);
+        if (threadIdx.x < KT) starts[buf][threadIdx.x] = start1;
+    };
+
+    if (t0 < t1) {
+        load(t0);
+        store(0);
+    }
+    __syncthreads();
+    for (int64_t t = t0; t < t1; ++t) {
+        const int buf = (int)(t - t0) & 1;
+        const bool more = t + 1 < t1;
+        if (more) load(t + 1);
+        const lds_t* kt = lds + buf * 2 * St::kBytes;
+        const lds_t* vt = kt + St::kBytes;
+        f16 s[NK];
+        const bool plain = !a.bias && (t + 1) * KT <= n;
+#pragma unroll
+        for (int k = 0; k < NK; ++k) {
+            if (plain) {
+#pragma unroll
+                for (int r = 0; r < 16; ++r) s[k][r] = 0.0f;
+            } else {
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    const f4 v = *(const f4*)&starts[buf][32 * k + 8 * q + 4 * (lane / 32)];
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) s[k][4 * q + r] = v[r];
+                }
+            }
+            s[k] = Tile::scores(kt, ln, k, qf, s[k]);
         }
-        const float m1 = fmaxf(m, block_max(t, red)), ms = m1 == -INFINITY ? 0.0f : m1;
-        const float e = exp2f(t - ms), f = exp2f(m - ms);
-        p[threadIdx.x] = e;
-        l = l * f + e;
-        o *= f;
-        m = m1;
+        float top = s[0][0];
+#pragma unroll
+        for (int k = 0; k < NK; ++k)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) top = fmaxf(top, s[k][r]);
+        top = fmaxf(top, other_half(top)) * scale2;
+        // The reference m follows the maximum only where it grew by more than
+        // 2^8: p stays below 2^8 and the accumulators are rarely rescaled.
+        if (__any(top > m + 8.0f)) {
+            const float m1 = fmaxf(m, top), f = __builtin_amdgcn_exp2f(m - (m1 == -INFINITY ? 0.0f : m1));
+            m = m1;
+            l *= f;
+#pragma unroll
+            for (int d = 0; d < DP / 32; ++d)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) o[d][r] *= f;
+        }
+        const float neg = m == -INFINITY ? 0.0f : -m;
+#pragma unroll
+        for (int k = 0; k < NK; ++k) {
+#pragma unroll
+            for (int r = 0; r < 16; ++r) {
+                s[k][r] = __builtin_amdgcn_exp2f(fmaf(s[k][r], scale2, neg));
+                l += s[k][r];
+            }
+            Tile::values(vt, ln, k, s[k], o);
+        }
+        if (more) store(buf ^ 1);
         __syncthreads();
-        if (d < a.dim)
-            for (int u = slice; u < kTile && j0 + u < n; u += kTile / dp)
-                if (p[u] != 0.0f) o = fmaf(p[u], (float)v[(j0 + u) * a.v.st + d], o);
     }
-    acc[threadIdx.x] = o;
-    __syncthreads();
-    for (int w = 32; w > 0; w >>= 1) l += __shfl_xor(l, w);
-    __syncthreads();
-    if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = l;
-    __syncthreads();
-    l = red[0] + red[1] + red[2] + red[3];
-    if (threadIdx.x < a.dim) {
-        float s = 0.0f;
-        for (int u = threadIdx.x; u < kTile; u += dp) s += acc[u];
-        T* out = (T*)a.out.p + b * a.out.sb + i * a.out.st + h * a.out.sh;
-        out[threadIdx.x] = (T)(l == 0.0f ? 0.0f : s / l);
+    l += other_half(l);
+    if (!live) return;
+    const int64_t stat = ((int64_t)b * a.heads + h) * a.queries + i;
+    if (c.splits > 1) {
+        const int64_t all = (int64_t)a.batch * a.kv_heads * c.rows;
+        const int64_t at = split * all + (int64_t)bh * c.rows + row;
+        store_column<float, DP>(c.part + at * a.dim, o, 1.0f, a.dim, a.dim % 4 == 0, lane);
+        if (lane < 32) {
+            c.stat[2 * at] = m;
+            c.stat[2 * at + 1] = l;
+        }
+        return;
     }
-    if (a.stats && threadIdx.x == 0) {
-        float* st = a.stats + ((int64_t)blockIdx.y * a.queries + i) * 2;
+    const float inv = l == 0.0f ? 0.0f : 1.0f / l;
+    store_column<T, DP>((T*)a.out.p + b * a.out.sb + i * a.out.st + h * a.out.sh, o, inv, a.dim, c.wide_o, lane);
+    if (a.stats && lane < 32) {
+        a.stats[2 * stat] = m;
+        a.stats[2 * stat + 1] = l;
+    }
+    if constexpr (std::is_same<T, __bf16>::value) {
+        if (a.low.p) {  // what rounding took from out
+#pragma unroll
+            for (int d = 0; d < DP / 32; ++d)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) {
+                    const float v = o[d][r] * inv;
+                    o[d][r] = v - (float)(__bf16)v;
+                }
+            store_column<T, DP>((T*)a.low.p + b * a.low.sb + i * a.low.st + h * a.low.sh, o, 1.0f, a.dim, c.wide_low, lane);
+        }
+    }
+}
+
+// Joins the parts of each row, in the order of the keys.  One wave a row.
+// grid: ceil(rows of all items / 4).
+template <typename T>
+__global__ __launch_bounds__(kAttendThreads) void k_attend_join(AttendArgs a, Cut c) {
+    const int lane = threadIdx.x % kWave, G = a.heads / a.kv_heads;
+    const int64_t all = (int64_t)a.batch * a.kv_heads * c.rows;
+    const int64_t at = (int64_t)blockIdx.x * kAttendWaves + threadIdx.x / kWave;
+    if (at >= all) return;
+    float m = -INFINITY;
+    for (int s = 0; s < c.splits; ++s) m = fmaxf(m, c.stat[2 * (s * all + at)]);
+    const float ms = m == -INFINITY ? 0.0f : m;
+    float l = 0.0f, o0 = 0.0f, o1 = 0.0f;
+    const bool d0 = lane < a.dim, d1 = lane + 64 < a.dim;
+#pragma unroll 4
+    for (int s = 0; s < c.splits; ++s) {
+        const float f = __builtin_amdgcn_exp2f(c.stat[2 * (s * all + at)] - ms);
+        const float* p = c.part + (s * all + at) * a.dim;
+        l = fmaf(f, c.stat[2 * (s * all + at) + 1], l);
+        if (d0) o0 = fmaf(f, p[lane], o0);
+        if (d1) o1 = fmaf(f, p[lane + 64], o1);
+    }
+    const float inv = l == 0.0f ? 0.0f : 1.0f / l;
+    const int64_t row = at % c.rows, bh = at / c.rows, b = bh / a.kv_heads, i = row / G;
+    const int h = (int)(bh % a.kv_heads) * G + (int)(row % G);
+    T* out = (T*)a.out.p + b * a.out.sb + i * a.out.st + h * a.out.sh;
+    o0 *= inv;
+    o1 *= inv;
+    if (d0) out[lane] = (T)o0;
+    if (d1) out[lane + 64] = (T)o1;
+    if (a.low.p) {
+        T* low = (T*)a.low.p + b * a.low.sb + i * a.low.st + h * a.low.sh;
+        if (d0) low[lane] = (T)(o0 - (float)(T)o0);
+        if (d1) low[lane + 64] = (T)(o1 - (float)(T)o1);
+    }
+    if (a.stats && lane == 0) {
+        float* st = a.stats + 2 * ((b * a.heads + h) * a.queries + i);
         st[0] = m;
         st[1] = l;
     }
 }
 
+Cut cut_of(const AttendArgs& a) {
+    Cut c{};
+    c.rows = a.queries * (a.heads / a.kv_heads);
+    c.row_blocks = (c.rows + kRows - 1) / kRows;
+    const int64_t blocks = c.row_blocks * a.batch * a.kv_heads;
+    const int KT = a.bf16 ? kKeys<__bf16> : kKeys<float>;
+    const int64_t tiles = (a.keys + KT - 1) / KT;
+    // Two workgroups a CU where there are keys enough for a part of four tiles each.
+    const int64_t want = blocks > 0 ? (2 * 256 + blocks - 1) / blocks : 1;
+    c.splits = (int32_t)std::max<int64_t>(1, std::min<int64_t>({want, tiles / 4, 256}));
+    c.items = blocks * c.splits;
+    return c;
+}
+
+size_t round256(size_t n) { return (n + 255) / 256 * 256; }
+size_t part_bytes(const AttendArgs& a, const Cut& c) {
+    return round256((size_t)c.splits * a.batch * a.kv_heads * c.rows * a.dim * sizeof(float));
+}
+
+template <typename T, int DP>
+void launch(const AttendArgs& a, const Cut& c) {
+    hipLaunchKernelGGL((k_attend<T, DP>), dim3(xcd_grid(c.items)), dim3(kAttendThreads), 0, a.stream, a, c);
+}
+
+template <typename T>
+void launch_dim(const AttendArgs& a, const Cut& c) {
+    if (a.dim <= 32) launch<T, 32>(a, c);
+    else if (a.dim <= 64) launch<T, 64>(a, c);
+    else if (a.dim <= 96) launch<T, 96>(a, c);
+    else launch<T, 128>(a, c);
+}
+
 }  // namespace
 
-size_t attend_ws_bytes(const AttendArgs&) { return 0; }
+size_t attend_ws_bytes(const AttendArgs& a) {
+    const Cut c = cut_of(a);
+    if (c.splits == 1) return 0;
+    return part_bytes(a, c) + (size_t)c.splits * a.batch * a.kv_heads * c.rows * 2 * sizeof(float);
+}
 
-hipError_t launch_attend(const AttendArgs& a, void*) {
-    const dim3 grid((unsigned)a.queries, (unsigned)(a.batch * a.heads));
-    const int tk = timing_begin("attend", a.stream);
-    if (a.bf16) hipLaunchKernelGGL(k_attend<__bf16>, grid, dim3(kTile), 0, a.stream, a);
-    else hipLaunchKernelGGL(k_attend<float>, grid, dim3(kTile), 0, a.stream, a);
+hipError_t launch_attend(const AttendArgs& a, void* ws) {
+    Cut c = cut_of(a);
+    const size_t e = a.bf16 ? 2 : 4;
+    const int ch = a.bf16 ? 8 : 4;
+    c.wide_q = wide_rows(a.q, a.dim, ch, e);
+    c.wide_k = wide_rows(a.k, a.dim, ch, e);
+    c.wide_v = wide_rows(a.v, a.dim, ch, e);
+    c.wide_o = wide_rows(a.out, a.dim, 4, e);
+    c.wide_low = wide_rows(a.low, a.dim, 4, e);
+    if (c.splits > 1) {
+        c.part = (float*)ws;
+        c.stat = (float*)((char*)ws + part_bytes(a, c));
+    }
+    int tk = timing_begin("attend", a.stream);
+    if (a.bf16) launch_dim<__bf16>(a, c);
+    else launch_dim<float>(a, c);
+    timing_end(tk, a.stream);
+    const hipError_t err = hipGetLastError();
+    if (err != hipSuccess || c.splits == 1) return err;
+    const int64_t all = (int64_t)a.batch * a.kv_heads * c.rows;
+    tk = timing_begin("attend_join", a.stream);
+    const dim3 grid((unsigned)((all + kAttendWaves - 1) / kAttendWaves));
+    if (a.bf16) hipLaunchKernelGGL(k_attend_join<__bf16>, grid, dim3(kAttendThreads), 0, a.stream, a, c);
+    else hipLaunchKernelGGL(k_attend_join<float>, grid, dim3(kAttendThreads), 0, a.stream, a, c);
     timing_end(tk, a.stream);
     return hipGetLastError();
 }

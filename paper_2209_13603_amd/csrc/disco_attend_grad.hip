@@ -2,7 +2,11 @@
 //
 //   delta_i = dout_i . out_i,   ds_ij = p_ij (dout_i . v_j - delta_i)
 //   dq_i = scale sum_j ds_ij k_j,  dk_j = scale sum_i ds_ij q_i,  dv_j = sum_i p_ij dout_i
-// with p rebuilt from the row maximum and sum that the forward call left.
+// with p rebuilt from the row reference and sum that the forward call left.
+//
+// Two kernels, one with the rows and one with the keys in its columns, each of
+// which keeps its own sums in registers: seven products instead of the five
+// of a single pass, but no atomics, so that every run gives the same bits.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -15,127 +19,358 @@ namespace disco {
 
 namespace {
 
-constexpr int kTile = 256;
+constexpr int kCols = 32 * kAttendWaves;  // rows (dq) or keys (dk, dv) of a workgroup
+constexpr int kKeys = 32, kQueries = 32;  // keys, queries of a tile
 
-template <typename T>
-__device__ __forceinline__ float dot(const T* a, const T* b, int D) {
-    float s = 0.0f;
-    for (int d = 0; d < D; ++d) s = fmaf((float)a[d], (float)b[d], s);
-    return s;
-}
+struct GradCut {
+    int64_t rows, row_blocks, key_blocks, items_q, items_k;
+    int32_t splits_q, splits_k;
+    float *delta, *part;  // [batch][heads][queries]; [splits][...][dim]
+    uint8_t wide_q, wide_k, wide_v, wide_o, wide_low, wide_do, wide_dq, wide_dk, wide_dv;
+};
 
-// p_ij from the row's statistics; 0 where the row has no key.
-__device__ __forceinline__ float weight(float t, float m, float l) {
-    return l == 0.0f ? 0.0f : exp2f(t - m) / l;
-}
+// Workgroups of a CU that the registers are sized for.
+template <typename T, int DP>
+constexpr int kWorkgroups = std::is_same<T, float>::value ? (DP > 32 ? 1 : 2) : (DP > 96 ? 1 : 2);
 
-// One workgroup a query row; grid: (queries, batch * heads).
-template <typename T>
-__global__ __launch_bounds__(kTile) void k_attend_dq(AttendArgs a) {
-    __shared__ float s[kTile], acc[kTile];
-    const int64_t i = blockIdx.x;
-    const int b = blockIdx.y / a.heads, h = blockIdx.y % a.heads, hk = h / (a.heads / a.kv_heads);
-    const T* q = (const T*)a.q.p + b * a.q.sb + i * a.q.st + h * a.q.sh;
-    const T* o = (const T*)a.out.p + b * a.out.sb + i * a.out.st + h * a.out.sh;
-    const T* g = (const T*)a.dout.p + b * a.dout.sb + i * a.dout.st + h * a.dout.sh;
-    const T* k = (const T*)a.k.p + b * a.k.sb + hk * a.k.sh;
-    const T* v = (const T*)a.v.p + b * a.v.sb + hk * a.v.sh;
-    const float* st = a.stats + ((int64_t)blockIdx.y * a.queries + i) * 2;
-    const float m = st[0], l = st[1], delta = dot(g, o, a.dim);
-    const int64_t n = key_count(a, b);
-    const int dp = a.dim <= 32 ? 32 : a.dim <= 64 ? 64 : 128, d = threadIdx.x % dp, slice = threadIdx.x / dp;
-    float sum = 0.0f;
-    for (int64_t j0 = 0; j0 < n; j0 += kTile) {
-        const int64_t j = j0 + threadIdx.x;
-        float ds = 0.0f;
-        if (j < n) {
-            const float bias2 = key_bias2(a, b, j);
-            if (bias2 != -INFINITY)
-                ds = weight(fmaf(dot(q, k + j * a.k.st, a.dim), a.scale2, bias2), m, l) *
-                     (dot(g, v + j * a.v.st, a.dim) - delta);
-        }
-        __syncthreads();
-        s[threadIdx.x] = ds;
-        __syncthreads();
-        if (d < a.dim)
-            for (int u = slice; u < kTile && j0 + u < n; u += kTile / dp)
-                if (s[u] != 0.0f) sum = fmaf(s[u], (float)k[(j0 + u) * a.k.st + d], sum);
+// dq: each wave holds 32 rows; keys and values come in tiles as in the forward pass.
+template <typename T, int DP>
+__global__ __launch_bounds__(kAttendThreads, (kWorkgroups<T, DP>)) void k_attend_dq(AttendArgs a, GradCut c) {
+    typedef TileOf<T, DP> Tile;
+    constexpr int KT = kKeys;
+    typedef Stage<T, DP, KT> St;
+    __shared__ __align__(16) char smem[2 * 2 * St::kBytes];
+    __shared__ float starts[2][KT];
+    lds_t* lds = (lds_t*)smem;
+
+    const int64_t id = xcd_item(c.items_q);
+    if (id >= c.items_q) return;
+    const int split = (int)(id % c.splits_q);
+    const int64_t rb = id / c.splits_q % c.row_blocks;
+    const int bh = (int)(id / c.splits_q / c.row_blocks), b = bh / a.kv_heads, hk = bh % a.kv_heads;
+    const int wave = threadIdx.x / kWave, lane = threadIdx.x % kWave, G = a.heads / a.kv_heads;
+    const int64_t row = rb * kCols + wave * 32 + lane % 32;
+    const bool live = row < c.rows;
+    const int64_t i = live ? row / G : 0;
+    const int h = hk * G + (int)(live ? row % G : 0);
+    const T* kp = (const T*)a.k.p + b * a.k.sb + hk * a.k.sh;
+    const T* vp = (const T*)a.v.p + b * a.v.sb + hk * a.v.sh;
+    const int64_t n = key_count(a, b), tiles = (n + KT - 1) / KT;
+    const int64_t t0 = tiles * split / c.splits_q, t1 = tiles * (split + 1) / c.splits_q;
+
+    typename Tile::Frag qf[Tile::NS], gf[Tile::NS];
+    load_frags<T, DP>((const T*)a.dout.p + b * a.dout.sb + i * a.dout.st + h * a.dout.sh, a.dim, c.wide_do, live, lane, gf);
+    // delta from this lane's half of the entries and the other's
+    float delta = 0.0f;
+    auto add = [&](const Heads& t, bool wide) {
+        load_frags<T, DP>((const T*)t.p + b * t.sb + i * t.st + h * t.sh, a.dim, wide, live, lane, qf);
+#pragma unroll
+        for (int s = 0; s < Tile::NS; ++s)
+#pragma unroll
+            for (int j = 0; j < Tile::CH; ++j) delta = fmaf((float)gf[s][j], (float)qf[s][j], delta);
+    };
+    add(a.out, c.wide_o);
+    if (a.low.p) add(a.low, c.wide_low);
+    delta += other_half(delta);
+    load_frags<T, DP>((const T*)a.q.p + b * a.q.sb + i * a.q.st + h * a.q.sh, a.dim, c.wide_q, live, lane, qf);
+    if (a.scale2 < 0.0f)
+#pragma unroll
+        for (int s = 0; s < Tile::NS; ++s) qf[s] = -qf[s];
+    const int64_t at = ((int64_t)b * a.heads + h) * a.queries + i;
+    const float m = a.stats[2 * at], l = a.stats[2 * at + 1];
+    const float neg = l == 0.0f ? -INFINITY : -m, inv = l == 0.0f ? 0.0f : 1.0f / l;
+    if (split == 0 && live && lane < 32) c.delta[at] = delta;
+    const float scale2 = fabsf(a.scale2), inv_scale = 1.0f / fabsf(a.scale);
+    const typename Tile::Lane ln = Tile::lane_of(lane);
+
+    f16 dq[DP / 32];
+#pragma unroll
+    for (int d = 0; d < DP / 32; ++d)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) dq[d][r] = 0.0f;
+
+    St sk, sv;
+    float start[St::N], start1 = 0.0f;
+    auto load = [&](int64_t t) {
+        sk.load(kp, a.k.st, t * KT, n, a.dim, c.wide_k, wave, lane);
+        sv.load(vp, a.v.st, t * KT, n, a.dim, c.wide_v, wave, lane);
+        auto start_at = [&](int64_t j) {
+            return j >= n ? -INFINITY : a.bias ? start_of(a.bias[b * a.bias_sb + j], inv_scale) : 0.0f;
+        };
+#pragma unroll
+        for (int u = 0; u < St::N; ++u) start[u] = start_at(t * KT + St::row_of(wave, lane, u));
+        if (threadIdx.x < KT) start1 = start_at(t * KT + threadIdx.x);
+    };
+    auto store = [&](int buf) {
+        auto keep = [&](int u) { return start[u] != -INFINITY; };
+        sk.store(lds + buf * 2 * St::kBytes, wave, lane, keep);
+        sv.store(lds + (buf * 2 + 1) * St::kBytes, wave, lane, keep);
+        if (threadIdx.x < KT) starts[buf][threadIdx.x] = start1;
+    };
+    if (t0 < t1) {
+        load(t0);
+        store(0);
     }
-    acc[threadIdx.x] = sum;
     __syncthreads();
-    if (threadIdx.x < a.dim) {
-        float r = 0.0f;
-        for (int u = threadIdx.x; u < kTile; u += dp) r += acc[u];
-        ((T*)a.dq.p + b * a.dq.sb + i * a.dq.st + h * a.dq.sh)[threadIdx.x] = (T)(r * a.scale);
+    for (int64_t t = t0; t < t1; ++t) {
+        const int buf = (int)(t - t0) & 1;
+        const bool more = t + 1 < t1;
+        if (more) load(t + 1);
+        const lds_t* kt = lds + buf * 2 * St::kBytes;
+        const lds_t* vt = kt + St::kBytes;
+        f16 s, dp;
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            const f4 v = *(const f4*)&starts[buf][8 * q + 4 * (lane / 32)];
+#pragma unroll
+            for (int r = 0; r < 4; ++r) s[4 * q + r] = v[r], dp[4 * q + r] = 0.0f;
+        }
+        s = Tile::scores(kt, ln, 0, qf, s);
+        dp = Tile::scores(vt, ln, 0, gf, dp);
+#pragma unroll
+        for (int r = 0; r < 16; ++r) s[r] = __builtin_amdgcn_exp2f(fmaf(s[r], scale2, neg)) * (dp[r] - delta);
+        Tile::values(kt, ln, 0, s, dq);
+        if (more) store(buf ^ 1);
+        __syncthreads();
+    }
+    if (!live) return;
+    const float f = inv * a.scale;
+    if (c.splits_q > 1) {
+        const int64_t all = (int64_t)a.batch * a.kv_heads * c.rows;
+        store_column<float, DP>(c.part + (split * all + (int64_t)bh * c.rows + row) * a.dim, dq, f, a.dim, a.dim % 4 == 0, lane);
+    } else {
+        store_column<T, DP>((T*)a.dq.p + b * a.dq.sb + i * a.dq.st + h * a.dq.sh, dq, f, a.dim, c.wide_dq, lane);
     }
 }
 
-// One workgroup a key; grid: (keys, batch * kv_heads).
-template <typename T>
-__global__ __launch_bounds__(kTile) void k_attend_dkv(AttendArgs a) {
-    __shared__ float s[kTile], w[kTile], acc[2][kTile];
-    const int64_t j = blockIdx.x;
-    const int b = blockIdx.y / a.kv_heads, hk = blockIdx.y % a.kv_heads, group = a.heads / a.kv_heads;
-    const T* k = (const T*)a.k.p + b * a.k.sb + j * a.k.st + hk * a.k.sh;
-    const T* v = (const T*)a.v.p + b * a.v.sb + j * a.v.st + hk * a.v.sh;
-    const float bias2 = key_bias2(a, b, j);
-    const bool live = j < key_count(a, b) && bias2 != -INFINITY;
-    const int dp = a.dim <= 32 ? 32 : a.dim <= 64 ? 64 : 128, d = threadIdx.x % dp, slice = threadIdx.x / dp;
-    float dk = 0.0f, dv = 0.0f;
-    for (int h = hk * group; live && h < (hk + 1) * group; ++h) {
-        const T* q = (const T*)a.q.p + b * a.q.sb + h * a.q.sh;
-        const T* o = (const T*)a.out.p + b * a.out.sb + h * a.out.sh;
-        const T* g = (const T*)a.dout.p + b * a.dout.sb + h * a.dout.sh;
-        const float* st = a.stats + (int64_t)(b * a.heads + h) * a.queries * 2;
-        for (int64_t i0 = 0; i0 < a.queries; i0 += kTile) {
-            const int64_t i = i0 + threadIdx.x;
-            float p = 0.0f, ds = 0.0f;
-            if (i < a.queries) {
-                p = weight(fmaf(dot(q + i * a.q.st, k, a.dim), a.scale2, bias2), st[2 * i], st[2 * i + 1]);
-                ds = p * (dot(g + i * a.dout.st, v, a.dim) - dot(g + i * a.dout.st, o + i * a.out.st, a.dim));
+// dk, dv: each wave holds 32 keys; queries and output gradients of every head
+// of the group come in tiles.
+template <typename T, int DP>
+__global__ __launch_bounds__(kAttendThreads, (kWorkgroups<T, DP>)) void k_attend_dkv(AttendArgs a, GradCut c) {
+    typedef TileOf<T, DP> Tile;
+    constexpr int QT = kQueries;
+    typedef Stage<T, DP, QT> St;
+    __shared__ __align__(16) char smem[2 * 2 * St::kBytes];
+    __shared__ float row_c[2][3][QT];  // -reference, 1 / sum, delta of the tile's rows
+    lds_t* lds = (lds_t*)smem;
+
+    const int64_t id = xcd_item(c.items_k);
+    if (id >= c.items_k) return;
+    const int split = (int)(id % c.splits_k);
+    const int64_t kb = id / c.splits_k % c.key_blocks;
+    const int bh = (int)(id / c.splits_k / c.key_blocks), b = bh / a.kv_heads, hk = bh % a.kv_heads;
+    const int wave = threadIdx.x / kWave, lane = threadIdx.x % kWave, G = a.heads / a.kv_heads;
+    const int64_t j = kb * kCols + wave * 32 + lane % 32, n = key_count(a, b);
+    const float scale2 = fabsf(a.scale2);
+    const float start = j >= n ? -INFINITY : a.bias ? start_of(a.bias[b * a.bias_sb + j], 1.0f / fabsf(a.scale)) : 0.0f;
+    const bool live = start != -INFINITY;
+    const int64_t jr = live ? j : 0;
+
+    typename Tile::Frag kf[Tile::NS], vf[Tile::NS];
+    load_frags<T, DP>((const T*)a.k.p + b * a.k.sb + jr * a.k.st + hk * a.k.sh, a.dim, c.wide_k, live, lane, kf);
+    load_frags<T, DP>((const T*)a.v.p + b * a.v.sb + jr * a.v.st + hk * a.v.sh, a.dim, c.wide_v, live, lane, vf);
+    if (a.scale2 < 0.0f)
+#pragma unroll
+        for (int s = 0; s < Tile::NS; ++s) kf[s] = -kf[s];
+    const typename Tile::Lane ln = Tile::lane_of(lane);
+    f16 dk[DP / 32], dv[DP / 32];
+#pragma unroll
+    for (int d = 0; d < DP / 32; ++d)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) dk[d][r] = dv[d][r] = 0.0f;
+
+    const int64_t tiles = (a.queries + QT - 1) / QT, steps = kb * kCols < n ? tiles * G : 0;
+    const int64_t t0 = steps * split / c.splits_k, t1 = steps * (split + 1) / c.splits_k;
+    St sq, sg;
+    float r0 = 0.0f, r1 = 0.0f, r2 = 0.0f;
+    int64_t left = 0;  // rows of the staged tile that exist
+    auto load = [&](int64_t t) {
+        const int h = hk * G + (int)(t / tiles);
+        const int64_t i0 = t % tiles * QT;
+        sq.load((const T*)a.q.p + b * a.q.sb + h * a.q.sh, a.q.st, i0, a.queries, a.dim, c.wide_q, wave, lane);
+        sg.load((const T*)a.dout.p + b * a.dout.sb + h * a.dout.sh, a.dout.st, i0, a.queries, a.dim, c.wide_do, wave, lane);
+        left = a.queries - i0;
+        if (threadIdx.x < QT) {
+            r0 = -INFINITY;
+            r1 = r2 = 0.0f;
+            if (threadIdx.x < left) {
+                const int64_t at = ((int64_t)b * a.heads + h) * a.queries + i0 + threadIdx.x;
+                const float m = a.stats[2 * at], l = a.stats[2 * at + 1];
+                r2 = c.delta[at];
+                if (l != 0.0f) r0 = -m, r1 = 1.0f / l;
             }
-            __syncthreads();
-            s[threadIdx.x] = ds;
-            w[threadIdx.x] = p;
-            __syncthreads();
-            if (d < a.dim)
-                for (int u = slice; u < kTile && i0 + u < a.queries; u += kTile / dp) {
-                    dk = fmaf(s[u], (float)q[(i0 + u) * a.q.st + d], dk);
-                    dv = fmaf(w[u], (float)g[(i0 + u) * a.dout.st + d], dv);
-                }
         }
+    };
+    auto store = [&](int buf) {
+        auto keep = [&](int u) { return St::row_of(wave, lane, u) < left; };
+        sq.store(lds + buf * 2 * St::kBytes, wave, lane, keep);
+        sg.store(lds + (buf * 2 + 1) * St::kBytes, wave, lane, keep);
+        if (threadIdx.x < QT) {
+            row_c[buf][0][threadIdx.x] = r0;
+            row_c[buf][1][threadIdx.x] = r1;
+            row_c[buf][2][threadIdx.x] = r2;
+        }
+    };
+    if (t0 < t1) {
+        load(t0);
+        store(0);
     }
-    acc[0][threadIdx.x] = dk;
-    acc[1][threadIdx.x] = dv;
     __syncthreads();
-    if (threadIdx.x < a.dim) {
-        float rk = 0.0f, rv = 0.0f;
-        for (int u = threadIdx.x; u < kTile; u += dp) rk += acc[0][u], rv += acc[1][u];
-        ((T*)a.dk.p + b * a.dk.sb + j * a.dk.st + hk * a.dk.sh)[threadIdx.x] = (T)(rk * a.scale);
-        ((T*)a.dv.p + b * a.dv.sb + j * a.dv.st + hk * a.dv.sh)[threadIdx.x] = (T)rv;
+    for (int64_t t = t0; t < t1; ++t) {
+        const int buf = (int)(t - t0) & 1;
+        const bool more = t + 1 < t1;
+        if (more) load(t + 1);
+        const lds_t* qt = lds + buf * 2 * St::kBytes;
+        const lds_t* gt = qt + St::kBytes;
+        f16 s, dp;
+#pragma unroll
+        for (int r = 0; r < 16; ++r) s[r] = start, dp[r] = 0.0f;
+        s = Tile::scores(qt, ln, 0, kf, s);
+        dp = Tile::scores(gt, ln, 0, vf, dp);
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            const int at = 8 * q + 4 * (lane / 32);
+            const f4 neg = *(const f4*)&row_c[buf][0][at], inv = *(const f4*)&row_c[buf][1][at];
+            const f4 delta = *(const f4*)&row_c[buf][2][at];
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                const float p = __builtin_amdgcn_exp2f(fmaf(s[4 * q + r], scale2, neg[r])) * inv[r];
+                s[4 * q + r] = p;
+                dp[4 * q + r] = p * (dp[4 * q + r] - delta[r]);
+            }
+        }
+        Tile::values(gt, ln, 0, s, dv);
+        Tile::values(qt, ln, 0, dp, dk);
+        if (more) store(buf ^ 1);
+        __syncthreads();
+    }
+    if (!live)  // nothing of a key that is taken out
+#pragma unroll
+        for (int d = 0; d < DP / 32; ++d)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) dk[d][r] = dv[d][r] = 0.0f;
+    if (j >= a.keys) return;
+    if (c.splits_k > 1) {
+        const int64_t all = (int64_t)a.batch * a.kv_heads * a.keys, at = split * 2 * all + (int64_t)bh * a.keys + j;
+        store_column<float, DP>(c.part + at * a.dim, dk, a.scale, a.dim, a.dim % 4 == 0, lane);
+        store_column<float, DP>(c.part + (at + all) * a.dim, dv, 1.0f, a.dim, a.dim % 4 == 0, lane);
+    } else {
+        store_column<T, DP>((T*)a.dk.p + b * a.dk.sb + j * a.dk.st + hk * a.dk.sh, dk, a.scale, a.dim, c.wide_dk, lane);
+        store_column<T, DP>((T*)a.dv.p + b * a.dv.sb + j * a.dv.st + hk * a.dv.sh, dv, 1.0f, a.dim, c.wide_dv, lane);
     }
 }
 
+// Adds the parts of each row in their order: entry e of part s of row r of
+// matrix blockIdx.y stands at part[(s * matrices + blockIdx.y) * all * dim + r * dim + e].
+// Rows are (batch, kv head, row), a row being (token, head of the group).
 template <typename T>
-hipError_t launch(const AttendArgs& a) {
-    int tk = timing_begin("attend_dq", a.stream);
-    if (a.queries > 0)
-        hipLaunchKernelGGL(k_attend_dq<T>, dim3((unsigned)a.queries, (unsigned)(a.batch * a.heads)), dim3(kTile), 0,
-                           a.stream, a);
-    timing_end(tk, a.stream);
-    const hipError_t e = hipGetLastError();
-    if (e != hipSuccess || a.keys == 0) return e;
-    tk = timing_begin("attend_dkv", a.stream);
-    hipLaunchKernelGGL(k_attend_dkv<T>, dim3((unsigned)a.keys, (unsigned)(a.batch * a.kv_heads)), dim3(kTile), 0,
-                       a.stream, a);
-    timing_end(tk, a.stream);
-    return hipGetLastError();
+__global__ __launch_bounds__(256) void k_attend_sum(const float* __restrict__ part, int splits, int64_t rows,
+                                                    int kv_heads, int G, int dim, int64_t all, Heads o0, Heads o1) {
+    const int64_t e = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    if (e >= all * dim) return;
+    const float* p = part + (int64_t)blockIdx.y * all * dim + e;
+    const int64_t step = (int64_t)gridDim.y * all * dim;
+    float v = 0.0f;
+#pragma unroll 4
+    for (int s = 0; s < splits; ++s) v += p[s * step];
+    const int64_t r = e / dim, bh = r / rows, row = r % rows;
+    const Heads& o = blockIdx.y ? o1 : o0;
+    T* out = (T*)o.p + bh / kv_heads * o.sb + row / G * o.st + (bh % kv_heads * G + row % G) * o.sh;
+    out[e % dim] = (T)v;
+}
+
+int32_t parts(int64_t blocks, int64_t steps, int64_t least) {
+    const int64_t want = blocks > 0 ? (2 * 256 + blocks - 1) / blocks : 1;
+    return (int32_t)std::max<int64_t>(1, std::min<int64_t>({want, steps / least, 256}));
+}
+
+GradCut cut_of(const AttendArgs& a) {
+    GradCut c{};
+    const int G = a.heads / a.kv_heads;
+    c.rows = a.queries * G;
+    c.row_blocks = (c.rows + kCols - 1) / kCols;
+    c.key_blocks = (a.keys + kCols - 1) / kCols;
+    const int64_t bq = c.row_blocks * a.batch * a.kv_heads, bk = c.key_blocks * a.batch * a.kv_heads;
+    // Parts of at least eight tiles, as many as give every CU two workgroups.
+    c.splits_q = parts(bq, (a.keys + kKeys - 1) / kKeys, 8);
+    c.splits_k = parts(bk, (a.queries + kQueries - 1) / kQueries * G, 8);
+    c.items_q = bq * c.splits_q;
+    c.items_k = bk * c.splits_k;
+    return c;
+}
+
+size_t round256(size_t n) { return (n + 255) / 256 * 256; }
+size_t delta_bytes(const AttendArgs& a) { return round256((size_t)a.batch * a.heads * a.queries * sizeof(float)); }
+
+template <typename T, int DP>
+void launch_dq(const AttendArgs& a, const GradCut& c) {
+    hipLaunchKernelGGL((k_attend_dq<T, DP>), dim3(xcd_grid(c.items_q)), dim3(kAttendThreads), 0, a.stream, a, c);
+}
+template <typename T, int DP>
+void launch_dkv(const AttendArgs& a, const GradCut& c) {
+    hipLaunchKernelGGL((k_attend_dkv<T, DP>), dim3(xcd_grid(c.items_k)), dim3(kAttendThreads), 0, a.stream, a, c);
+}
+
+template <typename T>
+hipError_t run(const AttendArgs& a, const GradCut& c) {
+    const int G = a.heads / a.kv_heads;
+    hipError_t e = hipSuccess;
+    auto sum = [&](int splits, int64_t rows, int g, int matrices, const Heads& o0, const Heads& o1) {
+        const int64_t all = (int64_t)a.batch * a.kv_heads * rows;
+        const int tk = timing_begin("attend_sum", a.stream);
+        hipLaunchKernelGGL(k_attend_sum<T>, dim3((unsigned)((all * a.dim + 255) / 256), (unsigned)matrices), dim3(256), 0,
+                           a.stream, c.part, splits, rows, a.kv_heads, g, a.dim, all, o0, o1);
+        timing_end(tk, a.stream);
+        return hipGetLastError();
+    };
+    if (c.items_q > 0) {
+        const int tk = timing_begin("attend_dq", a.stream);
+        if (a.dim <= 32) launch_dq<T, 32>(a, c);
+        else if (a.dim <= 64) launch_dq<T, 64>(a, c);
+        else if (a.dim <= 96) launch_dq<T, 96>(a, c);
+        else launch_dq<T, 128>(a, c);
+        timing_end(tk, a.stream);
+        e = hipGetLastError();
+        if (e == hipSuccess && c.splits_q > 1) e = sum(c.splits_q, c.rows, G, 1, a.dq, a.dq);
+    }
+    if (e == hipSuccess && c.items_k > 0) {
+        const int tk = timing_begin("attend_dkv", a.stream);
+        if (a.dim <= 32) launch_dkv<T, 32>(a, c);
+        else if (a.dim <= 64) launch_dkv<T, 64>(a, c);
+        else if (a.dim <= 96) launch_dkv<T, 96>(a, c);
+        else launch_dkv<T, 128>(a, c);
+        timing_end(tk, a.stream);
+        e = hipGetLastError();
+        if (e == hipSuccess && c.splits_k > 1) e = sum(c.splits_k, a.keys, 1, 2, a.dk, a.dv);
+    }
+    return e;
 }
 
 }  // namespace
 
-size_t attend_grad_ws_bytes(const AttendArgs&) { return 0; }
+size_t attend_grad_ws_bytes(const AttendArgs& a) {
+    const GradCut c = cut_of(a);
+    const size_t row = (size_t)a.batch * a.kv_heads * a.dim * sizeof(float);
+    const size_t q = c.splits_q > 1 ? c.splits_q * row * c.rows : 0, k = c.splits_k > 1 ? c.splits_k * 2 * row * a.keys : 0;
+    return delta_bytes(a) + std::max(q, k);
+}
 
-hipError_t launch_attend_grad(const AttendArgs& a, void*) { return a.bf16 ? launch<__bf16>(a) : launch<float>(a); }
+hipError_t launch_attend_grad(const AttendArgs& a, void* ws) {
+    GradCut c = cut_of(a);
+    const size_t e = a.bf16 ? 2 : 4;
+    const int ch = a.bf16 ? 8 : 4;
+    c.wide_q = wide_rows(a.q, a.dim, ch, e);
+    c.wide_k = wide_rows(a.k, a.dim, ch, e);
+    c.wide_v = wide_rows(a.v, a.dim, ch, e);
+    c.wide_o = wide_rows(a.out, a.dim, ch, e);
+    c.wide_low = wide_rows(a.low, a.dim, ch, e);
+    c.wide_do = wide_rows(a.dout, a.dim, ch, e);
+    c.wide_dq = wide_rows(a.dq, a.dim, 4, e);
+    c.wide_dk = wide_rows(a.dk, a.dim, 4, e);
+    c.wide_dv = wide_rows(a.dv, a.dim, 4, e);
+    c.delta = (float*)ws;
+    c.part = (float*)((char*)ws + delta_bytes(a));
+    return a.bf16 ? run<__bf16>(a, c) : run<float>(a, c);
+}
 
 }  // namespace disco

@@ -41,6 +41,7 @@ hipError_t launch_rotate_grad(const RotateArgs& a, float* ws);
 // ---- cross attention (disco_attend.hip, disco_attend_grad.hip) ---------------
 struct AttendArgs {
     Heads q, k, v, out, dout, dq, dk, dv;
+    Heads low;  // bf16: what rounding took from out, kept for the gradients
     const float* bias = nullptr;
     int64_t bias_sb = 0;
     const int32_t* lengths = nullptr;

@@ -477,7 +477,7 @@ disco_status_t disco_cross_attention_workspace(const disco_heads_t* q, const dis
 
 disco_status_t disco_cross_attention(const disco_heads_t* q, const disco_heads_t* k, const disco_heads_t* v,
                                      const disco_attention_t* options, disco_heads_t* out, float* stats,
-                                     void* workspace, size_t workspace_bytes, hipStream_t stream) {
+                                     disco_heads_t* low, void* workspace, size_t workspace_bytes, hipStream_t stream) {
     return guard([&] {
         TraceRange range("disco_cross_attention");
         if (!v) refuse(DISCO_ERR_INVALID_ARGUMENT, "v is NULL");
@@ -487,6 +487,15 @@ disco_status_t disco_cross_attention(const disco_heads_t* q, const disco_heads_t
         check_same(q, "q", out, "out");
         for (auto& t : {std::make_pair(q, "q"), std::make_pair(k, "k"), std::make_pair(v, "v")})
             check_apart(out, "out", t.first, t.second);
+        if (low) {
+            if (!a.bf16) refuse(DISCO_ERR_DTYPE, "low is for bf16");
+            check_output(low, "low");
+            check_same(q, "q", low, "low");
+            for (auto& t : {std::make_pair(q, "q"), std::make_pair(k, "k"), std::make_pair(v, "v"),
+                            std::make_pair((const disco_heads_t*)out, "out")})
+                check_apart(low, "low", t.first, t.second);
+            a.low = heads_of(low);
+        }
         if (empty(*q)) return;
         a.out = heads_of(out);
         a.stats = stats;
@@ -494,6 +503,7 @@ disco_status_t disco_cross_attention(const disco_heads_t* q, const disco_heads_t
         Device d;
         take_attend(&d, a, q, k);
         d.take(out->data, "out");
+        d.take(a.low.p, "low");
         d.take(stats, "stats");
         const size_t need = attend_ws_bytes(a);
         if (need && workspace) d.take(workspace, "workspace");
@@ -506,7 +516,7 @@ disco_status_t disco_cross_attention(const disco_heads_t* q, const disco_heads_t
 disco_status_t disco_cross_attention_backward(const disco_heads_t* q, const disco_heads_t* k,
                                               const disco_heads_t* v, const disco_attention_t* options,
                                               const disco_heads_t* out, const float* stats,
-                                              const disco_heads_t* dout, disco_heads_t* dq, disco_heads_t* dk,
+                                              const disco_heads_t* low, const disco_heads_t* dout, disco_heads_t* dq, disco_heads_t* dk,
                                               disco_heads_t* dv, void* workspace, size_t workspace_bytes,
                                               hipStream_t stream) {
     return guard([&] {
@@ -518,12 +528,19 @@ disco_status_t disco_cross_attention_backward(const disco_heads_t* q, const disc
         check_heads(dout, "dout");
         check_same(q, "q", out, "out");
         check_same(q, "q", dout, "dout");
+        if (low) {
+            if (!a.bf16) refuse(DISCO_ERR_DTYPE, "low is for bf16");
+            check_heads(low, "low");
+            check_same(q, "q", low, "low");
+            a.low = heads_of(low);
+        }
         const std::pair<disco_heads_t*, const char*> outs[] = {{dq, "dq"}, {dk, "dk"}, {dv, "dv"}};
         const std::pair<const disco_heads_t*, const char*> ins[] = {{q, "q"}, {k, "k"}, {v, "v"}, {out, "out"}, {dout, "dout"}};
         for (int i = 0; i < 3; ++i) {
             check_output(outs[i].first, outs[i].second);
             check_same(outs[i].first, outs[i].second, i == 0 ? q : k, i == 0 ? "q" : "k");
             for (const auto& in : ins) check_apart(outs[i].first, outs[i].second, in.first, in.second);
+            if (low) check_apart(outs[i].first, outs[i].second, low, "low");
             for (int j = 0; j < i; ++j) check_apart(outs[i].first, outs[i].second, outs[j].first, outs[j].second);
         }
         if (empty(*q) && empty(*k)) return;
@@ -539,6 +556,7 @@ disco_status_t disco_cross_attention_backward(const disco_heads_t* q, const disc
         take_attend(&d, a, q, k);
         if (!empty(*q)) {
             d.take(out->data, "out");
+            d.take(a.low.p, "low");
             d.take(dout->data, "dout");
             d.take(dq->data, "dq");
             d.take(stats, "stats");

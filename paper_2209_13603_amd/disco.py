@@ -201,8 +201,8 @@ def library(path: str = None) -> ctypes.CDLL:
         "disco_norm_rotate": [H, I32, T, ctypes.c_double, R, H, V],
         "disco_norm_rotate_backward": [H, I32, T, ctypes.c_double, R, H, H, T, V, Z, V],
         "disco_norm_rotate_workspace": [H, T, S],
-        "disco_cross_attention": [H, H, H, A, H, V, V, Z, V],
-        "disco_cross_attention_backward": [H, H, H, A, H, V, H, H, H, H, V, Z, V],
+        "disco_cross_attention": [H, H, H, A, H, V, H, V, Z, V],
+        "disco_cross_attention_backward": [H, H, H, A, H, V, H, H, H, H, H, V, Z, V],
         "disco_cross_attention_workspace": [H, H, I32, S],
         # the tensor arrays of many gradients come as addresses
         "disco_gradient_clip": [I32, V, V, ctypes.c_double, ctypes.c_double, V, V, Z, V],

@@ -1,0 +1,340 @@
+"""Cross attention and its gradients through the Python entry points against the
+definition in 64 bits, at the sizes, types, strides and masks where tiles, splits and
+masks can go wrong.
+
+Tolerances, in the 2-norm over each output.  Rounding to bf16 has a relative error of at most 2^-8, and of
+2^-8 / sqrt(3) times 0.735 (the mean of 1 / mantissa) in the mean square.  An output is rounded once, and each of
+the terms that it sums (p v, ds k, ds q, p dout) carries the rounding of its p or ds, independent of the
+others', so that the error is 0.42 * 2^-8 * sqrt(want^2 + sum of the terms' squares); the tests allow 0.75 * 2^-8 of
+that, where the sum of squares comes from the definition too (terms may cancel).  fp32: sums of up to 2048 products
+of relative error 2^-24 each, scores of up to about 10 whose exponential turns an absolute error into a relative
+one: 1e-5 of the same.
+"""
+import math
+
+import pytest
+
+pytestmark = pytest.mark.gpu
+
+TOL = {"bf16": 0.75 * 2.0 ** -8, "fp32": 1e-5}
+
+
+def _dt(name):
+    import torch
+    return {"bf16": torch.bfloat16, "fp32": torch.float32}[name]
+
+
+def _exact(q, k, v, dout, bias, lengths, scale):
+    """Definition on the CPU in fp64, on the keys that the mask leaves: (out, dq, dk, dv), each with the sum of its
+    terms' squares."""
+    import torch
+    B, Sq, H, D = q.shape
+    Sk, Hk = k.shape[1:3]
+    q, k, v, dout = (t.detach().cpu().double() for t in (q, k, v, dout))
+    out, dq = torch.zeros(B, Sq, H, D, dtype=torch.float64), torch.zeros(B, Sq, H, D, dtype=torch.float64)
+    dk, dv = torch.zeros(B, Sk, Hk, D, dtype=torch.float64), torch.zeros(B, Sk, Hk, D, dtype=torch.float64)
+    out2, dq2, dk2, dv2 = (torch.zeros_like(t) for t in (out, dq, dk, dv))
+    for b in range(B):
+        n = Sk if lengths is None else max(0, min(Sk, int(lengths[b])))
+        keep = torch.arange(n)
+        if bias is not None:
+            bb = bias.cpu().double()
+            bb = (bb if bb.dim() == 2 else bb[None]).expand(B, Sk)[b]
+            keep = keep[bb[:n] != -math.inf]
+        if keep.numel() == 0 or Sq == 0:
+            continue
+        for h in range(H):
+            hk = h // (H // Hk)
+            kk, vv = k[b, keep, hk], v[b, keep, hk]
+            s = q[b, :, h] @ kk.t() * scale
+            if bias is not None:
+                s = s + bb[keep]
+            p = torch.softmax(s, 1)
+            o = p @ vv
+            out[b, :, h] = o
+            g = dout[b, :, h]
+            ds = p * (g @ vv.t() - (g * o).sum(1, keepdim=True)) * scale
+            dq[b, :, h] = ds @ kk
+            dk[b, keep, hk] += ds.t() @ q[b, :, h]
+            dv[b, keep, hk] += p.t() @ g
+            out2[b, :, h] = (p * p) @ (vv * vv)
+            dq2[b, :, h] = (ds * ds) @ (kk * kk)
+            dk2[b, keep, hk] += (ds * ds).t() @ (q[b, :, h] ** 2)
+            dv2[b, keep, hk] += (p * p).t() @ (g * g)
+    return [(out, out2), (dq, dq2), (dk, dk2), (dv, dv2)]
+
+
+def _close(name, got, want, tol):
+    import torch
+    got = got.detach().cpu().double()
+    assert torch.isfinite(got).all(), name
+    want, squares = want
+    norm = float((want ** 2 + squares).sum().sqrt())
+    err = float((got - want).norm())
+    print("  %s rel %.3e" % (name, err / norm if norm else err), flush=True)
+    assert err <= tol * norm if norm else err == 0.0, name
+
+
+def _run(q, k, v, dout, **kw):
+    from paper_2209_13603_amd import attention
+    out, stats = attention.cross_attention(q, k, v, return_stats=True, **kw)
+    again = attention.cross_attention(q, k, v, **kw)
+    assert bool((again == out).all())
+    return (out, *attention.cross_attention_backward(q, k, v, out, stats, dout, **kw))
+
+
+# batch, queries, keys, heads, kv heads, dim
+SHAPES = [
+    (1, 1, 1, 1, 1, 64), (2, 1, 77, 4, 2, 64), (1, 3, 1000, 8, 1, 128), (2, 33, 65, 3, 3, 32), (1, 130, 64, 2, 1, 96),
+    (1, 257, 129, 2, 2, 128), (3, 31, 33, 2, 2, 16), (1, 64, 600, 1, 1, 80), (2, 45, 50, 6, 3, 36), (1, 70, 90, 2, 1, 1),
+    (1, 40, 40, 1, 1, 127), (1, 1500, 20, 2, 2, 64), (1, 700, 5, 4, 1, 48),
+]
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("shape", SHAPES)
+@pytest.mark.parametrize("mask", ["none", "bias", "holes"])
+def test_against_the_definition(shape, dtype, mask):
+    import torch
+    B, Sq, Sk, H, Hk, D = shape
+    g = torch.Generator(device="cuda:0").manual_seed(7 * Sq + Sk)
+    rnd = lambda *s: torch.randn(s, generator=g, device="cuda:0")
+    q, dout = (1.5 * rnd(B, Sq, H, D)).to(_dt(dtype)), rnd(B, Sq, H, D).to(_dt(dtype))
+    kv = rnd(B, Sk, 2, Hk, D).to(_dt(dtype))
+    k, v = kv[:, :, 0], kv[:, :, 1]
+    bias = lengths = None
+    if mask != "none":
+        bias = rnd(B, Sk)
+        lengths = torch.tensor([max(1, Sk - 5 * b) for b in range(B)], dtype=torch.int32, device="cuda:0")
+    if mask == "holes":
+        gone = torch.rand((B, Sk), generator=g, device="cuda:0") < 0.3
+        gone[:, 0] = False
+        bias = bias.masked_fill(gone, -math.inf)
+        # what stands at keys taken out must not matter
+        beyond = torch.arange(Sk, device="cuda:0")[None] >= lengths[:, None]
+        kv[gone | beyond] = float("nan")
+        kv[:, :, 1][gone | beyond] = float("inf")
+    want = _exact(q, k, v, dout, bias, lengths, 1 / math.sqrt(D))
+    got = _run(q, k, v, dout, key_bias=bias, key_lengths=lengths)
+    print(shape, dtype, mask)
+    for name, a, b in zip(("out", "dq", "dk", "dv"), got, want):
+        if Sk == 1 and name in ("dq", "dk"):  # one key: the scores' gradient is nothing but fp32 rounding
+            assert float(a.float().abs().max()) <= 1e-3
+            continue
+        _close(name, a, b, TOL[dtype])
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+def test_rows_without_keys_and_lengths_out_of_range(dtype):
+    import torch
+    g = torch.Generator(device="cuda:0").manual_seed(1)
+    B, Sq, Sk, H, D = 5, 40, 70, 2, 64
+    mk = lambda *s: torch.randn(s, generator=g, device="cuda:0").to(_dt(dtype))
+    q, k, v, dout = mk(B, Sq, H, D), mk(B, Sk, H, D), mk(B, Sk, H, D), mk(B, Sq, H, D)
+    lengths = torch.tensor([0, -3, 1000, 70, 30], dtype=torch.int32, device="cuda:0")
+    bias = torch.zeros(B, Sk, device="cuda:0")
+    bias[3] = -math.inf
+    k[0] = v[0] = float("nan")
+    want = _exact(q, k, v, dout, bias, lengths, 0.2)
+    got = _run(q, k, v, dout, key_bias=bias, key_lengths=lengths, scale=0.2)
+    for name, a, b in zip(("out", "dq", "dk", "dv"), got, want):
+        _close(name, a, b, TOL[dtype])
+        assert not a[0].any() and not a[1].any() and not a[3].any()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("queries", [1, 50])
+def test_masks_of_the_lowest_value(dtype, queries):
+    """Rows whose every key has the type's lowest bias weigh all keys alike."""
+    import torch
+    g = torch.Generator(device="cuda:0").manual_seed(2)
+    mk = lambda *s: torch.randn(s, generator=g, device="cuda:0").to(_dt(dtype))
+    q, k, v, dout = mk(2, queries, 2, 64), mk(2, 100, 2, 64), mk(2, 100, 2, 64), mk(2, queries, 2, 64)
+    low = torch.finfo(torch.float32).min
+    bias = torch.full((2, 100), low, device="cuda:0")
+    bias[1, :50] = 0.0
+    got = _run(q, k, v, dout, key_bias=bias)
+    uniform = torch.zeros(2, 100)
+    uniform[1, 50:] = -math.inf
+    zq = q.clone()
+    zq[0] = 0  # no score matters beside the lowest value
+    want = list(_exact(zq, k, v, dout, uniform, None, 1 / 8))
+    _close("out", got[0], want[0], TOL[dtype])
+    _close("dv", got[3], want[3], TOL[dtype])
+    exact = _exact(q, k, v, dout, bias, None, 1 / 8)  # 64 bits of such a bias hold no score either
+    for name, a, b in zip(("out", "dq", "dk", "dv"), got, exact):
+        _close(name, a, b, TOL[dtype])
+
+
+def test_negative_scale_and_large_bias():
+    import torch
+    g = torch.Generator(device="cuda:0").manual_seed(3)
+    mk = lambda *s: torch.randn(s, generator=g, device="cuda:0")
+    q, k, v, dout = mk(1, 60, 2, 32), mk(1, 90, 2, 32), mk(1, 90, 2, 32), mk(1, 60, 2, 32)
+    bias = 8 * mk(90)
+    want = _exact(q, k, v, dout, bias, None, -0.3)
+    for name, a, b in zip(("out", "dq", "dk", "dv"), _run(q, k, v, dout, key_bias=bias, scale=-0.3), want):
+        _close(name, a, b, 2e-5)  # scores of up to 40: their fp32 spacing is 4e-6
+
+
+def test_nan_and_infinity_stay_in_their_rows():
+    import torch
+    g = torch.Generator(device="cuda:0").manual_seed(4)
+    mk = lambda *s: torch.randn(s, generator=g, device="cuda:0").bfloat16()
+    q, k, v = mk(1, 40, 2, 64), mk(1, 80, 2, 64), mk(1, 80, 2, 64)
+    from paper_2209_13603_amd import attention
+    ref = attention.cross_attention(q, k, v)
+    q2 = q.clone()
+    q2[0, 7, 1, 3] = float("nan")
+    got = attention.cross_attention(q2, k, v)
+    assert torch.isnan(got[0, 7, 1].float()).all()
+    got[0, 7, 1] = ref[0, 7, 1]
+    assert bool((got == ref).all())
+    v2 = v.clone()
+    v2[0, 11, 0, 5] = float("inf")
+    got = attention.cross_attention(q, k, v2)
+    assert torch.isinf(got[0, :, 0, 5].float()).all()
+    assert bool((got[0, :, 1] == ref[0, :, 1]).all()) and bool(torch.isfinite(got[0, :, 0, 6].float()).all())
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+def test_strides_alignment_and_joint_gradients(dtype):
+    """Head-major tensors, rows off their alignment, gradients into one joint buffer."""
+    import torch
+    from paper_2209_13603_amd import attention
+    g = torch.Generator(device="cuda:0").manual_seed(5)
+    mk = lambda *s: torch.randn(s, generator=g, device="cuda:0").to(_dt(dtype))
+    q = mk(2, 3, 50, 64).transpose(1, 2)
+    wide = mk(2, 70, 3, 67)
+    k, v = wide[..., 1:65], mk(2, 70, 3, 64)
+    dout = mk(2, 50, 3, 66)[..., :64]
+    want = _exact(q, k, v, dout, None, None, 1 / 8)
+    out, stats = attention.cross_attention(q, k, v, return_stats=True)
+    joint = torch.full((2, 70, 2, 3, 64), float("nan"), device="cuda:0").to(_dt(dtype))
+    dq = torch.empty(2, 3, 50, 64, device="cuda:0", dtype=_dt(dtype)).transpose(1, 2)
+    attention.cross_attention_backward(q, k, v, out, stats, dout, dq=dq, dk=joint[:, :, 0], dv=joint[:, :, 1])
+    for name, a, b in zip(("out", "dq", "dk", "dv"), (out, dq, joint[:, :, 0], joint[:, :, 1]), want):
+        _close(name, a, b, TOL[dtype])
+
+
+def test_empty_axes():
+    import torch
+    mk = lambda *s: torch.randn(s, device="cuda:0")
+    q, dout = mk(2, 9, 2, 32), mk(2, 9, 2, 32)
+    none = mk(2, 0, 2, 32)
+    out, dq, dk, dv = _run(q, none, none, dout)
+    assert not out.any() and not dq.any() and dk.numel() == 0
+    out, dq, dk, dv = _run(none, q, q, none)
+    assert out.numel() == 0 and not dk.any() and not dv.any()
+    out, *_ = _run(mk(0, 3, 2, 32), mk(0, 4, 2, 32), mk(0, 4, 2, 32), mk(0, 3, 2, 32))
+    assert out.shape == (0, 3, 2, 32)
+
+
+def test_gradients_against_differences():
+    """Central differences of sum(out * dout) in fp32 along random directions: the difference's error is
+    about eps^2 of the third derivative plus 2^-23 |f| / eps, some 1e-4 of the slope at eps = 2^-6."""
+    import torch
+    from paper_2209_13603_amd import attention
+    g = torch.Generator(device="cuda:0").manual_seed(6)
+    mk = lambda *s: torch.randn(s, generator=g, device="cuda:0")
+    q, k, v, dout = mk(2, 20, 4, 24), mk(2, 35, 2, 24), mk(2, 35, 2, 24), mk(2, 20, 4, 24)
+    _, dq, dk, dv = _run(q, k, v, dout)
+    f = lambda *t: float((attention.cross_attention(*t).double() * dout.double()).sum())
+    eps = 2.0 ** -6
+    for n, grad in enumerate((dq, dk, dv)):
+        at = [q, k, v]
+        d = torch.sign(grad)
+        hi, lo = list(at), list(at)
+        hi[n], lo[n] = at[n] + eps * d, at[n] - eps * d
+        slope = (f(*hi) - f(*lo)) / (2 * eps)
+        want = float((grad.double() * d.double()).sum())
+        assert abs(slope - want) <= 5e-3 * abs(want), (n, slope, want)
+
+
+def test_long_cache_beyond_32_bit_offsets():
+    """Keys whose element offsets pass 2^31: the last rows of a cache shared by many heads."""
+    import torch
+    from paper_2209_13603_amd import attention
+    g = torch.Generator(device="cuda:0").manual_seed(8)
+    B, Sk, Hk, D = 1, 2200000, 8, 128
+    cache = torch.zeros(B, Sk, Hk, D, dtype=torch.bfloat16, device="cuda:0")
+    assert cache.numel() > 2 ** 31
+    tail = torch.randn(300, Hk, D, generator=g, device="cuda:0").bfloat16()
+    cache[0, -300:] = tail
+    bias = torch.full((Sk,), -math.inf, device="cuda:0")
+    bias[-300:] = 0.0
+    q = torch.randn(1, 2, Hk, D, generator=g, device="cuda:0").bfloat16()
+    got = attention.cross_attention(q, cache, cache, key_bias=bias)
+    want = attention.cross_attention(q, tail[None], tail[None])
+    err = float((got.float() - want.float()).norm() / want.float().norm())
+    assert err <= 2.0 ** -7, err  # both rounded
+
+
+def test_another_stream():
+    import torch
+    from paper_2209_13603_amd import attention
+    g = torch.Generator(device="cuda:0").manual_seed(9)
+    mk = lambda *s: torch.randn(s, generator=g, device="cuda:0").bfloat16()
+    q, k, v, dout = mk(2, 64, 4, 64), mk(2, 900, 4, 64), mk(2, 900, 4, 64), mk(2, 64, 4, 64)
+    ref = _run(q, k, v, dout)
+    torch.cuda.synchronize()
+    s = torch.cuda.Stream()
+    out, stats = attention.cross_attention(q, k, v, return_stats=True, stream=s)
+    got = (out, *attention.cross_attention_backward(q, k, v, out, stats, dout, stream=s))
+    s.synchronize()
+    assert all(bool((a == b).all()) for a, b in zip(got, ref))
+
+
+def test_graph_capture():
+    import torch
+    from paper_2209_13603_amd import attention
+    g = torch.Generator(device="cuda:0").manual_seed(10)
+    mk = lambda *s: torch.randn(s, generator=g, device="cuda:0").bfloat16()
+    q, k, v = mk(2, 1, 8, 64), mk(2, 3000, 2, 64), mk(2, 3000, 2, 64)
+    out = torch.empty_like(q)
+    attention.cross_attention(q, k, v, out=out)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        attention.cross_attention(q, k, v, out=out)
+    for i in range(4):
+        q.copy_(mk(2, 1, 8, 64))
+        want = attention.cross_attention(q, k, v)
+        out.fill_(float("nan"))
+        graph.replay()
+        torch.cuda.synchronize()
+        assert bool((out == want).all()), i
+
+
+def test_refusals():
+    import torch
+    from paper_2209_13603_amd import attention, disco
+    mk = lambda *s, dt=torch.float32: torch.randn(s, device="cuda:0").to(dt)
+    q, k = mk(2, 5, 4, 32), mk(2, 6, 2, 32)
+    out = torch.full_like(q, 3.0)
+
+    def status(*a, **kw):
+        with pytest.raises(disco.DiscoError) as e:
+            attention.cross_attention(*a, out=out, **kw)
+        return e.value.status
+
+    assert status(q, mk(2, 6, 3, 32), mk(2, 6, 3, 32)) == disco.DISCO_ERR_SHAPE       # 4 heads over 3
+    assert status(q, mk(1, 6, 2, 32), mk(1, 6, 2, 32)) == disco.DISCO_ERR_SHAPE       # batch
+    assert status(q, k, mk(2, 7, 2, 32)) == disco.DISCO_ERR_SHAPE                      # k and v differ
+    assert status(q, k.bfloat16(), k.bfloat16()) == disco.DISCO_ERR_DTYPE
+    assert status(q, k, k.bfloat16()) == disco.DISCO_ERR_DTYPE
+    assert status(q, k, k, scale=math.inf) == disco.DISCO_ERR_INVALID_ARGUMENT
+    assert status(mk(2, 5, 4, 129), mk(2, 6, 2, 129), mk(2, 6, 2, 129)) == disco.DISCO_ERR_SHAPE
+    assert status(q.half(), k.half(), k.half()) == disco.DISCO_ERR_DTYPE
+    with pytest.raises(disco.DiscoError):                                              # the output overlaps an input
+        attention.cross_attention(q, k, k, out=q)
+    with pytest.raises(disco.DiscoError):                                              # an output's rows overlap
+        attention.cross_attention(q, k, k, out=torch.empty(2, 5, 1, 32, device="cuda:0").expand(2, 5, 4, 32))
+    with pytest.raises(ValueError):
+        attention.cross_attention(q, k, k, key_bias=mk(2, 5))
+    with pytest.raises(ValueError):
+        attention.cross_attention(q, k, k, key_lengths=torch.zeros(2, dtype=torch.int64, device="cuda:0"))
+    with pytest.raises(ValueError):
+        attention.cross_attention(q, k, k, key_bias=mk(6).cpu())
+    torch.cuda.synchronize()
+    assert bool((out == 3.0).all())
