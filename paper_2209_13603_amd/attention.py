@@ -14,7 +14,6 @@ stream that the call runs on.
 """
 from __future__ import annotations
 
-import contextlib
 import ctypes
 import math
 from typing import NamedTuple
@@ -32,9 +31,15 @@ class Stats(NamedTuple):
     low: object
 
 
+# Storage types (DISCO_FLOAT32, DISCO_BFLOAT16); the library refuses the others.
+_DTYPES = {}
+
+
 def _dtype(t):
-    import torch
-    return DISCO_BFLOAT16 if t.dtype == torch.bfloat16 else DISCO_FLOAT32 if t.dtype == torch.float32 else 99
+    if not _DTYPES:
+        import torch
+        _DTYPES.update({torch.float32: DISCO_FLOAT32, torch.bfloat16: DISCO_BFLOAT16})
+    return _DTYPES.get(t.dtype, 99)
 
 
 def _heads(t, name) -> Heads:
@@ -44,51 +49,46 @@ def _heads(t, name) -> Heads:
     sb, st, sh, sd = t.stride()
     if sd != 1 and D > 1:
         raise ValueError("the last axis of %s must be contiguous" % name)
-    return Heads(t.data_ptr() if t.numel() else None, _dtype(t), D, H, 0, B, S, sb, st, sh)
+    return Heads(t.data_ptr() or None, _dtype(t), D, H, 0, B, S, sb, st, sh)
 
 
-def _flat(t, name, dtype, shape=None):
-    """A small fp32 or int32 argument: its type, and shape where one is given."""
+def _small(t, name, dtype, *shapes):
+    """A small argument of a given type and one of the given shapes; (address, batch stride)."""
     if t.dtype != dtype:
         raise ValueError("%s must be %s" % (name, dtype))
-    if shape is not None and tuple(t.shape) not in shape:
-        raise ValueError("%s must be one of the shapes %s" % (name, list(shape)))
-    if t.dim() and t.shape[-1] > 1 and t.stride(-1) != 1:
+    shape = tuple(t.shape)
+    if shape not in shapes:
+        raise ValueError("%s must be one of the shapes %s" % (name, list(shapes)))
+    if not t.is_contiguous() and shape[-1] > 1 and t.stride(-1) != 1:
         raise ValueError("the last axis of %s must be contiguous" % name)
-    return t
+    return t.data_ptr() or None, t.stride(0) if len(shape) == 2 and shape[0] > 1 else 0
 
 
 def _same_device(first, *others):
+    at = first.get_device()
     for t in others:
-        if t is not None and t.device != first.device:
+        if t is not None and t.get_device() != at:
             raise ValueError("all tensors must be on %s" % first.device)
 
 
-@contextlib.contextmanager
-def _on(stream):
-    """New tensors belong to the stream that the call runs on."""
-    import torch
-    with torch.cuda.stream(stream):
-        yield
-
-
 class _Call:
-    """The stream of one call, and where its outputs and scratch memory come from."""
+    """The stream of one call, and where its outputs and scratch memory come from: torch's allocator,
+    on that stream."""
+    __slots__ = ("device", "stream", "handle")
 
     def __init__(self, t, stream):
         import torch
         if not t.is_cuda:
             raise ValueError("tensors must be on a GPU")
         self.device = t.device
-        self.given = stream is not None
-        self.stream = stream if self.given else torch.cuda.current_stream(t.device)
-        self.handle = self.stream.cuda_stream
+        self.stream = stream
+        self.handle = torch._C._cuda_getCurrentRawStream(t.get_device()) if stream is None else stream.cuda_stream
 
     def empty(self, shape, dtype):
         import torch
-        if not self.given:
+        if self.stream is None:
             return torch.empty(shape, dtype=dtype, device=self.device)
-        with _on(self.stream):
+        with torch.cuda.stream(self.stream):
             return torch.empty(shape, dtype=dtype, device=self.device)
 
     def workspace(self, name, *args):
@@ -98,7 +98,7 @@ class _Call:
         _check(getattr(library(), name)(*args, need))
         if need.value == 0:
             return None, None, 0
-        ws = self.empty((need.value,), torch.uint8)
+        ws = self.empty(need.value, torch.uint8)
         return ws, ws.data_ptr(), need.value
 
 
@@ -108,22 +108,17 @@ def _rotation(rotation, layout, positions, first_position, x):
     if rotation is None:
         return None
     cos, sin = rotation
-    for t, name in ((cos, "cosines"), (sin, "sines")):
-        _flat(t, name, torch.float32)
-        if t.dim() != 2 or not t.is_contiguous():
-            raise ValueError("%s must be [rows, rotary / 2], contiguous" % name)
-    if cos.shape != sin.shape:
-        raise ValueError("cosines and sines differ in shape")
+    if cos.dtype != torch.float32 or sin.dtype != torch.float32:
+        raise ValueError("cosines and sines must be torch.float32")
+    if cos.dim() != 2 or cos.shape != sin.shape or not (cos.is_contiguous() and sin.is_contiguous()):
+        raise ValueError("cosines and sines must be [rows, rotary / 2], contiguous")
     _same_device(x, cos, sin, positions)
-    stride = 0
+    rows, half = cos.shape
+    address, stride = None, 0
     if positions is not None:
         B, S = x.shape[:2]
-        _flat(positions, "positions", torch.int32, ((S,), (1, S), (B, S)))
-        stride = positions.stride(0) if positions.dim() == 2 and positions.shape[0] > 1 else 0
-    has = cos.numel() > 0
-    return RotationArgs(2 * cos.shape[1], LAYOUTS[layout], cos.data_ptr() if has else None,
-                        sin.data_ptr() if has else None, cos.shape[0],
-                        positions.data_ptr() if positions is not None and positions.numel() else None, stride,
+        address, stride = _small(positions, "positions", torch.int32, (S,), (1, S), (B, S))
+    return RotationArgs(2 * half, LAYOUTS[layout], cos.data_ptr() or None, sin.data_ptr() or None, rows, address, stride,
                         first_position)
 
 
@@ -177,16 +172,14 @@ def norm_rotate_backward(x, weight, dy, rotation=None, layout="half", positions=
 def _options(q, k, key_bias, key_lengths, scale):
     import torch
     B, Sk = k.shape[:2]
+    bias = lengths = None
     stride = 0
     if key_bias is not None:
-        _flat(key_bias, "key_bias", torch.float32, ((Sk,), (1, Sk), (B, Sk)))
-        stride = key_bias.stride(0) if key_bias.dim() == 2 and key_bias.shape[0] > 1 else 0
+        bias, stride = _small(key_bias, "key_bias", torch.float32, (Sk,), (1, Sk), (B, Sk))
     if key_lengths is not None:
-        _flat(key_lengths, "key_lengths", torch.int32, ((B,),))
+        lengths, _ = _small(key_lengths, "key_lengths", torch.int32, (B,))
     _same_device(q, key_bias, key_lengths)
-    return AttentionArgs(0.0 if scale is None else scale,
-                         key_bias.data_ptr() if key_bias is not None and key_bias.numel() else None, stride,
-                         key_lengths.data_ptr() if key_lengths is not None and B else None)
+    return AttentionArgs(0.0 if scale is None else scale, bias, stride, lengths)
 
 
 def cross_attention(q, k, v, key_bias=None, key_lengths=None, scale=None, return_stats=False, out=None, stream=None):
@@ -211,7 +204,7 @@ def cross_attention(q, k, v, key_bias=None, key_lengths=None, scale=None, return
     opt = _options(q, k, key_bias, key_lengths, scale)
     keep, ws, n = call.workspace("disco_cross_attention_workspace", hq, hk, 0)
     _check(library().disco_cross_attention(hq, hk, _heads(v, "v"), opt, _heads(out, "out"),
-                                           rows.data_ptr() if rows is not None and rows.numel() else None, _ref(hlow),
+                                           rows.data_ptr() or None if rows is not None else None, _ref(hlow),
                                            ws, n, call.handle))
     return (out, Stats(rows, low)) if return_stats else out
 
@@ -230,7 +223,7 @@ def cross_attention_backward(q, k, v, out, stats, dout, key_bias=None, key_lengt
         raise ValueError("scale must not be 0")
     rows, low = stats
     _same_device(q, k, v, out, rows, low, dout, dq, dk, dv)
-    _flat(rows, "stats.rows", torch.float32, ((q.shape[0], q.shape[2], q.shape[1], 2),))
+    _small(rows, "stats.rows", torch.float32, (q.shape[0], q.shape[2], q.shape[1], 2))
     if not rows.is_contiguous():
         raise ValueError("stats.rows must be contiguous")
     hlow = _heads(low, "stats.low") if low is not None else None
@@ -238,7 +231,7 @@ def cross_attention_backward(q, k, v, out, stats, dout, key_bias=None, key_lengt
     opt = _options(q, k, key_bias, key_lengths, scale)
     keep, ws, n = call.workspace("disco_cross_attention_workspace", hq, hk, 1)
     _check(library().disco_cross_attention_backward(
-        hq, hk, _heads(v, "v"), opt, _heads(out, "out"), rows.data_ptr() if rows.numel() else None,
+        hq, hk, _heads(v, "v"), opt, _heads(out, "out"), rows.data_ptr() or None,
         _ref(hlow), _heads(dout, "dout"), _heads(dq, "dq"), _heads(dk, "dk"), _heads(dv, "dv"), ws, n, call.handle))
     return dq, dk, dv
 

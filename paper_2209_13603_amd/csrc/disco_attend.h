@@ -152,14 +152,21 @@ struct TileOf {
             }
         } else {
             typedef __attribute__((address_space(3))) const float V;
+            // The 32 rows' own sum first, then onto o: a chain of roundings as
+            // long as the tiles, not as the rows.
 #pragma unroll
-            for (int i = 0; i < 16; ++i)
+            for (int d = 0; d < DP / 32; ++d) {
+                f16 t;
 #pragma unroll
-                for (int d = 0; d < DP / 32; ++d) {
+                for (int i = 0; i < 16; ++i) t[i] = 0.0f;
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
                     const uint32_t at = 2 * d * 1024 + (2 * k + i / 8) * kStep16 + (i % 4) * 16;
                     const float v = *(V*)(tile + ((i / 4) % 2 ? l.t1 : l.t0) + at);
-                    o[d] = __builtin_amdgcn_mfma_f32_32x32x2f32(v, p[i], o[d], 0, 0, 0);
+                    t = __builtin_amdgcn_mfma_f32_32x32x2f32(v, p[i], t, 0, 0, 0);
                 }
+                o[d] += t;
+            }
         }
     }
 };

@@ -139,15 +139,17 @@ __global__ __launch_bounds__(kAttendThreads, (kWorkgroups<T, DP>)) void k_attend
                 for (int r = 0; r < 16; ++r) o[d][r] *= f;
         }
         const float neg = m == -INFINITY ? 0.0f : -m;
+        float sum = 0.0f;  // of the tile, then onto l: a shorter chain of roundings
 #pragma unroll
         for (int k = 0; k < NK; ++k) {
 #pragma unroll
             for (int r = 0; r < 16; ++r) {
                 s[k][r] = __builtin_amdgcn_exp2f(fmaf(s[k][r], scale2, neg));
-                l += s[k][r];
+                sum += s[k][r];
             }
             Tile::values(vt, ln, k, s[k], o);
         }
+        l += sum;
         if (more) store(buf ^ 1);
         __syncthreads();
     }

@@ -4,7 +4,7 @@ from __future__ import annotations
 
 import numpy as np
 
-from .attention import _Call, _dtype
+from .attention import _Call, _dtype, _same_device
 from .disco import _check, library
 
 # disco_tensor_t
@@ -14,9 +14,8 @@ _TENSOR = np.dtype([("data", "u8"), ("dtype", "i4"), ("ndim", "i4"), ("shape", "
 def _array(tensors):
     """The tensors as an array of disco_tensor_t, each as one axis of its entries."""
     a = np.zeros(len(tensors), dtype=_TENSOR)
-    for t in tensors:
-        if not t.is_contiguous():
-            raise ValueError("gradients must be contiguous")
+    if not all([t.is_contiguous() for t in tensors]):
+        raise ValueError("gradients must be contiguous")
     a["data"] = [t.data_ptr() for t in tensors]
     a["dtype"] = [_dtype(t) for t in tensors]
     a["ndim"] = 1
@@ -36,14 +35,14 @@ def clip(grads, max_norm, eps=1e-6, out=None, norm_only=False, stream=None):
     out = grads if out is None else list(out)
     if not grads:
         raise ValueError("no gradients")
-    if len(out) != len(grads) or any(o.shape != g.shape for o, g in zip(out, grads)):
+    apart = out is not grads
+    if apart and [t.shape for t in out] != [t.shape for t in grads]:
         raise ValueError("out must match the gradients one by one")
-    if any(t.device != grads[0].device for t in grads + out):
-        raise ValueError("all tensors must be on %s" % grads[0].device)
+    _same_device(*grads, *(out if apart else ()))
     call = _Call(grads[0], stream)
     norm = call.empty((), torch.float32)
     a = _array(grads)
-    b = a if norm_only or out is grads else _array(out)
+    b = _array(out) if apart and not norm_only else a
     keep, ws, n = call.workspace("disco_gradient_clip_workspace", len(grads), a.ctypes.data)
     _check(library().disco_gradient_clip(len(grads), a.ctypes.data, None if norm_only else b.ctypes.data, max_norm, eps,
                                          norm.data_ptr(), ws, n, call.handle))
