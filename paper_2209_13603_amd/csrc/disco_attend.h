@@ -63,13 +63,23 @@ __device__ __forceinline__ float start_of(float bias, float inv_scale) {
 
 // Workgroups go round the XCDs one by one: gives each XCD a run of consecutive
 // work items, which share keys, values or queries in its L2.  Grid: 8 * ceil(n / 8).
-__device__ __forceinline__ int64_t xcd_item(int64_t n) {
-    const int64_t per = (n + 7) / 8;
-    return (int64_t)(blockIdx.x % 8) * per + blockIdx.x / 8;
+__device__ __forceinline__ uint32_t xcd_item(uint32_t n) { return blockIdx.x % 8 * ((n + 7) / 8) + blockIdx.x / 8; }
+inline unsigned xcd_grid(uint32_t n) { return (n + 7) / 8 * 8; }
+
+// First of the tiles of part `part` when `tiles` are dealt to `parts`.
+__device__ __forceinline__ int first_tile(int tiles, int part, int parts) {
+    const int q = tiles / parts, r = tiles % parts;
+    return q * part + min(part, r);
 }
-inline unsigned xcd_grid(int64_t n) { return (unsigned)((n + 7) / 8 * 8); }
 
 __device__ __forceinline__ float other_half(float v) { return __shfl_xor(v, 32); }
+
+template <int N, typename F>
+__device__ __forceinline__ void flip(F (&f)[N], uint32_t mask) {
+    asm("" : "+v"(mask));  // not known to the compiler: the operation stays
+#pragma unroll
+    for (int s = 0; s < N; ++s) f[s] = __builtin_bit_cast(F, __builtin_bit_cast(u4, f[s]) ^ mask);
+}
 
 template <typename T>
 struct Mat;
@@ -77,6 +87,14 @@ template <>
 struct Mat<__bf16> {
     typedef bf8 Frag;
     static constexpr int CH = 8;  // entries of a chunk
+    // The fragments with the sign of `by`.  (Done before a loop it also ends the
+    // wait for their loads there; otherwise every round of the loop waits for
+    // all loads under way.)
+    template <int N>
+    static __device__ __forceinline__ void sign(Frag (&f)[N], float by) {
+        const uint32_t mask = (__float_as_uint(by) >> 31) * 0x80008000u;
+        flip<N>(f, mask);
+    }
     static __device__ __forceinline__ f16 scores(Frag a, Frag b, f16 c) {
         return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
     }
@@ -85,6 +103,10 @@ template <>
 struct Mat<float> {
     typedef f4 Frag;
     static constexpr int CH = 4;
+    template <int N>
+    static __device__ __forceinline__ void sign(Frag (&f)[N], float by) {
+        flip<N>(f, __float_as_uint(by) & 0x80000000u);
+    }
     static __device__ __forceinline__ f16 scores(Frag a, Frag b, f16 c) {
 #pragma unroll
         for (int j = 0; j < 4; ++j) c = __builtin_amdgcn_mfma_f32_32x32x2f32(a[j], b[j], c, 0, 0, 0);
@@ -130,6 +152,10 @@ struct TileOf {
         for (int s = 0; s < NS; ++s) c = Mat<T>::scores(row(tile, l, k, s), f[s], c);
         return c;
     }
+    static __device__ __forceinline__ f16 scores(const lds_t* tile, const Lane& l, int k, const Frag (&f)[NS]) {
+        const f16 zero = {0.0f};
+        return scores(tile, l, k, f, zero);
+    }
     // o[D / 32] += (rows 32 k .. 32 k + 31 of the tile)^T x p
     static __device__ __forceinline__ void values(const lds_t* tile, const Lane& l, int k, const f16& p,
                                                   f16 (&o)[DP / 32]) {
@@ -171,69 +197,104 @@ struct TileOf {
     }
 };
 
-// 16 bytes of a row from entry c on, zeros beyond D.
-template <typename T>
-__device__ __forceinline__ u4 load_chunk(const T* row, int c, int D, bool wide) {
+// 16 bytes of a row from entry c on, zeros beyond D.  W: in one load.
+template <typename T, bool W>
+__device__ __forceinline__ u4 load_chunk(const T* row, int c, int D) {
     constexpr int CH = Mat<T>::CH;
     if (c >= D) return u4{0u, 0u, 0u, 0u};
-    if (wide) return *(const u4*)(row + c);
+    if constexpr (W) return *(const u4*)(row + c);
     typename Mat<T>::Frag f;
 #pragma unroll
     for (int j = 0; j < CH; ++j) f[j] = c + j < D ? row[c + j] : (T)0.0f;
     return __builtin_bit_cast(u4, f);
 }
 
-// A tile of ROWS rows on its way from memory to LDS, spread over the
-// workgroup's waves: each wave takes segments (16 rows x 4 chunks, a row's 64
-// bytes by four lanes).
+// The rows that tiles are read from: D entries `stride` entries apart.
+template <typename T>
+struct Rows {
+    const T* p;
+    int64_t stride, rows;
+    int D;
+};
+
+// A tile of ROWS rows on its way from memory to LDS.  Each thread holds chunks
+// of one row: a row's 64 bytes by four lanes, a segment by a wave.
 template <typename T, int DP, int ROWS>
 struct Stage {
     typedef TileOf<T, DP> Tile;
-    static constexpr int kSegs = ROWS / 16 * Tile::SEGS;
-    static constexpr int N = (kSegs + kAttendWaves - 1) / kAttendWaves;
-    static constexpr int kBytes = kSegs * 1024;
+    static constexpr int kHalves = ROWS == 64 ? 1 : 2;  // waves to a row
+    static constexpr int N = (Tile::SEGS + kHalves - 1) / kHalves;
+    static constexpr int kBytes = ROWS / 16 * Tile::SEGS * 1024;
+    static_assert(ROWS * kHalves == 64, "a thread for each quarter of a row's segments");
     u4 v[N];
-    static __device__ __forceinline__ int seg(int wave, int u) { return wave * N + u; }
-    static __device__ __forceinline__ bool has(int wave, int u) { return kSegs % kAttendWaves == 0 || seg(wave, u) < kSegs; }
-    static __device__ __forceinline__ int row_of(int wave, int lane, int u) {
-        return seg(wave, u) / Tile::SEGS * 16 + lane / 4;
+    static __device__ __forceinline__ int row_of(int wave, int lane) { return wave / kHalves * 16 + lane / 4; }
+    // Segment u of this thread's row.
+    static __device__ __forceinline__ int seg(int wave, int u) { return kHalves * u + wave % kHalves; }
+    static __device__ __forceinline__ bool has(int wave, int u) {
+        return Tile::SEGS % kHalves == 0 || seg(wave, u) < Tile::SEGS;
     }
-    // Rows row0 .. of a matrix of `rows` > 0 rows; those beyond come as the last one.
-    __device__ __forceinline__ void load(const T* base, int64_t stride, int64_t row0, int64_t rows, int D, bool wide,
-                                         int wave, int lane) {
+    // W: 16-byte loads through a buffer over the tile's rows, to which the
+    // entries beyond D and the rows beyond the last are out of range and come
+    // as zeros: off is all that a thread needs.  Otherwise entry by entry, the
+    // rows beyond the last coming as the last.
+    uint32_t off[N];
+    template <bool W>
+    __device__ __forceinline__ void plan(const Rows<T>& m, int wave, int lane) {
+        if constexpr (W) {
 #pragma unroll
-        for (int u = 0; u < N; ++u) {
-            if (!has(wave, u)) continue;
-            const int64_t left = rows - 1 - row0;
-            const int r = (int)min((int64_t)row_of(wave, lane, u), left);
-            const int c = (seg(wave, u) % Tile::SEGS * 4 + lane % 4) * Mat<T>::CH;
-            v[u] = load_chunk(base + (row0 + r) * stride, c, D, wide);
+            for (int u = 0; u < N; ++u) {
+                const int c = (seg(wave, u) * 4 + lane % 4) * Mat<T>::CH;
+                off[u] = has(wave, u) && c < m.D ? (uint32_t)(row_of(wave, lane) * (int)m.stride + c) * (uint32_t)sizeof(T)
+                                                 : 0x80000000u;
+            }
         }
     }
-    // keep(row of the tile): whether the row's values count; zeros otherwise, so
-    // that whatever memory holds there meets no product.
-    template <typename F>
-    __device__ __forceinline__ void store(lds_t* tile, int wave, int lane, F&& keep) const {
+    template <bool W>
+    __device__ __forceinline__ void load(const Rows<T>& m, int64_t row0, int wave, int lane) {
+        const int64_t left = m.rows - 1 - row0;
+        if constexpr (W) {
+            const int64_t bytes = (left * m.stride + m.D) * (int64_t)sizeof(T);
+            const __amdgpu_buffer_rsrc_t r =
+                __builtin_amdgcn_make_buffer_rsrc(const_cast<T*>(m.p + row0 * m.stride), (short)0,
+                                                  bytes < 0x7fffffff ? (int)bytes : 0x7fffffff, 0x00020000);
+#pragma unroll
+            for (int u = 0; u < N; ++u)
+                v[u] = __builtin_bit_cast(u4, __builtin_amdgcn_raw_buffer_load_b128(r, (int)off[u], 0, 0));
+        } else {
+            const int r = min(row_of(wave, lane), (int)min(left, (int64_t)ROWS));
+            const int c = (seg(wave, 0) * 4 + lane % 4) * Mat<T>::CH;
+            constexpr int step = kHalves * 4 * Mat<T>::CH;
+#pragma unroll
+            for (int u = 0; u < N; ++u)
+                if (has(wave, u)) v[u] = load_chunk<T, false>(m.p + (row0 + r) * m.stride, c + u * step, m.D);
+        }
+    }
+    // keep: whether this thread's row counts; zeros otherwise, so that whatever
+    // memory holds there meets no product.
+    __device__ __forceinline__ void store(lds_t* tile, int wave, int lane, bool keep) {
         typedef __attribute__((address_space(3))) u4 V;
+        if (!__all(keep)) {
 #pragma unroll
-        for (int u = 0; u < N; ++u) {
-            if (!has(wave, u)) continue;
-            const u4 z = keep(u) ? v[u] : u4{0u, 0u, 0u, 0u};
-            *(V*)(tile + seg(wave, u) * 1024 + (lane % 4) * 256 + (((lane / 4) ^ (4 * (lane % 4))) * 16)) = z;
+            for (int u = 0; u < N; ++u) v[u] = keep ? v[u] : u4{0u, 0u, 0u, 0u};
         }
+        lds_t* to = tile + wave / kHalves * Tile::kStep16 + wave % kHalves * 1024 + (lane % 4) * 256 +
+                    (((lane / 4) ^ (4 * (lane % 4))) * 16);
+#pragma unroll
+        for (int u = 0; u < N; ++u)
+            if (has(wave, u)) *(V*)(to + u * kHalves * 1024) = v[u];
     }
 };
 
 // A lane's column vector as fragments: entries 2 CH s + CH h + j.
-template <typename T, int DP>
-__device__ __forceinline__ void load_frags(const T* row, int D, bool wide, bool live, int lane,
+template <typename T, int DP, bool W>
+__device__ __forceinline__ void load_frags(const T* row, int D, bool live, int lane,
                                            typename Mat<T>::Frag (&f)[TileOf<T, DP>::NS]) {
     constexpr int CH = Mat<T>::CH;
 #pragma unroll
     for (int s = 0; s < TileOf<T, DP>::NS; ++s) {
         const u4 z = {0u, 0u, 0u, 0u};
         f[s] = __builtin_bit_cast(typename Mat<T>::Frag,
-                                  live ? load_chunk(row, 2 * CH * s + CH * (lane / 32), D, wide) : z);
+                                  live ? load_chunk<T, W>(row, 2 * CH * s + CH * (lane / 32), D) : z);
     }
 }
 
@@ -243,15 +304,15 @@ __device__ __forceinline__ void store4(float* p, f4 v) { *(f4*)p = v; }
 
 // A lane's column of accumulators o (entry 32 d + 8 (i / 4) + 4 h + i % 4 in
 // register i), times f, to the row's D entries.
-template <typename T, int DP>
-__device__ __forceinline__ void store_column(T* row, const f16 (&o)[DP / 32], float f, int D, bool wide, int lane) {
+template <typename T, int DP, bool W>
+__device__ __forceinline__ void store_column(T* row, const f16 (&o)[DP / 32], float f, int D, int lane) {
 #pragma unroll
     for (int d = 0; d < DP / 32; ++d)
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
             const int c = 32 * d + 8 * q + 4 * (lane / 32);
             const f4 v = {o[d][4 * q] * f, o[d][4 * q + 1] * f, o[d][4 * q + 2] * f, o[d][4 * q + 3] * f};
-            if (wide) {
+            if constexpr (W) {
                 if (c < D) store4(row + c, v);
             } else {
 #pragma unroll
@@ -261,11 +322,12 @@ __device__ __forceinline__ void store_column(T* row, const f16 (&o)[DP / 32], fl
         }
 }
 
-// Host: whether rows of D entries can be read or written 16 (fp32 columns) or
-// 8 bytes at a time.
+// Host: whether rows of D entries can be read or written `entries` at a time,
+// and the rows of a tile through one buffer.
 inline bool wide_rows(const Heads& t, int dim, int entries, size_t elem) {
+    if (!t.p) return true;  // not there
     return dim % entries == 0 && (uintptr_t)t.p % (entries * elem) == 0 && t.sb % entries == 0 && t.st % entries == 0 &&
-           t.sh % entries == 0;
+           t.sh % entries == 0 && t.st >= dim && t.st * (int64_t)elem < (int64_t)1 << 24;
 }
 
 }  // namespace disco

@@ -20,11 +20,11 @@ namespace {
 // keys in `splits` parts.  Parts leave unnormed sums, joined by k_attend_join.
 constexpr int kRows = 32 * kAttendWaves;
 struct Cut {
-    int64_t rows, row_blocks, items;
+    uint32_t rows, row_blocks, items;
     int32_t splits;
     float* part;   // [splits][all rows][dim]
     float* stat;   // [splits][all rows][2]
-    uint8_t wide_q, wide_k, wide_v, wide_o, wide_low;
+    bool wide;     // rows of all tensors go by 16 bytes (out by four entries)
 };
 
 // Workgroups of a CU that the registers are sized for.
@@ -35,7 +35,7 @@ constexpr int kKeys = std::is_same<T, __bf16>::value ? 64 : 32;  // keys of a ti
 
 // Each wave holds 32 rows; the workgroup's waves share the tiles of keys and
 // values, double-buffered in LDS, the next tile's loads in flight in registers.
-template <typename T, int DP>
+template <typename T, int DP, bool W>
 __global__ __launch_bounds__(kAttendThreads, (kWorkgroups<T, DP>)) void k_attend(AttendArgs a, Cut c) {
     typedef TileOf<T, DP> Tile;
     constexpr int KT = kKeys<T>, NK = KT / 32;
@@ -44,26 +44,23 @@ __global__ __launch_bounds__(kAttendThreads, (kWorkgroups<T, DP>)) void k_attend
     __shared__ float starts[2][KT];
     lds_t* lds = (lds_t*)smem;
 
-    const int64_t id = xcd_item(c.items);
+    const uint32_t id = xcd_item(c.items);
     if (id >= c.items) return;
     const int split = (int)(id % c.splits);
-    const int64_t rb = id / c.splits % c.row_blocks;
+    const uint32_t rb = id / c.splits % c.row_blocks;
     const int bh = (int)(id / c.splits / c.row_blocks), b = bh / a.kv_heads, hk = bh % a.kv_heads;
     const int wave = threadIdx.x / kWave, lane = threadIdx.x % kWave, G = a.heads / a.kv_heads;
-    const int64_t row = rb * kRows + wave * 32 + lane % 32;
+    const uint32_t row = rb * kRows + wave * 32 + lane % 32;
     const bool live = row < c.rows;
-    const int64_t i = live ? row / G : 0;
-    const int h = hk * G + (int)(live ? row % G : 0);
-    const T* kp = (const T*)a.k.p + b * a.k.sb + hk * a.k.sh;
-    const T* vp = (const T*)a.v.p + b * a.v.sb + hk * a.v.sh;
-    const int64_t n = key_count(a, b), tiles = (n + KT - 1) / KT;
-    const int64_t t0 = tiles * split / c.splits, t1 = tiles * (split + 1) / c.splits;
+    const int64_t i = live ? row / (uint32_t)G : 0;
+    const int h = hk * G + (int)(live ? row % (uint32_t)G : 0);
+    const int64_t n = key_count(a, b);
+    const int tiles = (int)((n + KT - 1) / KT);
+    const int t0 = first_tile(tiles, split, c.splits), t1 = first_tile(tiles, split + 1, c.splits);
 
     typename Tile::Frag qf[Tile::NS];
-    load_frags<T, DP>((const T*)a.q.p + b * a.q.sb + i * a.q.st + h * a.q.sh, a.dim, c.wide_q, live, lane, qf);
-    if (a.scale2 < 0.0f)
-#pragma unroll
-        for (int s = 0; s < Tile::NS; ++s) qf[s] = -qf[s];
+    load_frags<T, DP, W>((const T*)a.q.p + b * a.q.sb + i * a.q.st + h * a.q.sh, a.dim, live, lane, qf);
+    Mat<T>::template sign<Tile::NS>(qf, a.scale2);
     const float scale2 = fabsf(a.scale2), inv_scale = 1.0f / fabsf(a.scale);
     const typename Tile::Lane ln = Tile::lane_of(lane);
 
@@ -75,51 +72,52 @@ __global__ __launch_bounds__(kAttendThreads, (kWorkgroups<T, DP>)) void k_attend
     float m = -INFINITY, l = 0.0f;
 
     St sk, sv;
-    float start[St::N], start1 = 0.0f;  // of the staged rows, and of key threadIdx.x of the tile
-    auto load = [&](int64_t t) {
-        sk.load(kp, a.k.st, t * KT, n, a.dim, c.wide_k, wave, lane);
-        sv.load(vp, a.v.st, t * KT, n, a.dim, c.wide_v, wave, lane);
-        auto start_at = [&](int64_t j) {
-            return j >= n ? -INFINITY : a.bias ? start_of(a.bias[b * a.bias_sb + j], inv_scale) : 0.0f;
-        };
-#pragma unroll
-        for (int u = 0; u < St::N; ++u) start[u] = start_at(t * KT + St::row_of(wave, lane, u));
-        if (threadIdx.x < KT) start1 = start_at(t * KT + threadIdx.x);
+    float bias = 0.0f;  // of the staged row
+    int left = 0;       // rows of the staged tile that exist
+    const Rows<T> keys{(const T*)a.k.p + b * a.k.sb + hk * a.k.sh, a.k.st, n, a.dim};
+    const Rows<T> vals{(const T*)a.v.p + b * a.v.sb + hk * a.v.sh, a.v.st, n, a.dim};
+    const int srow = St::row_of(wave, lane);
+    sk.template plan<W>(keys, wave, lane);
+    sv.template plan<W>(vals, wave, lane);
+    auto load = [&](int t) {
+        sk.template load<W>(keys, (int64_t)t * KT, wave, lane);
+        sv.template load<W>(vals, (int64_t)t * KT, wave, lane);
+        left = (int)(n - (int64_t)t * KT);
+        if (a.bias) bias = a.bias[b * a.bias_sb + (int64_t)t * KT + min(srow, left - 1)];
     };
     auto store = [&](int buf) {
-        auto keep = [&](int u) { return start[u] != -INFINITY; };
+        const float start = srow < left ? start_of(bias, inv_scale) : -INFINITY;
+        const bool keep = start != -INFINITY;
         sk.store(lds + buf * 2 * St::kBytes, wave, lane, keep);
         sv.store(lds + (buf * 2 + 1) * St::kBytes, wave, lane, keep);
-        if (threadIdx.x < KT) starts[buf][threadIdx.x] = start1;
+        if (lane % 4 == 0) starts[buf][srow] = start;  // (two waves to a row: the same value)
     };
-
     if (t0 < t1) {
         load(t0);
         store(0);
     }
     __syncthreads();
-    for (int64_t t = t0; t < t1; ++t) {
-        const int buf = (int)(t - t0) & 1;
+    for (int t = t0; t < t1; ++t) {
+        const int buf = (t - t0) & 1;
         const bool more = t + 1 < t1;
         if (more) load(t + 1);
         const lds_t* kt = lds + buf * 2 * St::kBytes;
         const lds_t* vt = kt + St::kBytes;
         f16 s[NK];
-        const bool plain = !a.bias && (t + 1) * KT <= n;
+        if (!a.bias && (int64_t)(t + 1) * KT <= n) {
 #pragma unroll
-        for (int k = 0; k < NK; ++k) {
-            if (plain) {
+            for (int k = 0; k < NK; ++k) s[k] = Tile::scores(kt, ln, k, qf);
+        } else {
 #pragma unroll
-                for (int r = 0; r < 16; ++r) s[k][r] = 0.0f;
-            } else {
+            for (int k = 0; k < NK; ++k) {
 #pragma unroll
                 for (int q = 0; q < 4; ++q) {
                     const f4 v = *(const f4*)&starts[buf][32 * k + 8 * q + 4 * (lane / 32)];
 #pragma unroll
                     for (int r = 0; r < 4; ++r) s[k][4 * q + r] = v[r];
                 }
+                s[k] = Tile::scores(kt, ln, k, qf, s[k]);
             }
-            s[k] = Tile::scores(kt, ln, k, qf, s[k]);
         }
         float top = s[0][0];
 #pragma unroll
@@ -159,7 +157,7 @@ __global__ __launch_bounds__(kAttendThreads, (kWorkgroups<T, DP>)) void k_attend
     if (c.splits > 1) {
         const int64_t all = (int64_t)a.batch * a.kv_heads * c.rows;
         const int64_t at = split * all + (int64_t)bh * c.rows + row;
-        store_column<float, DP>(c.part + at * a.dim, o, 1.0f, a.dim, a.dim % 4 == 0, lane);
+        store_column<float, DP, W>(c.part + at * a.dim, o, 1.0f, a.dim, lane);
         if (lane < 32) {
             c.stat[2 * at] = m;
             c.stat[2 * at + 1] = l;
@@ -167,7 +165,7 @@ __global__ __launch_bounds__(kAttendThreads, (kWorkgroups<T, DP>)) void k_attend
         return;
     }
     const float inv = l == 0.0f ? 0.0f : 1.0f / l;
-    store_column<T, DP>((T*)a.out.p + b * a.out.sb + i * a.out.st + h * a.out.sh, o, inv, a.dim, c.wide_o, lane);
+    store_column<T, DP, W>((T*)a.out.p + b * a.out.sb + i * a.out.st + h * a.out.sh, o, inv, a.dim, lane);
     if (a.stats && lane < 32) {
         a.stats[2 * stat] = m;
         a.stats[2 * stat + 1] = l;
@@ -181,7 +179,7 @@ __global__ __launch_bounds__(kAttendThreads, (kWorkgroups<T, DP>)) void k_attend
                     const float v = o[d][r] * inv;
                     o[d][r] = v - (float)(__bf16)v;
                 }
-            store_column<T, DP>((T*)a.low.p + b * a.low.sb + i * a.low.st + h * a.low.sh, o, 1.0f, a.dim, c.wide_low, lane);
+            store_column<T, DP, W>((T*)a.low.p + b * a.low.sb + i * a.low.st + h * a.low.sh, o, 1.0f, a.dim, lane);
         }
     }
 }
@@ -229,15 +227,15 @@ __global__ __launch_bounds__(kAttendThreads) void k_attend_join(AttendArgs a, Cu
 
 Cut cut_of(const AttendArgs& a) {
     Cut c{};
-    c.rows = a.queries * (a.heads / a.kv_heads);
+    c.rows = (uint32_t)(a.queries * (a.heads / a.kv_heads));
     c.row_blocks = (c.rows + kRows - 1) / kRows;
-    const int64_t blocks = c.row_blocks * a.batch * a.kv_heads;
+    const int64_t blocks = (int64_t)c.row_blocks * a.batch * a.kv_heads;
     const int KT = a.bf16 ? kKeys<__bf16> : kKeys<float>;
     const int64_t tiles = (a.keys + KT - 1) / KT;
     // Two workgroups a CU where there are keys enough for a part of four tiles each.
     const int64_t want = blocks > 0 ? (2 * 256 + blocks - 1) / blocks : 1;
     c.splits = (int32_t)std::max<int64_t>(1, std::min<int64_t>({want, tiles / 4, 256}));
-    c.items = blocks * c.splits;
+    c.items = (uint32_t)(blocks * c.splits);
     return c;
 }
 
@@ -248,7 +246,8 @@ size_t part_bytes(const AttendArgs& a, const Cut& c) {
 
 template <typename T, int DP>
 void launch(const AttendArgs& a, const Cut& c) {
-    hipLaunchKernelGGL((k_attend<T, DP>), dim3(xcd_grid(c.items)), dim3(kAttendThreads), 0, a.stream, a, c);
+    if (c.wide) hipLaunchKernelGGL((k_attend<T, DP, true>), dim3(xcd_grid(c.items)), dim3(kAttendThreads), 0, a.stream, a, c);
+    else hipLaunchKernelGGL((k_attend<T, DP, false>), dim3(xcd_grid(c.items)), dim3(kAttendThreads), 0, a.stream, a, c);
 }
 
 template <typename T>
@@ -271,11 +270,8 @@ hipError_t launch_attend(const AttendArgs& a, void* ws) {
     Cut c = cut_of(a);
     const size_t e = a.bf16 ? 2 : 4;
     const int ch = a.bf16 ? 8 : 4;
-    c.wide_q = wide_rows(a.q, a.dim, ch, e);
-    c.wide_k = wide_rows(a.k, a.dim, ch, e);
-    c.wide_v = wide_rows(a.v, a.dim, ch, e);
-    c.wide_o = wide_rows(a.out, a.dim, 4, e);
-    c.wide_low = wide_rows(a.low, a.dim, 4, e);
+    c.wide = wide_rows(a.q, a.dim, ch, e) && wide_rows(a.k, a.dim, ch, e) && wide_rows(a.v, a.dim, ch, e) &&
+             wide_rows(a.out, a.dim, 4, e) && wide_rows(a.low, a.dim, 4, e);
     if (c.splits > 1) {
         c.part = (float*)ws;
         c.stat = (float*)((char*)ws + part_bytes(a, c));

@@ -23,10 +23,10 @@ constexpr int kCols = 32 * kAttendWaves;  // rows (dq) or keys (dk, dv) of a wor
 constexpr int kKeys = 32, kQueries = 32;  // keys, queries of a tile
 
 struct GradCut {
-    int64_t rows, row_blocks, key_blocks, items_q, items_k;
+    uint32_t rows, row_blocks, key_blocks, items_q, items_k;
     int32_t splits_q, splits_k;
     float *delta, *part;  // [batch][heads][queries]; [splits][...][dim]
-    uint8_t wide_q, wide_k, wide_v, wide_o, wide_low, wide_do, wide_dq, wide_dk, wide_dv;
+    bool wide;            // rows of all tensors go by 16 bytes (written ones by four entries)
 };
 
 // Workgroups of a CU that the registers are sized for.
@@ -34,7 +34,7 @@ template <typename T, int DP>
 constexpr int kWorkgroups = std::is_same<T, float>::value ? (DP > 32 ? 1 : 2) : (DP > 96 ? 1 : 2);
 
 // dq: each wave holds 32 rows; keys and values come in tiles as in the forward pass.
-template <typename T, int DP>
+template <typename T, int DP, bool W>
 __global__ __launch_bounds__(kAttendThreads, (kWorkgroups<T, DP>)) void k_attend_dq(AttendArgs a, GradCut c) {
     typedef TileOf<T, DP> Tile;
     constexpr int KT = kKeys;
@@ -43,39 +43,37 @@ __global__ __launch_bounds__(kAttendThreads, (kWorkgroups<T, DP>)) void k_attend
     __shared__ float starts[2][KT];
     lds_t* lds = (lds_t*)smem;
 
-    const int64_t id = xcd_item(c.items_q);
+    const uint32_t id = xcd_item(c.items_q);
     if (id >= c.items_q) return;
     const int split = (int)(id % c.splits_q);
-    const int64_t rb = id / c.splits_q % c.row_blocks;
+    const uint32_t rb = id / c.splits_q % c.row_blocks;
     const int bh = (int)(id / c.splits_q / c.row_blocks), b = bh / a.kv_heads, hk = bh % a.kv_heads;
     const int wave = threadIdx.x / kWave, lane = threadIdx.x % kWave, G = a.heads / a.kv_heads;
-    const int64_t row = rb * kCols + wave * 32 + lane % 32;
+    const uint32_t row = rb * kCols + wave * 32 + lane % 32;
     const bool live = row < c.rows;
-    const int64_t i = live ? row / G : 0;
-    const int h = hk * G + (int)(live ? row % G : 0);
-    const T* kp = (const T*)a.k.p + b * a.k.sb + hk * a.k.sh;
-    const T* vp = (const T*)a.v.p + b * a.v.sb + hk * a.v.sh;
-    const int64_t n = key_count(a, b), tiles = (n + KT - 1) / KT;
-    const int64_t t0 = tiles * split / c.splits_q, t1 = tiles * (split + 1) / c.splits_q;
+    const int64_t i = live ? row / (uint32_t)G : 0;
+    const int h = hk * G + (int)(live ? row % (uint32_t)G : 0);
+    const int64_t n = key_count(a, b);
+    const int tiles = (int)((n + KT - 1) / KT);
+    const int t0 = first_tile(tiles, split, c.splits_q), t1 = first_tile(tiles, split + 1, c.splits_q);
 
     typename Tile::Frag qf[Tile::NS], gf[Tile::NS];
-    load_frags<T, DP>((const T*)a.dout.p + b * a.dout.sb + i * a.dout.st + h * a.dout.sh, a.dim, c.wide_do, live, lane, gf);
+    load_frags<T, DP, W>((const T*)a.dout.p + b * a.dout.sb + i * a.dout.st + h * a.dout.sh, a.dim, live, lane, gf);
     // delta from this lane's half of the entries and the other's
     float delta = 0.0f;
-    auto add = [&](const Heads& t, bool wide) {
-        load_frags<T, DP>((const T*)t.p + b * t.sb + i * t.st + h * t.sh, a.dim, wide, live, lane, qf);
+    auto add = [&](const Heads& t) {
+        load_frags<T, DP, W>((const T*)t.p + b * t.sb + i * t.st + h * t.sh, a.dim, live, lane, qf);
 #pragma unroll
         for (int s = 0; s < Tile::NS; ++s)
 #pragma unroll
             for (int j = 0; j < Tile::CH; ++j) delta = fmaf((float)gf[s][j], (float)qf[s][j], delta);
     };
-    add(a.out, c.wide_o);
-    if (a.low.p) add(a.low, c.wide_low);
+    add(a.out);
+    if (a.low.p) add(a.low);
     delta += other_half(delta);
-    load_frags<T, DP>((const T*)a.q.p + b * a.q.sb + i * a.q.st + h * a.q.sh, a.dim, c.wide_q, live, lane, qf);
-    if (a.scale2 < 0.0f)
-#pragma unroll
-        for (int s = 0; s < Tile::NS; ++s) qf[s] = -qf[s];
+    load_frags<T, DP, W>((const T*)a.q.p + b * a.q.sb + i * a.q.st + h * a.q.sh, a.dim, live, lane, qf);
+    Mat<T>::template sign<Tile::NS>(qf, a.scale2);
+    Mat<T>::template sign<Tile::NS>(gf, 1.0f);
     const int64_t at = ((int64_t)b * a.heads + h) * a.queries + i;
     const float m = a.stats[2 * at], l = a.stats[2 * at + 1];
     const float neg = l == 0.0f ? -INFINITY : -m, inv = l == 0.0f ? 0.0f : 1.0f / l;
@@ -90,43 +88,50 @@ __global__ __launch_bounds__(kAttendThreads, (kWorkgroups<T, DP>)) void k_attend
         for (int r = 0; r < 16; ++r) dq[d][r] = 0.0f;
 
     St sk, sv;
-    float start[St::N], start1 = 0.0f;
-    auto load = [&](int64_t t) {
-        sk.load(kp, a.k.st, t * KT, n, a.dim, c.wide_k, wave, lane);
-        sv.load(vp, a.v.st, t * KT, n, a.dim, c.wide_v, wave, lane);
-        auto start_at = [&](int64_t j) {
-            return j >= n ? -INFINITY : a.bias ? start_of(a.bias[b * a.bias_sb + j], inv_scale) : 0.0f;
-        };
-#pragma unroll
-        for (int u = 0; u < St::N; ++u) start[u] = start_at(t * KT + St::row_of(wave, lane, u));
-        if (threadIdx.x < KT) start1 = start_at(t * KT + threadIdx.x);
+    float bias = 0.0f;  // of the staged row
+    int left = 0;       // rows of the staged tile that exist
+    const Rows<T> keys{(const T*)a.k.p + b * a.k.sb + hk * a.k.sh, a.k.st, n, a.dim};
+    const Rows<T> vals{(const T*)a.v.p + b * a.v.sb + hk * a.v.sh, a.v.st, n, a.dim};
+    const int srow = St::row_of(wave, lane);
+    sk.template plan<W>(keys, wave, lane);
+    sv.template plan<W>(vals, wave, lane);
+    auto load = [&](int t) {
+        sk.template load<W>(keys, (int64_t)t * KT, wave, lane);
+        sv.template load<W>(vals, (int64_t)t * KT, wave, lane);
+        left = (int)(n - (int64_t)t * KT);
+        if (a.bias) bias = a.bias[b * a.bias_sb + (int64_t)t * KT + min(srow, left - 1)];
     };
     auto store = [&](int buf) {
-        auto keep = [&](int u) { return start[u] != -INFINITY; };
+        const float start = srow < left ? start_of(bias, inv_scale) : -INFINITY;
+        const bool keep = start != -INFINITY;
         sk.store(lds + buf * 2 * St::kBytes, wave, lane, keep);
         sv.store(lds + (buf * 2 + 1) * St::kBytes, wave, lane, keep);
-        if (threadIdx.x < KT) starts[buf][threadIdx.x] = start1;
+        if (lane % 4 == 0) starts[buf][srow] = start;  // (two waves to a row: the same value)
     };
     if (t0 < t1) {
         load(t0);
         store(0);
     }
     __syncthreads();
-    for (int64_t t = t0; t < t1; ++t) {
-        const int buf = (int)(t - t0) & 1;
+    for (int t = t0; t < t1; ++t) {
+        const int buf = (t - t0) & 1;
         const bool more = t + 1 < t1;
         if (more) load(t + 1);
         const lds_t* kt = lds + buf * 2 * St::kBytes;
         const lds_t* vt = kt + St::kBytes;
-        f16 s, dp;
+        f16 s;
+        if (!a.bias && (int64_t)(t + 1) * KT <= n) {
+            s = Tile::scores(kt, ln, 0, qf);
+        } else {
 #pragma unroll
-        for (int q = 0; q < 4; ++q) {
-            const f4 v = *(const f4*)&starts[buf][8 * q + 4 * (lane / 32)];
+            for (int q = 0; q < 4; ++q) {
+                const f4 v = *(const f4*)&starts[buf][8 * q + 4 * (lane / 32)];
 #pragma unroll
-            for (int r = 0; r < 4; ++r) s[4 * q + r] = v[r], dp[4 * q + r] = 0.0f;
+                for (int r = 0; r < 4; ++r) s[4 * q + r] = v[r];
+            }
+            s = Tile::scores(kt, ln, 0, qf, s);
         }
-        s = Tile::scores(kt, ln, 0, qf, s);
-        dp = Tile::scores(vt, ln, 0, gf, dp);
+        const f16 dp = Tile::scores(vt, ln, 0, gf);
 #pragma unroll
         for (int r = 0; r < 16; ++r) s[r] = __builtin_amdgcn_exp2f(fmaf(s[r], scale2, neg)) * (dp[r] - delta);
         Tile::values(kt, ln, 0, s, dq);
@@ -137,15 +142,15 @@ __global__ __launch_bounds__(kAttendThreads, (kWorkgroups<T, DP>)) void k_attend
     const float f = inv * a.scale;
     if (c.splits_q > 1) {
         const int64_t all = (int64_t)a.batch * a.kv_heads * c.rows;
-        store_column<float, DP>(c.part + (split * all + (int64_t)bh * c.rows + row) * a.dim, dq, f, a.dim, a.dim % 4 == 0, lane);
+        store_column<float, DP, W>(c.part + (split * all + (int64_t)bh * c.rows + row) * a.dim, dq, f, a.dim, lane);
     } else {
-        store_column<T, DP>((T*)a.dq.p + b * a.dq.sb + i * a.dq.st + h * a.dq.sh, dq, f, a.dim, c.wide_dq, lane);
+        store_column<T, DP, W>((T*)a.dq.p + b * a.dq.sb + i * a.dq.st + h * a.dq.sh, dq, f, a.dim, lane);
     }
 }
 
 // dk, dv: each wave holds 32 keys; queries and output gradients of every head
 // of the group come in tiles.
-template <typename T, int DP>
+template <typename T, int DP, bool W>
 __global__ __launch_bounds__(kAttendThreads, (kWorkgroups<T, DP>)) void k_attend_dkv(AttendArgs a, GradCut c) {
     typedef TileOf<T, DP> Tile;
     constexpr int QT = kQueries;
@@ -154,24 +159,23 @@ __global__ __launch_bounds__(kAttendThreads, (kWorkgroups<T, DP>)) void k_attend
     __shared__ float row_c[2][3][QT];  // -reference, 1 / sum, delta of the tile's rows
     lds_t* lds = (lds_t*)smem;
 
-    const int64_t id = xcd_item(c.items_k);
+    const uint32_t id = xcd_item(c.items_k);
     if (id >= c.items_k) return;
     const int split = (int)(id % c.splits_k);
-    const int64_t kb = id / c.splits_k % c.key_blocks;
+    const uint32_t kb = id / c.splits_k % c.key_blocks;
     const int bh = (int)(id / c.splits_k / c.key_blocks), b = bh / a.kv_heads, hk = bh % a.kv_heads;
     const int wave = threadIdx.x / kWave, lane = threadIdx.x % kWave, G = a.heads / a.kv_heads;
-    const int64_t j = kb * kCols + wave * 32 + lane % 32, n = key_count(a, b);
+    const int64_t j = (int64_t)kb * kCols + wave * 32 + lane % 32, n = key_count(a, b);
     const float scale2 = fabsf(a.scale2);
     const float start = j >= n ? -INFINITY : a.bias ? start_of(a.bias[b * a.bias_sb + j], 1.0f / fabsf(a.scale)) : 0.0f;
     const bool live = start != -INFINITY;
     const int64_t jr = live ? j : 0;
 
     typename Tile::Frag kf[Tile::NS], vf[Tile::NS];
-    load_frags<T, DP>((const T*)a.k.p + b * a.k.sb + jr * a.k.st + hk * a.k.sh, a.dim, c.wide_k, live, lane, kf);
-    load_frags<T, DP>((const T*)a.v.p + b * a.v.sb + jr * a.v.st + hk * a.v.sh, a.dim, c.wide_v, live, lane, vf);
-    if (a.scale2 < 0.0f)
-#pragma unroll
-        for (int s = 0; s < Tile::NS; ++s) kf[s] = -kf[s];
+    load_frags<T, DP, W>((const T*)a.k.p + b * a.k.sb + jr * a.k.st + hk * a.k.sh, a.dim, live, lane, kf);
+    load_frags<T, DP, W>((const T*)a.v.p + b * a.v.sb + jr * a.v.st + hk * a.v.sh, a.dim, live, lane, vf);
+    Mat<T>::template sign<Tile::NS>(kf, a.scale2);
+    Mat<T>::template sign<Tile::NS>(vf, 1.0f);
     const typename Tile::Lane ln = Tile::lane_of(lane);
     f16 dk[DP / 32], dv[DP / 32];
 #pragma unroll
@@ -179,16 +183,22 @@ __global__ __launch_bounds__(kAttendThreads, (kWorkgroups<T, DP>)) void k_attend
 #pragma unroll
         for (int r = 0; r < 16; ++r) dk[d][r] = dv[d][r] = 0.0f;
 
-    const int64_t tiles = (a.queries + QT - 1) / QT, steps = kb * kCols < n ? tiles * G : 0;
-    const int64_t t0 = steps * split / c.splits_k, t1 = steps * (split + 1) / c.splits_k;
+    // The tiles of the group's heads one after the other.
+    const int tiles = (int)((a.queries + QT - 1) / QT), steps = (int64_t)kb * kCols < n ? tiles * G : 0;
+    const int t0 = first_tile(steps, split, c.splits_k), t1 = first_tile(steps, split + 1, c.splits_k);
     St sq, sg;
     float r0 = 0.0f, r1 = 0.0f, r2 = 0.0f;
     int64_t left = 0;  // rows of the staged tile that exist
-    auto load = [&](int64_t t) {
-        const int h = hk * G + (int)(t / tiles);
-        const int64_t i0 = t % tiles * QT;
-        sq.load((const T*)a.q.p + b * a.q.sb + h * a.q.sh, a.q.st, i0, a.queries, a.dim, c.wide_q, wave, lane);
-        sg.load((const T*)a.dout.p + b * a.dout.sb + h * a.dout.sh, a.dout.st, i0, a.queries, a.dim, c.wide_do, wave, lane);
+    Rows<T> qs{nullptr, a.q.st, a.queries, a.dim}, gs{nullptr, a.dout.st, a.queries, a.dim};
+    sq.template plan<W>(qs, wave, lane);
+    sg.template plan<W>(gs, wave, lane);
+    auto load = [&](int t) {
+        const int h = hk * G + t / tiles;
+        const int64_t i0 = (int64_t)(t % tiles) * QT;
+        qs.p = (const T*)a.q.p + b * a.q.sb + h * a.q.sh;
+        gs.p = (const T*)a.dout.p + b * a.dout.sb + h * a.dout.sh;
+        sq.template load<W>(qs, i0, wave, lane);
+        sg.template load<W>(gs, i0, wave, lane);
         left = a.queries - i0;
         if (threadIdx.x < QT) {
             r0 = -INFINITY;
@@ -202,7 +212,7 @@ __global__ __launch_bounds__(kAttendThreads, (kWorkgroups<T, DP>)) void k_attend
         }
     };
     auto store = [&](int buf) {
-        auto keep = [&](int u) { return St::row_of(wave, lane, u) < left; };
+        const bool keep = St::row_of(wave, lane) < left;
         sq.store(lds + buf * 2 * St::kBytes, wave, lane, keep);
         sg.store(lds + (buf * 2 + 1) * St::kBytes, wave, lane, keep);
         if (threadIdx.x < QT) {
@@ -216,17 +226,17 @@ __global__ __launch_bounds__(kAttendThreads, (kWorkgroups<T, DP>)) void k_attend
         store(0);
     }
     __syncthreads();
-    for (int64_t t = t0; t < t1; ++t) {
-        const int buf = (int)(t - t0) & 1;
+    for (int t = t0; t < t1; ++t) {
+        const int buf = (t - t0) & 1;
         const bool more = t + 1 < t1;
         if (more) load(t + 1);
         const lds_t* qt = lds + buf * 2 * St::kBytes;
         const lds_t* gt = qt + St::kBytes;
-        f16 s, dp;
+        f16 s;
 #pragma unroll
-        for (int r = 0; r < 16; ++r) s[r] = start, dp[r] = 0.0f;
+        for (int r = 0; r < 16; ++r) s[r] = start;
         s = Tile::scores(qt, ln, 0, kf, s);
-        dp = Tile::scores(gt, ln, 0, vf, dp);
+        f16 dp = Tile::scores(gt, ln, 0, vf);
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
             const int at = 8 * q + 4 * (lane / 32);
@@ -252,11 +262,11 @@ __global__ __launch_bounds__(kAttendThreads, (kWorkgroups<T, DP>)) void k_attend
     if (j >= a.keys) return;
     if (c.splits_k > 1) {
         const int64_t all = (int64_t)a.batch * a.kv_heads * a.keys, at = split * 2 * all + (int64_t)bh * a.keys + j;
-        store_column<float, DP>(c.part + at * a.dim, dk, a.scale, a.dim, a.dim % 4 == 0, lane);
-        store_column<float, DP>(c.part + (at + all) * a.dim, dv, 1.0f, a.dim, a.dim % 4 == 0, lane);
+        store_column<float, DP, W>(c.part + at * a.dim, dk, a.scale, a.dim, lane);
+        store_column<float, DP, W>(c.part + (at + all) * a.dim, dv, 1.0f, a.dim, lane);
     } else {
-        store_column<T, DP>((T*)a.dk.p + b * a.dk.sb + j * a.dk.st + hk * a.dk.sh, dk, a.scale, a.dim, c.wide_dk, lane);
-        store_column<T, DP>((T*)a.dv.p + b * a.dv.sb + j * a.dv.st + hk * a.dv.sh, dv, 1.0f, a.dim, c.wide_dv, lane);
+        store_column<T, DP, W>((T*)a.dk.p + b * a.dk.sb + j * a.dk.st + hk * a.dk.sh, dk, a.scale, a.dim, lane);
+        store_column<T, DP, W>((T*)a.dv.p + b * a.dv.sb + j * a.dv.st + hk * a.dv.sh, dv, 1.0f, a.dim, lane);
     }
 }
 
@@ -287,15 +297,15 @@ int32_t parts(int64_t blocks, int64_t steps, int64_t least) {
 GradCut cut_of(const AttendArgs& a) {
     GradCut c{};
     const int G = a.heads / a.kv_heads;
-    c.rows = a.queries * G;
+    c.rows = (uint32_t)(a.queries * G);
     c.row_blocks = (c.rows + kCols - 1) / kCols;
-    c.key_blocks = (a.keys + kCols - 1) / kCols;
-    const int64_t bq = c.row_blocks * a.batch * a.kv_heads, bk = c.key_blocks * a.batch * a.kv_heads;
+    c.key_blocks = (uint32_t)((a.keys + kCols - 1) / kCols);
+    const int64_t bq = (int64_t)c.row_blocks * a.batch * a.kv_heads, bk = (int64_t)c.key_blocks * a.batch * a.kv_heads;
     // Parts of at least eight tiles, as many as give every CU two workgroups.
     c.splits_q = parts(bq, (a.keys + kKeys - 1) / kKeys, 8);
     c.splits_k = parts(bk, (a.queries + kQueries - 1) / kQueries * G, 8);
-    c.items_q = bq * c.splits_q;
-    c.items_k = bk * c.splits_k;
+    c.items_q = (uint32_t)(bq * c.splits_q);
+    c.items_k = (uint32_t)(bk * c.splits_k);
     return c;
 }
 
@@ -304,11 +314,13 @@ size_t delta_bytes(const AttendArgs& a) { return round256((size_t)a.batch * a.he
 
 template <typename T, int DP>
 void launch_dq(const AttendArgs& a, const GradCut& c) {
-    hipLaunchKernelGGL((k_attend_dq<T, DP>), dim3(xcd_grid(c.items_q)), dim3(kAttendThreads), 0, a.stream, a, c);
+    if (c.wide) hipLaunchKernelGGL((k_attend_dq<T, DP, true>), dim3(xcd_grid(c.items_q)), dim3(kAttendThreads), 0, a.stream, a, c);
+    else hipLaunchKernelGGL((k_attend_dq<T, DP, false>), dim3(xcd_grid(c.items_q)), dim3(kAttendThreads), 0, a.stream, a, c);
 }
 template <typename T, int DP>
 void launch_dkv(const AttendArgs& a, const GradCut& c) {
-    hipLaunchKernelGGL((k_attend_dkv<T, DP>), dim3(xcd_grid(c.items_k)), dim3(kAttendThreads), 0, a.stream, a, c);
+    if (c.wide) hipLaunchKernelGGL((k_attend_dkv<T, DP, true>), dim3(xcd_grid(c.items_k)), dim3(kAttendThreads), 0, a.stream, a, c);
+    else hipLaunchKernelGGL((k_attend_dkv<T, DP, false>), dim3(xcd_grid(c.items_k)), dim3(kAttendThreads), 0, a.stream, a, c);
 }
 
 template <typename T>
@@ -359,15 +371,9 @@ hipError_t launch_attend_grad(const AttendArgs& a, void* ws) {
     GradCut c = cut_of(a);
     const size_t e = a.bf16 ? 2 : 4;
     const int ch = a.bf16 ? 8 : 4;
-    c.wide_q = wide_rows(a.q, a.dim, ch, e);
-    c.wide_k = wide_rows(a.k, a.dim, ch, e);
-    c.wide_v = wide_rows(a.v, a.dim, ch, e);
-    c.wide_o = wide_rows(a.out, a.dim, ch, e);
-    c.wide_low = wide_rows(a.low, a.dim, ch, e);
-    c.wide_do = wide_rows(a.dout, a.dim, ch, e);
-    c.wide_dq = wide_rows(a.dq, a.dim, 4, e);
-    c.wide_dk = wide_rows(a.dk, a.dim, 4, e);
-    c.wide_dv = wide_rows(a.dv, a.dim, 4, e);
+    c.wide = true;
+    for (const Heads* t : {&a.q, &a.k, &a.v, &a.out, &a.low, &a.dout}) c.wide = c.wide && wide_rows(*t, a.dim, ch, e);
+    for (const Heads* t : {&a.dq, &a.dk, &a.dv}) c.wide = c.wide && wide_rows(*t, a.dim, 4, e);
     c.delta = (float*)ws;
     c.part = (float*)((char*)ws + delta_bytes(a));
     return a.bf16 ? run<__bf16>(a, c) : run<float>(a, c);

@@ -266,7 +266,10 @@ void check_attend(const disco_heads_t* q, const disco_heads_t* k, const disco_he
     if (q->batch != k->batch || q->dim != k->dim) refuse(DISCO_ERR_SHAPE, "q and k differ in batch or dim");
     if (k->heads < 1 || q->heads < 1 || q->heads % k->heads)
         refuse(DISCO_ERR_SHAPE, "the heads of q must be a multiple of those of k and v");
-    if (q->batch * q->heads > 65535 * 8) refuse(DISCO_ERR_SHAPE, "batch * heads out of range");
+    // (the kernels count the rows of one kv head, tiles and workgroups in 32 bits)
+    if (q->batch * q->heads > 65535 * 8 || q->tokens * q->heads >= kMaxRows || k->tokens * k->heads >= kMaxRows * 128 ||
+        q->batch * q->tokens * q->heads >= kMaxRows * 16 || k->batch * k->tokens * k->heads >= kMaxRows * 16)
+        refuse(DISCO_ERR_SHAPE, "batch * tokens * heads out of range");
     const double scale = o && o->scale != 0.0 ? o->scale : 1.0 / std::sqrt((double)q->dim);
     if (!std::isfinite(scale)) refuse(DISCO_ERR_INVALID_ARGUMENT, "scale must be finite");
     a->batch = (int32_t)q->batch;
