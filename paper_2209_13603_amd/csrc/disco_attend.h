@@ -16,11 +16,11 @@
 // v_mfma_f32_32x32x2_f32 (its operands are single values, so nothing needs to be
 // transposed) and is exact to fp32 rounding.
 //
-// LDS tile: chunks of 16 bytes, 16 rows x 4 chunks to a segment of 1 KB, at
-// (c % 4) * 256 + ((row % 16) ^ 4 (c % 4)) * 16.  Row reads (a lane a row, 16
-// bytes), transposed reads (4 rows x 16 entries) and the staging writes (4 lanes
-// a row) all spread over the banks, and every address is a lane's own offset plus a
-// constant.
+// LDS tile: chunks of 16 bytes, 16 rows x 4 chunks to a segment of 1 KB, chunk c
+// of row r at (r % 16) * 64 + ((c % 4) ^ (r / 4 % 4)) * 16.  Row reads (a lane a
+// row, 16 bytes), transposed reads (4 rows x 16 entries) and the staging writes (4
+// lanes a row) all spread over the banks, and every address is a lane's own
+// offset plus a constant.
 #pragma once
 #include <hip/hip_runtime.h>
 
@@ -128,17 +128,17 @@ struct TileOf {
         const int h = lane / 32, i = lane % 16;
         Lane o;
         const uint32_t r = (uint32_t)((lane % 32) / 16) * kStep16;
-        o.even = r + h * 256 + ((i ^ (4 * h)) * 16);
-        o.odd = r + (2 + h) * 256 + ((i ^ (8 + 4 * h)) * 16);
+        o.even = r + i * 64 + ((h ^ (i / 4)) * 16);
+        o.odd = r + i * 64 + (((2 + h) ^ (i / 4)) * 16);
         if (std::is_same<T, __bf16>::value) {
             const int cm = 2 * ((lane / 16) % 2) + (i % 4) / 2, row = 4 * h + i / 4;
-            o.t0 = cm * 256 + ((row ^ (4 * cm)) * 16) + (i % 2) * 8;
-            o.t1 = cm * 256 + (((row + 8) ^ (4 * cm)) * 16) + (i % 2) * 8;
+            o.t0 = row * 64 + ((cm ^ h) * 16) + (i % 2) * 8;
+            o.t1 = (row + 8) * 64 + ((cm ^ (2 + h)) * 16) + (i % 2) * 8;
         } else {
             const int cm = (lane / 4) % 4;
-            const uint32_t base = ((lane % 32) / 16) * 1024 + cm * 256 + (lane % 4) * 4;
-            o.t0 = base + (((4 * h) ^ (4 * cm)) * 16);
-            o.t1 = base + (((8 + 4 * h) ^ (4 * cm)) * 16);
+            const uint32_t base = ((lane % 32) / 16) * 1024 + (lane % 4) * 4;
+            o.t0 = base + 4 * h * 64 + ((cm ^ h) * 16);
+            o.t1 = base + (8 + 4 * h) * 64 + ((cm ^ (2 + h)) * 16);
         }
         return o;
     }
@@ -150,6 +150,20 @@ struct TileOf {
     static __device__ __forceinline__ f16 scores(const lds_t* tile, const Lane& l, int k, const Frag (&f)[NS], f16 c) {
 #pragma unroll
         for (int s = 0; s < NS; ++s) c = Mat<T>::scores(row(tile, l, k, s), f[s], c);
+        return c;
+    }
+    // Fragments that each lane keeps in LDS for itself (NS KB a wave) where they
+    // would not fit the registers.
+    static __device__ __forceinline__ void keep(lds_t* at, int lane, const Frag (&f)[NS]) {
+        typedef __attribute__((address_space(3))) Frag F;
+#pragma unroll
+        for (int s = 0; s < NS; ++s) *(F*)(at + s * 1024 + lane * 16) = f[s];
+    }
+    static __device__ __forceinline__ f16 scores_kept(const lds_t* tile, const Lane& l, int k, const lds_t* at, int lane,
+                                                      f16 c) {
+        typedef __attribute__((address_space(3))) const Frag F;
+#pragma unroll
+        for (int s = 0; s < NS; ++s) c = Mat<T>::scores(row(tile, l, k, s), *(F*)(at + s * 1024 + lane * 16), c);
         return c;
     }
     static __device__ __forceinline__ f16 scores(const lds_t* tile, const Lane& l, int k, const Frag (&f)[NS]) {
@@ -187,7 +201,7 @@ struct TileOf {
                 for (int i = 0; i < 16; ++i) t[i] = 0.0f;
 #pragma unroll
                 for (int i = 0; i < 16; ++i) {
-                    const uint32_t at = 2 * d * 1024 + (2 * k + i / 8) * kStep16 + (i % 4) * 16;
+                    const uint32_t at = 2 * d * 1024 + (2 * k + i / 8) * kStep16 + (i % 4) * 64;
                     const float v = *(V*)(tile + ((i / 4) % 2 ? l.t1 : l.t0) + at);
                     t = __builtin_amdgcn_mfma_f32_32x32x2f32(v, p[i], t, 0, 0, 0);
                 }
@@ -277,8 +291,8 @@ struct Stage {
 #pragma unroll
             for (int u = 0; u < N; ++u) v[u] = keep ? v[u] : u4{0u, 0u, 0u, 0u};
         }
-        lds_t* to = tile + wave / kHalves * Tile::kStep16 + wave % kHalves * 1024 + (lane % 4) * 256 +
-                    (((lane / 4) ^ (4 * (lane % 4))) * 16);
+        lds_t* to = tile + wave / kHalves * Tile::kStep16 + wave % kHalves * 1024 + (lane / 4) * 64 +
+                    (((lane % 4) ^ (lane / 16)) * 16);
 #pragma unroll
         for (int u = 0; u < N; ++u)
             if (has(wave, u)) *(V*)(to + u * kHalves * 1024) = v[u];

@@ -31,7 +31,11 @@ struct GradCut {
 
 // Workgroups of a CU that the registers are sized for.
 template <typename T, int DP>
-constexpr int kWorkgroups = std::is_same<T, float>::value ? (DP > 32 ? 1 : 2) : (DP > 96 ? 1 : 2);
+constexpr int kWorkgroups = std::is_same<T, float>::value && DP > 64 ? 1 : 2;
+// The key fragments of the dk, dv kernel stay in LDS where the registers
+// (fragments of k and v, sums of dk and dv) would not hold them.
+template <typename T, int DP>
+constexpr bool kKeysInLds = DP > (std::is_same<T, float>::value ? 32 : 96);
 
 // dq: each wave holds 32 rows; keys and values come in tiles as in the forward pass.
 template <typename T, int DP, bool W>
@@ -156,6 +160,8 @@ __global__ __launch_bounds__(kAttendThreads, (kWorkgroups<T, DP>)) void k_attend
     constexpr int QT = kQueries;
     typedef Stage<T, DP, QT> St;
     __shared__ __align__(16) char smem[2 * 2 * St::kBytes];
+    constexpr bool kept = kKeysInLds<T, DP>;
+    __shared__ __align__(16) char kmem[kept ? kAttendWaves * Tile::NS * 1024 : 16];
     __shared__ float row_c[2][3][QT];  // -reference, 1 / sum, delta of the tile's rows
     lds_t* lds = (lds_t*)smem;
 
@@ -176,6 +182,8 @@ __global__ __launch_bounds__(kAttendThreads, (kWorkgroups<T, DP>)) void k_attend
     load_frags<T, DP, W>((const T*)a.v.p + b * a.v.sb + jr * a.v.st + hk * a.v.sh, a.dim, live, lane, vf);
     Mat<T>::template sign<Tile::NS>(kf, a.scale2);
     Mat<T>::template sign<Tile::NS>(vf, 1.0f);
+    lds_t* const mine = (lds_t*)kmem + wave * Tile::NS * 1024;
+    if constexpr (kept) Tile::keep(mine, lane, kf);
     const typename Tile::Lane ln = Tile::lane_of(lane);
     f16 dk[DP / 32], dv[DP / 32];
 #pragma unroll
@@ -235,7 +243,8 @@ __global__ __launch_bounds__(kAttendThreads, (kWorkgroups<T, DP>)) void k_attend
         f16 s;
 #pragma unroll
         for (int r = 0; r < 16; ++r) s[r] = start;
-        s = Tile::scores(qt, ln, 0, kf, s);
+        if constexpr (kept) s = Tile::scores_kept(qt, ln, 0, mine, lane, s);
+        else s = Tile::scores(qt, ln, 0, kf, s);
         f16 dp = Tile::scores(gt, ln, 0, vf);
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
