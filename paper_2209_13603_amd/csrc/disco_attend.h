@@ -223,12 +223,17 @@ __device__ __forceinline__ u4 load_chunk(const T* row, int c, int D) {
     return __builtin_bit_cast(u4, f);
 }
 
-// The rows that tiles are read from: D entries `stride` entries apart.
+// Where the next tile of a matrix begins: rows of D entries, `stride` entries apart.
 template <typename T>
-struct Rows {
+struct Cursor {
     const T* p;
-    int64_t stride, rows;
+    int64_t stride;
+    int left;  // rows from p on
     int D;
+    __device__ __forceinline__ void advance(int rows) {
+        p += rows * stride;
+        left -= rows;
+    }
 };
 
 // A tile of ROWS rows on its way from memory to LDS.  Each thread holds chunks
@@ -249,38 +254,27 @@ struct Stage {
     }
     // W: 16-byte loads through a buffer over the tile's rows, to which the
     // entries beyond D and the rows beyond the last are out of range and come
-    // as zeros: off is all that a thread needs.  Otherwise entry by entry, the
-    // rows beyond the last coming as the last.
-    uint32_t off[N];
+    // as zeros.  Otherwise entry by entry, the rows beyond the last coming as
+    // the last.
     template <bool W>
-    __device__ __forceinline__ void plan(const Rows<T>& m, int wave, int lane) {
+    __device__ __forceinline__ void load(const Cursor<T>& m, int wave, int lane) {
+        const int c = (seg(wave, 0) * 4 + lane % 4) * Mat<T>::CH;
+        constexpr int step = kHalves * 4 * Mat<T>::CH;
         if constexpr (W) {
+            const int bytes = ((min(m.left, ROWS) - 1) * (int)m.stride + m.D) * (int)sizeof(T);
+            const __amdgpu_buffer_rsrc_t r = __builtin_amdgcn_make_buffer_rsrc(const_cast<T*>(m.p), (short)0, bytes, 0x00020000);
+            const int off = (row_of(wave, lane) * (int)m.stride + c) * (int)sizeof(T);
 #pragma unroll
             for (int u = 0; u < N; ++u) {
-                const int c = (seg(wave, u) * 4 + lane % 4) * Mat<T>::CH;
-                off[u] = has(wave, u) && c < m.D ? (uint32_t)(row_of(wave, lane) * (int)m.stride + c) * (uint32_t)sizeof(T)
-                                                 : 0x80000000u;
+                const bool in = has(wave, u) && c + u * step < m.D;
+                v[u] = __builtin_bit_cast(u4, __builtin_amdgcn_raw_buffer_load_b128(
+                                                  r, in ? off + u * step * (int)sizeof(T) : (int)0x80000000, 0, 0));
             }
-        }
-    }
-    template <bool W>
-    __device__ __forceinline__ void load(const Rows<T>& m, int64_t row0, int wave, int lane) {
-        const int64_t left = m.rows - 1 - row0;
-        if constexpr (W) {
-            const int64_t bytes = (left * m.stride + m.D) * (int64_t)sizeof(T);
-            const __amdgpu_buffer_rsrc_t r =
-                __builtin_amdgcn_make_buffer_rsrc(const_cast<T*>(m.p + row0 * m.stride), (short)0,
-                                                  bytes < 0x7fffffff ? (int)bytes : 0x7fffffff, 0x00020000);
-#pragma unroll
-            for (int u = 0; u < N; ++u)
-                v[u] = __builtin_bit_cast(u4, __builtin_amdgcn_raw_buffer_load_b128(r, (int)off[u], 0, 0));
         } else {
-            const int r = min(row_of(wave, lane), (int)min(left, (int64_t)ROWS));
-            const int c = (seg(wave, 0) * 4 + lane % 4) * Mat<T>::CH;
-            constexpr int step = kHalves * 4 * Mat<T>::CH;
+            const int r = min(row_of(wave, lane), m.left - 1);
 #pragma unroll
             for (int u = 0; u < N; ++u)
-                if (has(wave, u)) v[u] = load_chunk<T, false>(m.p + (row0 + r) * m.stride, c + u * step, m.D);
+                if (has(wave, u)) v[u] = load_chunk<T, false>(m.p + r * m.stride, c + u * step, m.D);
         }
     }
     // keep: whether this thread's row counts; zeros otherwise, so that whatever

@@ -74,16 +74,21 @@ __global__ __launch_bounds__(kAttendThreads, (kWorkgroups<T, DP>)) void k_attend
     St sk, sv;
     float bias = 0.0f;  // of the staged row
     int left = 0;       // rows of the staged tile that exist
-    const Rows<T> keys{(const T*)a.k.p + b * a.k.sb + hk * a.k.sh, a.k.st, n, a.dim};
-    const Rows<T> vals{(const T*)a.v.p + b * a.v.sb + hk * a.v.sh, a.v.st, n, a.dim};
+    const int64_t key0 = (int64_t)t0 * KT;
+    Cursor<T> keys{(const T*)a.k.p + b * a.k.sb + hk * a.k.sh + key0 * a.k.st, a.k.st, (int)(n - key0), a.dim};
+    Cursor<T> vals{(const T*)a.v.p + b * a.v.sb + hk * a.v.sh + key0 * a.v.st, a.v.st, (int)(n - key0), a.dim};
+    const float* biases = a.bias ? a.bias + b * a.bias_sb + key0 : nullptr;
     const int srow = St::row_of(wave, lane);
-    sk.template plan<W>(keys, wave, lane);
-    sv.template plan<W>(vals, wave, lane);
-    auto load = [&](int t) {
-        sk.template load<W>(keys, (int64_t)t * KT, wave, lane);
-        sv.template load<W>(vals, (int64_t)t * KT, wave, lane);
-        left = (int)(n - (int64_t)t * KT);
-        if (a.bias) bias = a.bias[b * a.bias_sb + (int64_t)t * KT + min(srow, left - 1)];
+    auto load = [&] {
+        sk.template load<W>(keys, wave, lane);
+        sv.template load<W>(vals, wave, lane);
+        left = keys.left;
+        if (biases) {
+            bias = biases[min(srow, left - 1)];
+            biases += KT;
+        }
+        keys.advance(KT);
+        vals.advance(KT);
     };
     auto store = [&](int buf) {
         const float start = srow < left ? start_of(bias, inv_scale) : -INFINITY;
@@ -93,18 +98,18 @@ __global__ __launch_bounds__(kAttendThreads, (kWorkgroups<T, DP>)) void k_attend
         if (lane % 4 == 0) starts[buf][srow] = start;  // (two waves to a row: the same value)
     };
     if (t0 < t1) {
-        load(t0);
+        load();
         store(0);
     }
     __syncthreads();
     for (int t = t0; t < t1; ++t) {
         const int buf = (t - t0) & 1;
-        const bool more = t + 1 < t1;
-        if (more) load(t + 1);
+        const bool more = t + 1 < t1, plain = !a.bias && left >= KT;
+        if (more) load();
         const lds_t* kt = lds + buf * 2 * St::kBytes;
         const lds_t* vt = kt + St::kBytes;
         f16 s[NK];
-        if (!a.bias && (int64_t)(t + 1) * KT <= n) {
+        if (plain) {
 #pragma unroll
             for (int k = 0; k < NK; ++k) s[k] = Tile::scores(kt, ln, k, qf);
         } else {

@@ -25,8 +25,9 @@ constexpr int kKeys = 32, kQueries = 32;  // keys, queries of a tile
 struct GradCut {
     uint32_t rows, row_blocks, key_blocks, items_q, items_k;
     int32_t splits_q, splits_k;
-    float *delta, *part;  // [batch][heads][queries]; [splits][...][dim]
-    bool wide;            // rows of all tensors go by 16 bytes (written ones by four entries)
+    f4* row_c;    // [batch][heads][queries]: -reference, 1 / sum, delta, written with dq for dk and dv
+    float* part;  // [splits][...][dim]
+    bool wide;    // rows of all tensors go by 16 bytes (written ones by four entries)
 };
 
 // Workgroups of a CU that the registers are sized for.
@@ -81,7 +82,7 @@ __global__ __launch_bounds__(kAttendThreads, (kWorkgroups<T, DP>)) void k_attend
     const int64_t at = ((int64_t)b * a.heads + h) * a.queries + i;
     const float m = a.stats[2 * at], l = a.stats[2 * at + 1];
     const float neg = l == 0.0f ? -INFINITY : -m, inv = l == 0.0f ? 0.0f : 1.0f / l;
-    if (split == 0 && live && lane < 32) c.delta[at] = delta;
+    if (split == 0 && live && lane < 32) c.row_c[at] = f4{neg, inv, delta, 0.0f};
     const float scale2 = fabsf(a.scale2), inv_scale = 1.0f / fabsf(a.scale);
     const typename Tile::Lane ln = Tile::lane_of(lane);
 
@@ -94,16 +95,21 @@ __global__ __launch_bounds__(kAttendThreads, (kWorkgroups<T, DP>)) void k_attend
     St sk, sv;
     float bias = 0.0f;  // of the staged row
     int left = 0;       // rows of the staged tile that exist
-    const Rows<T> keys{(const T*)a.k.p + b * a.k.sb + hk * a.k.sh, a.k.st, n, a.dim};
-    const Rows<T> vals{(const T*)a.v.p + b * a.v.sb + hk * a.v.sh, a.v.st, n, a.dim};
+    const int64_t key0 = (int64_t)t0 * KT;
+    Cursor<T> keys{(const T*)a.k.p + b * a.k.sb + hk * a.k.sh + key0 * a.k.st, a.k.st, (int)(n - key0), a.dim};
+    Cursor<T> vals{(const T*)a.v.p + b * a.v.sb + hk * a.v.sh + key0 * a.v.st, a.v.st, (int)(n - key0), a.dim};
+    const float* biases = a.bias ? a.bias + b * a.bias_sb + key0 : nullptr;
     const int srow = St::row_of(wave, lane);
-    sk.template plan<W>(keys, wave, lane);
-    sv.template plan<W>(vals, wave, lane);
-    auto load = [&](int t) {
-        sk.template load<W>(keys, (int64_t)t * KT, wave, lane);
-        sv.template load<W>(vals, (int64_t)t * KT, wave, lane);
-        left = (int)(n - (int64_t)t * KT);
-        if (a.bias) bias = a.bias[b * a.bias_sb + (int64_t)t * KT + min(srow, left - 1)];
+    auto load = [&] {
+        sk.template load<W>(keys, wave, lane);
+        sv.template load<W>(vals, wave, lane);
+        left = keys.left;
+        if (biases) {
+            bias = biases[min(srow, left - 1)];
+            biases += KT;
+        }
+        keys.advance(KT);
+        vals.advance(KT);
     };
     auto store = [&](int buf) {
         const float start = srow < left ? start_of(bias, inv_scale) : -INFINITY;
@@ -113,18 +119,18 @@ __global__ __launch_bounds__(kAttendThreads, (kWorkgroups<T, DP>)) void k_attend
         if (lane % 4 == 0) starts[buf][srow] = start;  // (two waves to a row: the same value)
     };
     if (t0 < t1) {
-        load(t0);
+        load();
         store(0);
     }
     __syncthreads();
     for (int t = t0; t < t1; ++t) {
         const int buf = (t - t0) & 1;
-        const bool more = t + 1 < t1;
-        if (more) load(t + 1);
+        const bool more = t + 1 < t1, plain = !a.bias && left >= KT;
+        if (more) load();
         const lds_t* kt = lds + buf * 2 * St::kBytes;
         const lds_t* vt = kt + St::kBytes;
         f16 s;
-        if (!a.bias && (int64_t)(t + 1) * KT <= n) {
+        if (plain) {
             s = Tile::scores(kt, ln, 0, qf);
         } else {
 #pragma unroll
@@ -162,7 +168,7 @@ __global__ __launch_bounds__(kAttendThreads, (kWorkgroups<T, DP>)) void k_attend
     __shared__ __align__(16) char smem[2 * 2 * St::kBytes];
     constexpr bool kept = kKeysInLds<T, DP>;
     __shared__ __align__(16) char kmem[kept ? kAttendWaves * Tile::NS * 1024 : 16];
-    __shared__ float row_c[2][3][QT];  // -reference, 1 / sum, delta of the tile's rows
+    __shared__ __align__(16) float row_c[2][3][QT];  // of the tile's rows
     lds_t* lds = (lds_t*)smem;
 
     const uint32_t id = xcd_item(c.items_k);
@@ -195,28 +201,30 @@ __global__ __launch_bounds__(kAttendThreads, (kWorkgroups<T, DP>)) void k_attend
     const int tiles = (int)((a.queries + QT - 1) / QT), steps = (int64_t)kb * kCols < n ? tiles * G : 0;
     const int t0 = first_tile(steps, split, c.splits_k), t1 = first_tile(steps, split + 1, c.splits_k);
     St sq, sg;
-    float r0 = 0.0f, r1 = 0.0f, r2 = 0.0f;
-    int64_t left = 0;  // rows of the staged tile that exist
-    Rows<T> qs{nullptr, a.q.st, a.queries, a.dim}, gs{nullptr, a.dout.st, a.queries, a.dim};
-    sq.template plan<W>(qs, wave, lane);
-    sg.template plan<W>(gs, wave, lane);
-    auto load = [&](int t) {
-        const int h = hk * G + t / tiles;
-        const int64_t i0 = (int64_t)(t % tiles) * QT;
-        qs.p = (const T*)a.q.p + b * a.q.sb + h * a.q.sh;
-        gs.p = (const T*)a.dout.p + b * a.dout.sb + h * a.dout.sh;
-        sq.template load<W>(qs, i0, wave, lane);
-        sg.template load<W>(gs, i0, wave, lane);
-        left = a.queries - i0;
-        if (threadIdx.x < QT) {
-            r0 = -INFINITY;
-            r1 = r2 = 0.0f;
-            if (threadIdx.x < left) {
-                const int64_t at = ((int64_t)b * a.heads + h) * a.queries + i0 + threadIdx.x;
-                const float m = a.stats[2 * at], l = a.stats[2 * at + 1];
-                r2 = c.delta[at];
-                if (l != 0.0f) r0 = -m, r1 = 1.0f / l;
-            }
+    f4 rc;
+    int left = 0;  // rows of the staged tile that exist
+    const int g0 = tiles > 0 ? t0 / tiles : 0;
+    int at = tiles > 0 ? t0 % tiles : 0;  // tile of the next load among its head's
+    int64_t head = hk * G + g0;
+    Cursor<T> qs{(const T*)a.q.p + b * a.q.sb + head * a.q.sh + (int64_t)at * QT * a.q.st, a.q.st, (int)a.queries - at * QT, a.dim};
+    Cursor<T> gs{(const T*)a.dout.p + b * a.dout.sb + head * a.dout.sh + (int64_t)at * QT * a.dout.st, a.dout.st, qs.left, a.dim};
+    const f4* consts = c.row_c + ((int64_t)b * a.heads + head) * a.queries + (int64_t)at * QT;
+    auto load = [&] {
+        sq.template load<W>(qs, wave, lane);
+        sg.template load<W>(gs, wave, lane);
+        left = qs.left;
+        rc = consts[min((int)threadIdx.x % QT, left - 1)];
+        if (++at < tiles) {
+            qs.advance(QT);
+            gs.advance(QT);
+            consts += QT;
+        } else {  // the next head of the group
+            at = 0;
+            ++head;
+            qs.p = (const T*)a.q.p + b * a.q.sb + head * a.q.sh;
+            gs.p = (const T*)a.dout.p + b * a.dout.sb + head * a.dout.sh;
+            qs.left = gs.left = (int)a.queries;
+            consts = c.row_c + ((int64_t)b * a.heads + head) * a.queries;
         }
     };
     auto store = [&](int buf) {
@@ -224,20 +232,21 @@ __global__ __launch_bounds__(kAttendThreads, (kWorkgroups<T, DP>)) void k_attend
         sq.store(lds + buf * 2 * St::kBytes, wave, lane, keep);
         sg.store(lds + (buf * 2 + 1) * St::kBytes, wave, lane, keep);
         if (threadIdx.x < QT) {
-            row_c[buf][0][threadIdx.x] = r0;
-            row_c[buf][1][threadIdx.x] = r1;
-            row_c[buf][2][threadIdx.x] = r2;
+            const bool in = (int)threadIdx.x < left;
+            row_c[buf][0][threadIdx.x] = in ? rc[0] : -INFINITY;
+            row_c[buf][1][threadIdx.x] = in ? rc[1] : 0.0f;
+            row_c[buf][2][threadIdx.x] = in ? rc[2] : 0.0f;
         }
     };
     if (t0 < t1) {
-        load(t0);
+        load();
         store(0);
     }
     __syncthreads();
     for (int t = t0; t < t1; ++t) {
         const int buf = (t - t0) & 1;
         const bool more = t + 1 < t1;
-        if (more) load(t + 1);
+        if (more) load();
         const lds_t* qt = lds + buf * 2 * St::kBytes;
         const lds_t* gt = qt + St::kBytes;
         f16 s;
@@ -248,9 +257,9 @@ __global__ __launch_bounds__(kAttendThreads, (kWorkgroups<T, DP>)) void k_attend
         f16 dp = Tile::scores(gt, ln, 0, vf);
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
-            const int at = 8 * q + 4 * (lane / 32);
-            const f4 neg = *(const f4*)&row_c[buf][0][at], inv = *(const f4*)&row_c[buf][1][at];
-            const f4 delta = *(const f4*)&row_c[buf][2][at];
+            const int at4 = 8 * q + 4 * (lane / 32);
+            const f4 neg = *(const f4*)&row_c[buf][0][at4], inv = *(const f4*)&row_c[buf][1][at4];
+            const f4 delta = *(const f4*)&row_c[buf][2][at4];
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
                 const float p = __builtin_amdgcn_exp2f(fmaf(s[4 * q + r], scale2, neg[r])) * inv[r];
@@ -319,7 +328,7 @@ GradCut cut_of(const AttendArgs& a) {
 }
 
 size_t round256(size_t n) { return (n + 255) / 256 * 256; }
-size_t delta_bytes(const AttendArgs& a) { return round256((size_t)a.batch * a.heads * a.queries * sizeof(float)); }
+size_t row_bytes(const AttendArgs& a) { return round256((size_t)a.batch * a.heads * a.queries * sizeof(f4)); }
 
 template <typename T, int DP>
 void launch_dq(const AttendArgs& a, const GradCut& c) {
@@ -373,7 +382,7 @@ size_t attend_grad_ws_bytes(const AttendArgs& a) {
     const GradCut c = cut_of(a);
     const size_t row = (size_t)a.batch * a.kv_heads * a.dim * sizeof(float);
     const size_t q = c.splits_q > 1 ? c.splits_q * row * c.rows : 0, k = c.splits_k > 1 ? c.splits_k * 2 * row * a.keys : 0;
-    return delta_bytes(a) + std::max(q, k);
+    return row_bytes(a) + std::max(q, k);
 }
 
 hipError_t launch_attend_grad(const AttendArgs& a, void* ws) {
@@ -383,8 +392,8 @@ hipError_t launch_attend_grad(const AttendArgs& a, void* ws) {
     c.wide = true;
     for (const Heads* t : {&a.q, &a.k, &a.v, &a.out, &a.low, &a.dout}) c.wide = c.wide && wide_rows(*t, a.dim, ch, e);
     for (const Heads* t : {&a.dq, &a.dk, &a.dv}) c.wide = c.wide && wide_rows(*t, a.dim, 4, e);
-    c.delta = (float*)ws;
-    c.part = (float*)((char*)ws + delta_bytes(a));
+    c.row_c = (f4*)ws;
+    c.part = (float*)((char*)ws + row_bytes(a));
     return a.bf16 ? run<__bf16>(a, c) : run<float>(a, c);
 }
 
