@@ -98,6 +98,21 @@ struct Mat<__bf16> {
     static __device__ __forceinline__ f16 scores(Frag a, Frag b, f16 c) {
         return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
     }
+    // P as the values' operand.  Rounded to nearest: an error of 2^-9 in the mean
+    // of each term, as large as that of the result's own rounding.
+    struct Probs {
+        bf8 v[2];
+        __device__ __forceinline__ Probs() {}
+        __device__ __forceinline__ Probs(const f16& p) {
+#pragma unroll
+            for (int q = 0; q < 4; ++q) set(q, f4{p[4 * q], p[4 * q + 1], p[4 * q + 2], p[4 * q + 3]});
+        }
+        __device__ __forceinline__ void set(int q, f4 p) {
+            const bf4 b = __builtin_convertvector(p, bf4);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) v[q / 2][q % 2 * 4 + j] = b[j];
+        }
+    };
 };
 template <>
 struct Mat<float> {
@@ -112,6 +127,15 @@ struct Mat<float> {
         for (int j = 0; j < 4; ++j) c = __builtin_amdgcn_mfma_f32_32x32x2f32(a[j], b[j], c, 0, 0, 0);
         return c;
     }
+    struct Probs {
+        f16 v;
+        __device__ __forceinline__ Probs() {}
+        __device__ __forceinline__ Probs(const f16& p) : v(p) {}
+        __device__ __forceinline__ void set(int q, f4 p) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) v[4 * q + j] = p[j];
+        }
+    };
 };
 
 template <typename T, int DP>
@@ -147,9 +171,14 @@ struct TileOf {
         typedef __attribute__((address_space(3))) const Frag F;
         return *(F*)(tile + (s % 2 ? l.odd : l.even) + (s / 2) * 1024 + k * 2 * kStep16);
     }
-    static __device__ __forceinline__ f16 scores(const lds_t* tile, const Lane& l, int k, const Frag (&f)[NS], f16 c) {
+    // Fragments wholly beyond D are left out in fp32, where one costs four products.
+    static __device__ __forceinline__ bool used(int s, int D) {
+        return std::is_same<T, __bf16>::value || 2 * CH * s < DP - 32 || 2 * CH * s < D;
+    }
+    static __device__ __forceinline__ f16 scores(const lds_t* tile, const Lane& l, int k, const Frag (&f)[NS], int D, f16 c) {
 #pragma unroll
-        for (int s = 0; s < NS; ++s) c = Mat<T>::scores(row(tile, l, k, s), f[s], c);
+        for (int s = 0; s < NS; ++s)
+            if (used(s, D)) c = Mat<T>::scores(row(tile, l, k, s), f[s], c);
         return c;
     }
     // Fragments that each lane keeps in LDS for itself (NS KB a wave) where they
@@ -160,34 +189,31 @@ struct TileOf {
         for (int s = 0; s < NS; ++s) *(F*)(at + s * 1024 + lane * 16) = f[s];
     }
     static __device__ __forceinline__ f16 scores_kept(const lds_t* tile, const Lane& l, int k, const lds_t* at, int lane,
-                                                      f16 c) {
+                                                      int D, f16 c) {
         typedef __attribute__((address_space(3))) const Frag F;
 #pragma unroll
-        for (int s = 0; s < NS; ++s) c = Mat<T>::scores(row(tile, l, k, s), *(F*)(at + s * 1024 + lane * 16), c);
+        for (int s = 0; s < NS; ++s)
+            if (used(s, D)) c = Mat<T>::scores(row(tile, l, k, s), *(F*)(at + s * 1024 + lane * 16), c);
         return c;
     }
-    static __device__ __forceinline__ f16 scores(const lds_t* tile, const Lane& l, int k, const Frag (&f)[NS]) {
+    static __device__ __forceinline__ f16 scores(const lds_t* tile, const Lane& l, int k, const Frag (&f)[NS], int D) {
         const f16 zero = {0.0f};
-        return scores(tile, l, k, f, zero);
+        return scores(tile, l, k, f, D, zero);
     }
     // o[D / 32] += (rows 32 k .. 32 k + 31 of the tile)^T x p
-    static __device__ __forceinline__ void values(const lds_t* tile, const Lane& l, int k, const f16& p,
+    static __device__ __forceinline__ void values(const lds_t* tile, const Lane& l, int k, const typename Mat<T>::Probs& p,
                                                   f16 (&o)[DP / 32]) {
         if constexpr (std::is_same<T, __bf16>::value) {
             typedef __attribute__((address_space(3))) s4 V;
 #pragma unroll
             for (int ks = 0; ks < 2; ++ks) {
-                f8 e;
-#pragma unroll
-                for (int j = 0; j < 8; ++j) e[j] = p[8 * ks + j];
-                const bf8 b = __builtin_convertvector(e, bf8);  // to nearest: half of the result's own rounding
 #pragma unroll
                 for (int d = 0; d < DP / 32; ++d) {
                     const uint32_t at = d * 1024 + (2 * k + ks) * kStep16;
                     const s4 v0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((V*)(tile + l.t0 + at));
                     const s4 v1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((V*)(tile + l.t1 + at));
                     const bf8 a = __builtin_bit_cast(bf8, __builtin_shufflevector(v0, v1, 0, 1, 2, 3, 4, 5, 6, 7));
-                    o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, o[d], 0, 0, 0);
+                    o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, p.v[ks], o[d], 0, 0, 0);
                 }
             }
         } else {
@@ -203,7 +229,7 @@ struct TileOf {
                 for (int i = 0; i < 16; ++i) {
                     const uint32_t at = 2 * d * 1024 + (2 * k + i / 8) * kStep16 + (i % 4) * 64;
                     const float v = *(V*)(tile + ((i / 4) % 2 ? l.t1 : l.t0) + at);
-                    t = __builtin_amdgcn_mfma_f32_32x32x2f32(v, p[i], t, 0, 0, 0);
+                    t = __builtin_amdgcn_mfma_f32_32x32x2f32(v, p.v[i], t, 0, 0, 0);
                 }
                 o[d] += t;
             }
@@ -306,14 +332,43 @@ __device__ __forceinline__ void load_frags(const T* row, int D, bool live, int l
     }
 }
 
-// Writes four consecutive entries.
-__device__ __forceinline__ void store4(__bf16* p, f4 v) { *(bf4*)p = __builtin_convertvector(v, bf4); }
-__device__ __forceinline__ void store4(float* p, f4 v) { *(f4*)p = v; }
+// Exchanges a's upper 32 lanes with b's lower 32.
+__device__ __forceinline__ void swap_halves(uint32_t& a, uint32_t& b) {
+    const auto r = __builtin_amdgcn_permlane32_swap(a, b, false, false);
+    a = r[0];
+    b = r[1];
+}
 
 // A lane's column of accumulators o (entry 32 d + 8 (i / 4) + 4 h + i % 4 in
-// register i), times f, to the row's D entries.
+// register i), times f, to the row's D entries.  W: in 16-byte stores.  bf16
+// lanes first trade groups of four with the lane that holds the other half of
+// their row, so that each has eight in a row (stores of 8 bytes: 66 us for the
+// forward pass of 2 x 32768 queries, 8 heads of 64, to 77 keys; so 53 us).  All
+// lanes call it; `live`: whether this one's row exists.
 template <typename T, int DP, bool W>
-__device__ __forceinline__ void store_column(T* row, const f16 (&o)[DP / 32], float f, int D, int lane) {
+__device__ __forceinline__ void store_column(T* row, const f16 (&o)[DP / 32], float f, int D, int lane, bool live) {
+    if constexpr (W && std::is_same<T, __bf16>::value) {
+#pragma unroll
+        for (int d = 0; d < DP / 32; ++d)
+#pragma unroll
+            for (int q = 0; q < 4; q += 2) {
+                uint32_t w[2][2];
+#pragma unroll
+                for (int k = 0; k < 2; ++k) {
+                    const f4 v = {o[d][4 * (q + k)] * f, o[d][4 * (q + k) + 1] * f, o[d][4 * (q + k) + 2] * f,
+                                  o[d][4 * (q + k) + 3] * f};
+                    const uint2 u = __builtin_bit_cast(uint2, __builtin_convertvector(v, bf4));
+                    w[k][0] = u.x;
+                    w[k][1] = u.y;
+                }
+                swap_halves(w[0][0], w[1][0]);
+                swap_halves(w[0][1], w[1][1]);
+                const int c = 32 * d + 8 * (q + lane / 32);
+                if (live && c < D) *(u4*)(row + c) = u4{w[0][0], w[0][1], w[1][0], w[1][1]};
+            }
+        return;
+    }
+    if (!live) return;
 #pragma unroll
     for (int d = 0; d < DP / 32; ++d)
 #pragma unroll
@@ -321,7 +376,7 @@ __device__ __forceinline__ void store_column(T* row, const f16 (&o)[DP / 32], fl
             const int c = 32 * d + 8 * q + 4 * (lane / 32);
             const f4 v = {o[d][4 * q] * f, o[d][4 * q + 1] * f, o[d][4 * q + 2] * f, o[d][4 * q + 3] * f};
             if constexpr (W) {
-                if (c < D) store4(row + c, v);
+                if (c < D) *(f4*)(row + c) = v;
             } else {
 #pragma unroll
                 for (int j = 0; j < 4; ++j)

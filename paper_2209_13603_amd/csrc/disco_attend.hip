@@ -24,7 +24,7 @@ struct Cut {
     int32_t splits;
     float* part;   // [splits][all rows][dim]
     float* stat;   // [splits][all rows][2]
-    bool wide;     // rows of all tensors go by 16 bytes (out by four entries)
+    bool wide;     // rows of all tensors go by 16 bytes
 };
 
 // Workgroups of a CU that the registers are sized for.
@@ -111,7 +111,7 @@ __global__ __launch_bounds__(kAttendThreads, (kWorkgroups<T, DP>)) void k_attend
         f16 s[NK];
         if (plain) {
 #pragma unroll
-            for (int k = 0; k < NK; ++k) s[k] = Tile::scores(kt, ln, k, qf);
+            for (int k = 0; k < NK; ++k) s[k] = Tile::scores(kt, ln, k, qf, a.dim);
         } else {
 #pragma unroll
             for (int k = 0; k < NK; ++k) {
@@ -121,7 +121,7 @@ __global__ __launch_bounds__(kAttendThreads, (kWorkgroups<T, DP>)) void k_attend
 #pragma unroll
                     for (int r = 0; r < 4; ++r) s[k][4 * q + r] = v[r];
                 }
-                s[k] = Tile::scores(kt, ln, k, qf, s[k]);
+                s[k] = Tile::scores(kt, ln, k, qf, a.dim, s[k]);
             }
         }
         float top = s[0][0];
@@ -157,21 +157,20 @@ __global__ __launch_bounds__(kAttendThreads, (kWorkgroups<T, DP>)) void k_attend
         __syncthreads();
     }
     l += other_half(l);
-    if (!live) return;
     const int64_t stat = ((int64_t)b * a.heads + h) * a.queries + i;
     if (c.splits > 1) {
         const int64_t all = (int64_t)a.batch * a.kv_heads * c.rows;
         const int64_t at = split * all + (int64_t)bh * c.rows + row;
-        store_column<float, DP, W>(c.part + at * a.dim, o, 1.0f, a.dim, lane);
-        if (lane < 32) {
+        store_column<float, DP, W>(c.part + at * a.dim, o, 1.0f, a.dim, lane, live);
+        if (live && lane < 32) {
             c.stat[2 * at] = m;
             c.stat[2 * at + 1] = l;
         }
         return;
     }
     const float inv = l == 0.0f ? 0.0f : 1.0f / l;
-    store_column<T, DP, W>((T*)a.out.p + b * a.out.sb + i * a.out.st + h * a.out.sh, o, inv, a.dim, lane);
-    if (a.stats && lane < 32) {
+    store_column<T, DP, W>((T*)a.out.p + b * a.out.sb + i * a.out.st + h * a.out.sh, o, inv, a.dim, lane, live);
+    if (a.stats && live && lane < 32) {
         a.stats[2 * stat] = m;
         a.stats[2 * stat + 1] = l;
     }
@@ -184,7 +183,7 @@ __global__ __launch_bounds__(kAttendThreads, (kWorkgroups<T, DP>)) void k_attend
                     const float v = o[d][r] * inv;
                     o[d][r] = v - (float)(__bf16)v;
                 }
-            store_column<T, DP, W>((T*)a.low.p + b * a.low.sb + i * a.low.st + h * a.low.sh, o, 1.0f, a.dim, lane);
+            store_column<T, DP, W>((T*)a.low.p + b * a.low.sb + i * a.low.st + h * a.low.sh, o, 1.0f, a.dim, lane, live);
         }
     }
 }
@@ -276,7 +275,7 @@ hipError_t launch_attend(const AttendArgs& a, void* ws) {
     const size_t e = a.bf16 ? 2 : 4;
     const int ch = a.bf16 ? 8 : 4;
     c.wide = wide_rows(a.q, a.dim, ch, e) && wide_rows(a.k, a.dim, ch, e) && wide_rows(a.v, a.dim, ch, e) &&
-             wide_rows(a.out, a.dim, 4, e) && wide_rows(a.low, a.dim, 4, e);
+             wide_rows(a.out, a.dim, ch, e) && wide_rows(a.low, a.dim, ch, e);
     if (c.splits > 1) {
         c.part = (float*)ws;
         c.stat = (float*)((char*)ws + part_bytes(a, c));

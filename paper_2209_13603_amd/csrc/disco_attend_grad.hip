@@ -27,7 +27,7 @@ struct GradCut {
     int32_t splits_q, splits_k;
     f4* row_c;    // [batch][heads][queries]: -reference, 1 / sum, delta, written with dq for dk and dv
     float* part;  // [splits][...][dim]
-    bool wide;    // rows of all tensors go by 16 bytes (written ones by four entries)
+    bool wide;    // rows of all tensors go by 16 bytes
 };
 
 // Workgroups of a CU that the registers are sized for.
@@ -131,7 +131,7 @@ __global__ __launch_bounds__(kAttendThreads, (kWorkgroups<T, DP>)) void k_attend
         const lds_t* vt = kt + St::kBytes;
         f16 s;
         if (plain) {
-            s = Tile::scores(kt, ln, 0, qf);
+            s = Tile::scores(kt, ln, 0, qf, a.dim);
         } else {
 #pragma unroll
             for (int q = 0; q < 4; ++q) {
@@ -139,22 +139,21 @@ __global__ __launch_bounds__(kAttendThreads, (kWorkgroups<T, DP>)) void k_attend
 #pragma unroll
                 for (int r = 0; r < 4; ++r) s[4 * q + r] = v[r];
             }
-            s = Tile::scores(kt, ln, 0, qf, s);
+            s = Tile::scores(kt, ln, 0, qf, a.dim, s);
         }
-        const f16 dp = Tile::scores(vt, ln, 0, gf);
+        const f16 dp = Tile::scores(vt, ln, 0, gf, a.dim);
 #pragma unroll
         for (int r = 0; r < 16; ++r) s[r] = __builtin_amdgcn_exp2f(fmaf(s[r], scale2, neg)) * (dp[r] - delta);
         Tile::values(kt, ln, 0, s, dq);
         if (more) store(buf ^ 1);
         __syncthreads();
     }
-    if (!live) return;
     const float f = inv * a.scale;
     if (c.splits_q > 1) {
         const int64_t all = (int64_t)a.batch * a.kv_heads * c.rows;
-        store_column<float, DP, W>(c.part + (split * all + (int64_t)bh * c.rows + row) * a.dim, dq, f, a.dim, lane);
+        store_column<float, DP, W>(c.part + (split * all + (int64_t)bh * c.rows + row) * a.dim, dq, f, a.dim, lane, live);
     } else {
-        store_column<T, DP, W>((T*)a.dq.p + b * a.dq.sb + i * a.dq.st + h * a.dq.sh, dq, f, a.dim, lane);
+        store_column<T, DP, W>((T*)a.dq.p + b * a.dq.sb + i * a.dq.st + h * a.dq.sh, dq, f, a.dim, lane, live);
     }
 }
 
@@ -168,7 +167,7 @@ __global__ __launch_bounds__(kAttendThreads, (kWorkgroups<T, DP>)) void k_attend
     __shared__ __align__(16) char smem[2 * 2 * St::kBytes];
     constexpr bool kept = kKeysInLds<T, DP>;
     __shared__ __align__(16) char kmem[kept ? kAttendWaves * Tile::NS * 1024 : 16];
-    __shared__ __align__(16) float row_c[2][3][QT];  // of the tile's rows
+    __shared__ __align__(16) float row_c[2][4][QT];  // GradCut::row_c of the tile's rows
     lds_t* lds = (lds_t*)smem;
 
     const uint32_t id = xcd_item(c.items_k);
@@ -201,7 +200,7 @@ __global__ __launch_bounds__(kAttendThreads, (kWorkgroups<T, DP>)) void k_attend
     const int tiles = (int)((a.queries + QT - 1) / QT), steps = (int64_t)kb * kCols < n ? tiles * G : 0;
     const int t0 = first_tile(steps, split, c.splits_k), t1 = first_tile(steps, split + 1, c.splits_k);
     St sq, sg;
-    f4 rc;
+    float rc = 0.0f;  // entry threadIdx.x of the staged tile's row constants
     int left = 0;  // rows of the staged tile that exist
     const int g0 = tiles > 0 ? t0 / tiles : 0;
     int at = tiles > 0 ? t0 % tiles : 0;  // tile of the next load among its head's
@@ -213,7 +212,7 @@ __global__ __launch_bounds__(kAttendThreads, (kWorkgroups<T, DP>)) void k_attend
         sq.template load<W>(qs, wave, lane);
         sg.template load<W>(gs, wave, lane);
         left = qs.left;
-        rc = consts[min((int)threadIdx.x % QT, left - 1)];
+        rc = ((const float*)consts)[min((int)threadIdx.x, 4 * left - 1)];
         if (++at < tiles) {
             qs.advance(QT);
             gs.advance(QT);
@@ -231,11 +230,9 @@ __global__ __launch_bounds__(kAttendThreads, (kWorkgroups<T, DP>)) void k_attend
         const bool keep = St::row_of(wave, lane) < left;
         sq.store(lds + buf * 2 * St::kBytes, wave, lane, keep);
         sg.store(lds + (buf * 2 + 1) * St::kBytes, wave, lane, keep);
-        if (threadIdx.x < QT) {
-            const bool in = (int)threadIdx.x < left;
-            row_c[buf][0][threadIdx.x] = in ? rc[0] : -INFINITY;
-            row_c[buf][1][threadIdx.x] = in ? rc[1] : 0.0f;
-            row_c[buf][2][threadIdx.x] = in ? rc[2] : 0.0f;
+        if (threadIdx.x < 4 * QT) {
+            const int k = threadIdx.x % 4;
+            row_c[buf][k][threadIdx.x / 4] = (int)threadIdx.x < 4 * left ? rc : k == 0 ? -INFINITY : 0.0f;
         }
     };
     if (t0 < t1) {
@@ -252,23 +249,30 @@ __global__ __launch_bounds__(kAttendThreads, (kWorkgroups<T, DP>)) void k_attend
         f16 s;
 #pragma unroll
         for (int r = 0; r < 16; ++r) s[r] = start;
-        if constexpr (kept) s = Tile::scores_kept(qt, ln, 0, mine, lane, s);
-        else s = Tile::scores(qt, ln, 0, kf, s);
-        f16 dp = Tile::scores(gt, ln, 0, vf);
+        if constexpr (kept) s = Tile::scores_kept(qt, ln, 0, mine, lane, a.dim, s);
+        else s = Tile::scores(qt, ln, 0, kf, a.dim, s);
+        if constexpr (kept) __builtin_amdgcn_sched_barrier(0);
+        const f16 dp = Tile::scores(gt, ln, 0, vf, a.dim);
+        if constexpr (kept) __builtin_amdgcn_sched_barrier(0);
+        typename Mat<T>::Probs p, ds;
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
             const int at4 = 8 * q + 4 * (lane / 32);
             const f4 neg = *(const f4*)&row_c[buf][0][at4], inv = *(const f4*)&row_c[buf][1][at4];
             const f4 delta = *(const f4*)&row_c[buf][2][at4];
+            f4 e, f;
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
-                const float p = __builtin_amdgcn_exp2f(fmaf(s[4 * q + r], scale2, neg[r])) * inv[r];
-                s[4 * q + r] = p;
-                dp[4 * q + r] = p * (dp[4 * q + r] - delta[r]);
+                e[r] = __builtin_amdgcn_exp2f(fmaf(s[4 * q + r], scale2, neg[r])) * inv[r];
+                f[r] = e[r] * (dp[4 * q + r] - delta[r]);
             }
+            p.set(q, e);
+            ds.set(q, f);
         }
-        Tile::values(gt, ln, 0, s, dv);
-        Tile::values(qt, ln, 0, dp, dk);
+        if constexpr (kept) __builtin_amdgcn_sched_barrier(0);
+        Tile::values(gt, ln, 0, p, dv);
+        if constexpr (kept) __builtin_amdgcn_sched_barrier(0);
+        Tile::values(qt, ln, 0, ds, dk);
         if (more) store(buf ^ 1);
         __syncthreads();
     }
@@ -277,14 +281,14 @@ __global__ __launch_bounds__(kAttendThreads, (kWorkgroups<T, DP>)) void k_attend
         for (int d = 0; d < DP / 32; ++d)
 #pragma unroll
             for (int r = 0; r < 16; ++r) dk[d][r] = dv[d][r] = 0.0f;
-    if (j >= a.keys) return;
+    const bool there = j < a.keys;
     if (c.splits_k > 1) {
         const int64_t all = (int64_t)a.batch * a.kv_heads * a.keys, at = split * 2 * all + (int64_t)bh * a.keys + j;
-        store_column<float, DP, W>(c.part + at * a.dim, dk, a.scale, a.dim, lane);
-        store_column<float, DP, W>(c.part + (at + all) * a.dim, dv, 1.0f, a.dim, lane);
+        store_column<float, DP, W>(c.part + at * a.dim, dk, a.scale, a.dim, lane, there);
+        store_column<float, DP, W>(c.part + (at + all) * a.dim, dv, 1.0f, a.dim, lane, there);
     } else {
-        store_column<T, DP, W>((T*)a.dk.p + b * a.dk.sb + j * a.dk.st + hk * a.dk.sh, dk, a.scale, a.dim, lane);
-        store_column<T, DP, W>((T*)a.dv.p + b * a.dv.sb + j * a.dv.st + hk * a.dv.sh, dv, 1.0f, a.dim, lane);
+        store_column<T, DP, W>((T*)a.dk.p + b * a.dk.sb + j * a.dk.st + hk * a.dk.sh, dk, a.scale, a.dim, lane, there);
+        store_column<T, DP, W>((T*)a.dv.p + b * a.dv.sb + j * a.dv.st + hk * a.dv.sh, dv, 1.0f, a.dim, lane, there);
     }
 }
 
@@ -390,8 +394,8 @@ hipError_t launch_attend_grad(const AttendArgs& a, void* ws) {
     const size_t e = a.bf16 ? 2 : 4;
     const int ch = a.bf16 ? 8 : 4;
     c.wide = true;
-    for (const Heads* t : {&a.q, &a.k, &a.v, &a.out, &a.low, &a.dout}) c.wide = c.wide && wide_rows(*t, a.dim, ch, e);
-    for (const Heads* t : {&a.dq, &a.dk, &a.dv}) c.wide = c.wide && wide_rows(*t, a.dim, 4, e);
+    for (const Heads* t : {&a.q, &a.k, &a.v, &a.out, &a.low, &a.dout, &a.dq, &a.dk, &a.dv})
+        c.wide = c.wide && wide_rows(*t, a.dim, ch, e);
     c.row_c = (f4*)ws;
     c.part = (float*)((char*)ws + row_bytes(a));
     return a.bf16 ? run<__bf16>(a, c) : run<float>(a, c);
