@@ -215,6 +215,8 @@ void check_rotate(const disco_heads_t* x, int32_t norm, const disco_tensor_t* w,
         a->weight = w->data;
         a->weight_sh = shared ? 0 : x->dim;
     }
+    if (x->batch * x->tokens * x->heads >= kMaxRows)
+        refuse(DISCO_ERR_SHAPE, "2^31 rows (batch * tokens * heads) or more");
     a->batch = (int32_t)x->batch;
     a->heads = x->heads;
     a->dim = x->dim;

@@ -29,7 +29,6 @@ namespace disco {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kUnroll = 4;  // heads whose loads are in flight together
 
 template <typename T, int V>
 using Vec = T __attribute__((ext_vector_type(V)));
@@ -48,8 +47,26 @@ __device__ __forceinline__ void store(T* p, const float* f) {
     *(Vec<T, V>*)p = __builtin_convertvector(v, Vec<T, V>);
 }
 
+// Division of n < 2^31 by a fixed d: (mulhi(n, m) + n) >> s with s = ceil(log2 d),
+// m = floor(2^32 (2^s - d) / d) + 1.
+struct Divisor {
+    uint32_t d, m, s;
+    __device__ __forceinline__ uint32_t quotient(uint32_t n) const { return (__umulhi(n, m) + n) >> s; }
+};
+Divisor divisor(uint32_t d) {
+    Divisor r{d, 0, 0};
+    while (((uint64_t)1 << r.s) < d) ++r.s;
+    r.m = (uint32_t)((((uint64_t)1 << 32) * (((uint64_t)1 << r.s) - d)) / d + 1);
+    return r;
+}
+
+// lanes: of a row; slots: rows of a workgroup's pass; rows: of one grid column
+// (all heads of all tokens, or the tokens of head blockIdx.y with per_head).
 struct Shape {
-    int items, rot_items, lanes, slots, hpb, gx, gy;
+    int items, rot_items, lanes, slots, gx, gy;
+    uint32_t rows;
+    bool per_head;
+    Divisor heads, tokens;
 };
 
 // The part of a row that a lane holds: entries [a, a + V) and [b, b + V).
@@ -109,131 +126,119 @@ __device__ __forceinline__ bool load_angles(const RotateArgs& a, int64_t b, int6
     return true;
 }
 
-// grid: (token blocks, groups of hpb heads).
+// Token and head of a row.
+struct Place {
+    int64_t b, tok;
+    int h;
+};
+__device__ __forceinline__ Place place_of(const RotateArgs& a, const Shape& s, uint32_t row) {
+    Place p;
+    uint32_t t = row;
+    if (s.per_head) {
+        p.h = blockIdx.y;
+    } else {
+        t = s.heads.quotient(row);
+        p.h = (int)(row - t * s.heads.d);
+    }
+    const uint32_t b = s.tokens.quotient(t);
+    p.b = b;
+    p.tok = t - b * s.tokens.d;
+    return p;
+}
+template <typename T>
+__device__ __forceinline__ T* row_at(const Heads& t, const Place& p) {
+    return (T*)t.p + p.b * t.sb + p.tok * t.st + p.h * t.sh;
+}
+
+// A row's part for each thread: one load or two, and as many stores.
 template <typename T, int V, bool INTER>
 __global__ __launch_bounds__(kThreads) void k_rotate(RotateArgs a, Shape sh) {
     const int item = threadIdx.x % sh.lanes, slot = threadIdx.x / sh.lanes;
-    const int64_t t = (int64_t)blockIdx.x * sh.slots + slot, n_tok = (int64_t)a.batch * a.tokens;
-    if (t >= n_tok) return;  // whole rows: the shuffles below stay within one
-    const int64_t b = (uint32_t)t / (uint32_t)a.tokens, tok = t - b * a.tokens;
-    const int h0 = blockIdx.y * sh.hpb, h1 = min(h0 + sh.hpb, a.heads);
+    const uint32_t row = blockIdx.x * (uint32_t)sh.slots + slot;
+    if (row >= sh.rows) return;  // whole rows: the sums below stay within one
     const Item it = item_of<V, INTER>(item, sh, a.rotary, a.dim);
-    const T* x = (const T*)a.x.p + b * a.x.sb + tok * a.x.st;
-    T* y = (T*)a.y.p + b * a.y.sb + tok * a.y.st;
-    float c[V], s[V], w[2 * V];
-    const float poison = load_angles<V>(a, b, tok, item, it.rot, c, s) ? 1.0f : __builtin_nanf("");
+    const Place p = place_of(a, sh, row);
+    float e[2 * V], w[2 * V], c[V], s[V];
 #pragma unroll
-    for (int i = 0; i < 2 * V; ++i) w[i] = 1.0f;
-    auto load_weight = [&](int h) {
-        const T* wp = (const T*)a.weight + (int64_t)h * a.weight_sh;
+    for (int i = 0; i < 2 * V; ++i) e[i] = 0.0f, w[i] = 1.0f;
+    const T* x = row_at<const T>(a.x, p);
+    if (it.has_a) load<T, V>(x + it.a, e);
+    if (it.has_b) load<T, V>(x + it.b, e + V);
+    float r = load_angles<V>(a, p.b, p.tok, item, it.rot, c, s) ? 1.0f : __builtin_nanf("");
+    if (a.weight) {
+        const T* wp = (const T*)a.weight + p.h * a.weight_sh;
         if (it.has_a) load<T, V>(wp + it.a, w);
         if (it.has_b) load<T, V>(wp + it.b, w + V);
-    };
-    if (a.weight && a.weight_sh == 0) load_weight(0);
-    const float inv_d = 1.0f / (float)a.dim;
-    for (int h = h0; h < h1; h += kUnroll) {
-        float e[kUnroll][2 * V];
-#pragma unroll
-        for (int u = 0; u < kUnroll; ++u) {
-#pragma unroll
-            for (int i = 0; i < 2 * V; ++i) e[u][i] = 0.0f;
-            const T* xp = x + (int64_t)min(h + u, h1 - 1) * a.x.sh;
-            if (it.has_a) load<T, V>(xp + it.a, e[u]);
-            if (it.has_b) load<T, V>(xp + it.b, e[u] + V);
-        }
-#pragma unroll
-        for (int u = 0; u < kUnroll; ++u) {
-            if (h + u >= h1) break;
-            if (a.weight && a.weight_sh != 0) load_weight(h + u);
-            float r = poison;
-            if (a.norm) {
-                float ss = 0.0f;
-#pragma unroll
-                for (int i = 0; i < 2 * V; ++i) ss = fmaf(e[u][i], e[u][i], ss);
-                r *= rsqrtf(fmaf(lane_sum(ss, sh.lanes), inv_d, a.eps));
-            }
-#pragma unroll
-            for (int i = 0; i < 2 * V; ++i) e[u][i] = e[u][i] * r * w[i];
-            if (it.rot) turn<V, INTER>(e[u], c, s, 1.0f);
-            T* yp = y + (int64_t)(h + u) * a.y.sh;
-            if (it.has_a) store<T, V>(yp + it.a, e[u]);
-            if (it.has_b) store<T, V>(yp + it.b, e[u] + V);
-        }
     }
+    if (a.norm) {
+        float ss = 0.0f;
+#pragma unroll
+        for (int i = 0; i < 2 * V; ++i) ss = fmaf(e[i], e[i], ss);
+        r *= rsqrtf(fmaf(lane_sum(ss, sh.lanes), 1.0f / (float)a.dim, a.eps));
+    }
+#pragma unroll
+    for (int i = 0; i < 2 * V; ++i) e[i] = e[i] * r * w[i];
+    if (it.rot) turn<V, INTER>(e, c, s, 1.0f);
+    T* y = row_at<T>(a.y, p);
+    if (it.has_a) store<T, V>(y + it.a, e);
+    if (it.has_b) store<T, V>(y + it.b, e + V);
 }
 
-// Gradients.  Each workgroup walks the token blocks with the grid's stride and
+// Gradients.  Each workgroup walks the runs of rows with the grid's stride and
 // leaves its sum of g n in partial[(blockIdx.y, blockIdx.x)][D].
 template <typename T, int V, bool INTER>
 __global__ __launch_bounds__(kThreads) void k_rotate_grad(RotateArgs a, Shape sh, float* __restrict__ partial) {
     __shared__ float red[kThreads * 2 * V];
     const int item = threadIdx.x % sh.lanes, slot = threadIdx.x / sh.lanes;
-    const int64_t n_tok = (int64_t)a.batch * a.tokens;
-    const int h0 = blockIdx.y * sh.hpb, h1 = min(h0 + sh.hpb, a.heads);
     const Item it = item_of<V, INTER>(item, sh, a.rotary, a.dim);
     const float inv_d = 1.0f / (float)a.dim;
     float w[2 * V], dw[2 * V];
 #pragma unroll
     for (int i = 0; i < 2 * V; ++i) w[i] = 1.0f, dw[i] = 0.0f;
     auto load_weight = [&](int h) {
-        const T* wp = (const T*)a.weight + (int64_t)h * a.weight_sh;
+        const T* wp = (const T*)a.weight + h * a.weight_sh;
         if (it.has_a) load<T, V>(wp + it.a, w);
         if (it.has_b) load<T, V>(wp + it.b, w + V);
     };
-    if (a.weight && a.weight_sh == 0) load_weight(0);
-    for (int64_t t = (int64_t)blockIdx.x * sh.slots + slot; t < n_tok; t += (int64_t)sh.gx * sh.slots) {
-        const int64_t b = (uint32_t)t / (uint32_t)a.tokens, tok = t - b * a.tokens;
-        const T* x = a.norm ? (const T*)a.x.p + b * a.x.sb + tok * a.x.st : nullptr;
-        const T* dy = (const T*)a.dy.p + b * a.dy.sb + tok * a.dy.st;
-        T* dx = a.dx.p ? (T*)a.dx.p + b * a.dx.sb + tok * a.dx.st : nullptr;
-        float c[V], s[V];
-        const float poison = load_angles<V>(a, b, tok, item, it.rot, c, s) ? 1.0f : __builtin_nanf("");
-        constexpr int kU = kUnroll / 2;
-        for (int h = h0; h < h1; h += kU) {
-            float e[kU][2 * V], g[kU][2 * V];
+    if (a.weight && (a.weight_sh == 0 || sh.per_head)) load_weight(sh.per_head ? blockIdx.y : 0);
+    for (uint64_t row = (uint64_t)blockIdx.x * sh.slots + slot; row < sh.rows; row += (uint64_t)sh.gx * sh.slots) {
+        const Place p = place_of(a, sh, (uint32_t)row);
+        float e[2 * V], g[2 * V], c[V], s[V];
 #pragma unroll
-            for (int u = 0; u < kU; ++u) {
+        for (int i = 0; i < 2 * V; ++i) e[i] = g[i] = 0.0f;
+        const T* dy = row_at<const T>(a.dy, p);
+        if (it.has_a) load<T, V>(dy + it.a, g);
+        if (it.has_b) load<T, V>(dy + it.b, g + V);
+        if (a.norm) {
+            const T* x = row_at<const T>(a.x, p);
+            if (it.has_a) load<T, V>(x + it.a, e);
+            if (it.has_b) load<T, V>(x + it.b, e + V);
+        }
+        const float poison = load_angles<V>(a, p.b, p.tok, item, it.rot, c, s) ? 1.0f : __builtin_nanf("");
+        if (a.weight && a.weight_sh && !sh.per_head) load_weight(p.h);
+        if (it.rot) turn<V, INTER>(g, c, s, -1.0f);
+        if (a.norm) {
+            float ss = 0.0f, tx = 0.0f;
 #pragma unroll
-                for (int i = 0; i < 2 * V; ++i) e[u][i] = g[u][i] = 0.0f;
-                const int hu = min(h + u, h1 - 1);
-                const T* gp = dy + (int64_t)hu * a.dy.sh;
-                if (it.has_a) load<T, V>(gp + it.a, g[u]);
-                if (it.has_b) load<T, V>(gp + it.b, g[u] + V);
-                if (a.norm) {
-                    const T* xp = x + (int64_t)hu * a.x.sh;
-                    if (it.has_a) load<T, V>(xp + it.a, e[u]);
-                    if (it.has_b) load<T, V>(xp + it.b, e[u] + V);
-                }
+            for (int i = 0; i < 2 * V; ++i) {
+                ss = fmaf(e[i], e[i], ss);
+                tx = fmaf(w[i] * g[i], e[i], tx);
             }
+            const float r = poison * rsqrtf(fmaf(lane_sum(ss, sh.lanes), inv_d, a.eps));
+            const float m = r * r * lane_sum(tx, sh.lanes) * inv_d;  // mean(t n) r
 #pragma unroll
-            for (int u = 0; u < kU; ++u) {
-                if (h + u >= h1) break;
-                if (a.weight && a.weight_sh != 0) load_weight(h + u);
-                if (it.rot) turn<V, INTER>(g[u], c, s, -1.0f);
-                if (a.norm) {
-                    float ss = 0.0f, tx = 0.0f;
-#pragma unroll
-                    for (int i = 0; i < 2 * V; ++i) {
-                        ss = fmaf(e[u][i], e[u][i], ss);
-                        tx = fmaf(w[i] * g[u][i], e[u][i], tx);
-                    }
-                    const float r = poison * rsqrtf(fmaf(lane_sum(ss, sh.lanes), inv_d, a.eps));
-                    const float m = r * r * lane_sum(tx, sh.lanes) * inv_d;  // mean(t n) r
-#pragma unroll
-                    for (int i = 0; i < 2 * V; ++i) {
-                        dw[i] = fmaf(g[u][i] * r, e[u][i], dw[i]);
-                        g[u][i] = r * fmaf(-m, e[u][i], w[i] * g[u][i]);
-                    }
-                } else {
-#pragma unroll
-                    for (int i = 0; i < 2 * V; ++i) g[u][i] *= poison;
-                }
-                if (dx) {
-                    T* dp = dx + (int64_t)(h + u) * a.dx.sh;
-                    if (it.has_a) store<T, V>(dp + it.a, g[u]);
-                    if (it.has_b) store<T, V>(dp + it.b, g[u] + V);
-                }
+            for (int i = 0; i < 2 * V; ++i) {
+                dw[i] = fmaf(g[i] * r, e[i], dw[i]);
+                g[i] = r * fmaf(-m, e[i], w[i] * g[i]);
             }
+        } else {
+#pragma unroll
+            for (int i = 0; i < 2 * V; ++i) g[i] *= poison;
+        }
+        if (a.dx.p) {
+            T* dx = row_at<T>(a.dx, p);
+            if (it.has_a) store<T, V>(dx + it.a, g);
+            if (it.has_b) store<T, V>(dx + it.b, g + V);
         }
     }
     if (!partial) return;
@@ -291,29 +296,27 @@ int width(const RotateArgs& a) {
     return 1;
 }
 
-Shape shape_of(const RotateArgs& a, int v, bool per_head, int max_blocks) {
+// per_head: a grid column for each head; blocks: the most workgroups (0: a
+// thread for every part of a row).
+Shape shape_of(const RotateArgs& a, int v, bool per_head, int blocks) {
     Shape s;
     s.rot_items = a.rotary / 2 / v;
     s.items = s.rot_items + (a.dim - a.rotary + 2 * v - 1) / (2 * v);
     s.lanes = 1;
     while (s.lanes < s.items) s.lanes *= 2;
     s.slots = kThreads / s.lanes;
-    const int64_t tokens = (int64_t)a.batch * a.tokens, gx = std::max<int64_t>(1, (tokens + s.slots - 1) / s.slots);
-    // All heads of a token by one lane where that leaves the chip full (the
-    // tables and weight are then read once a token), fewer below.
-    s.hpb = per_head ? 1 : std::max(a.heads, 1);
-    while (s.hpb > 1 && gx * ((a.heads + s.hpb - 1) / s.hpb) < 1024) s.hpb = (s.hpb + 1) / 2;
-    s.gy = std::max(1, (a.heads + s.hpb - 1) / s.hpb);
-    s.gx = (int)std::min<int64_t>(gx, max_blocks > 0 ? std::max(1, max_blocks / s.gy) : gx);
+    s.per_head = per_head;
+    s.heads = divisor((uint32_t)std::max(a.heads, 1));
+    s.tokens = divisor((uint32_t)std::max<int64_t>(a.tokens, 1));
+    s.gy = per_head ? std::max(a.heads, 1) : 1;
+    s.rows = (uint32_t)((int64_t)a.batch * a.tokens * (per_head ? 1 : a.heads));
+    const int64_t gx = std::max<int64_t>(1, ((int64_t)s.rows + s.slots - 1) / s.slots);
+    s.gx = (int)std::min<int64_t>(gx, blocks > 0 ? std::max(1, blocks / s.gy) : gx);
     return s;
 }
 
 // Workgroups of the gradient when it sums dw: each leaves one partial row.
-constexpr int kGradBlocks = 2048;
-
-Shape grad_shape(const RotateArgs& a, int v) {
-    return shape_of(a, v, a.weight && a.weight_sh != 0 && a.dweight, a.dweight ? kGradBlocks : 0);
-}
+constexpr int kGradBlocks = 1024;
 
 // Calls f with the kernels' types for the storage type, width and layout.
 template <typename F>
@@ -340,8 +343,8 @@ hipError_t launch_rotate(const RotateArgs& a) {
     const Shape s = shape_of(a, v, false, 0);
     const int tk = timing_begin("norm_rotate", a.stream);
     const hipError_t e = dispatch(a, v, [&](auto t, auto vv, auto inter) {
-        hipLaunchKernelGGL((k_rotate<decltype(t), decltype(vv)::value, decltype(inter)::value>),
-                           dim3((unsigned)s.gx, (unsigned)s.gy), dim3(kThreads), 0, a.stream, a, s);
+        hipLaunchKernelGGL((k_rotate<decltype(t), decltype(vv)::value, decltype(inter)::value>), dim3((unsigned)s.gx),
+                           dim3(kThreads), 0, a.stream, a, s);
         return hipGetLastError();
     });
     timing_end(tk, a.stream);
@@ -352,7 +355,7 @@ size_t rotate_grad_ws_bytes(const RotateArgs& a) { return (size_t)(kGradBlocks +
 
 hipError_t launch_rotate_grad(const RotateArgs& a, float* ws) {
     const int v = width(a);
-    const Shape s = grad_shape(a, v);
+    const Shape s = shape_of(a, v, a.weight && a.weight_sh != 0 && a.dweight, a.dweight ? kGradBlocks : 0);
     int tk = timing_begin("norm_rotate_grad", a.stream);
     hipError_t e = dispatch(a, v, [&](auto t, auto vv, auto inter) {
         hipLaunchKernelGGL((k_rotate_grad<decltype(t), decltype(vv)::value, decltype(inter)::value>),
