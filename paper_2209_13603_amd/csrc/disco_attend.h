@@ -61,10 +61,17 @@ __device__ __forceinline__ float start_of(float bias, float inv_scale) {
     return t < kLowestBias && bias != -INFINITY ? kLowestBias : t;
 }
 
-// Workgroups go round the XCDs one by one: gives each XCD a run of consecutive
-// work items, which share keys, values or queries in its L2.  Grid: 8 * ceil(n / 8).
-__device__ __forceinline__ uint32_t xcd_item(uint32_t n) { return blockIdx.x % 8 * ((n + 7) / 8) + blockIdx.x / 8; }
-inline unsigned xcd_grid(uint32_t n) { return (n + 7) / 8 * 8; }
+// Workgroups go round the XCDs one by one: gives each XCD runs of `run`
+// consecutive work items, which share keys, values or queries in its L2.
+__device__ __forceinline__ uint32_t xcd_item(uint32_t run) {
+    const uint32_t k = blockIdx.x / 8;
+    return (k / run * 8 + blockIdx.x % 8) * run + k % run;
+}
+inline unsigned xcd_grid(uint32_t n, uint32_t run) { return ((n + run - 1) / run + 7) / 8 * 8 * run; }
+// One run an XCD where all items cost the same.  With lengths, which the host
+// does not see, whole runs may have nothing to do: eight and more an XCD (3 x
+// 4050 queries of 5 heads, fp32, 1013, 845 and no keys: the step 615 us with one run, 458 us so).
+inline uint32_t xcd_run(const AttendArgs& a, uint32_t n) { return (n + (a.lengths ? 63 : 7)) / (a.lengths ? 64 : 8) + (n == 0); }
 
 // First of the tiles of part `part` when `tiles` are dealt to `parts`.
 __device__ __forceinline__ int first_tile(int tiles, int part, int parts) {
@@ -200,9 +207,25 @@ struct TileOf {
         const f16 zero = {0.0f};
         return scores(tile, l, k, f, D, zero);
     }
+    // fp32 heads whose last 32 entries are eight or fewer in use: 16 products of
+    // 64 clocks for those would take more time than their multiply-adds on the
+    // vector unit (heads of 36, dk and dv of 4050 queries and 1013 keys: 275 us, 217 so).  The
+    // first registers of the last accumulator then hold the lane's own sums over
+    // the rows that stand in its registers, which settle() joins and puts in place.
+    static __device__ __forceinline__ bool tail(int D) { return std::is_same<T, float>::value && D <= DP - 24; }
+    static __device__ __forceinline__ void settle(f16 (&o)[DP / 32], int D, int lane) {
+        if (!tail(D)) return;
+        f16& e = o[DP / 32 - 1];
+#pragma unroll
+        for (int r = 0; r < 8; ++r) e[r] += other_half(e[r]);
+#pragma unroll
+        for (int r = 0; r < 4; ++r) e[r] = lane < 32 ? e[r] : e[4 + r];
+#pragma unroll
+        for (int r = 4; r < 16; ++r) e[r] = 0.0f;
+    }
     // o[D / 32] += (rows 32 k .. 32 k + 31 of the tile)^T x p
     static __device__ __forceinline__ void values(const lds_t* tile, const Lane& l, int k, const typename Mat<T>::Probs& p,
-                                                  f16 (&o)[DP / 32]) {
+                                                  int D, int lane, f16 (&o)[DP / 32]) {
         if constexpr (std::is_same<T, __bf16>::value) {
             typedef __attribute__((address_space(3))) s4 V;
 #pragma unroll
@@ -220,8 +243,29 @@ struct TileOf {
             typedef __attribute__((address_space(3))) const float V;
             // The 32 rows' own sum first, then onto o: a chain of roundings as
             // long as the tiles, not as the rows.
+            const bool few = tail(D);
 #pragma unroll
             for (int d = 0; d < DP / 32; ++d) {
+                if (d == DP / 32 - 1 && few) {
+                    const int h = lane / 32;
+                    f4 t0 = {0.0f}, t1 = {0.0f};
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) {
+                        // chunks 8 d and 8 d + 1 of row 8 (i / 4) + 4 h + i % 4
+                        typedef __attribute__((address_space(3))) const f4 C;
+                        const int r = 8 * ((i / 4) % 2) + 4 * h + i % 4, f = r / 4;
+                        const lds_t* at = tile + 2 * d * 1024 + (2 * k + i / 8) * kStep16 + r * 64;
+                        const f4 a = *(C*)(at + f * 16), b = *(C*)(at + (1 ^ f) * 16);
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) {
+                            t0[j] = fmaf(p.v[i], a[j], t0[j]);
+                            t1[j] = fmaf(p.v[i], b[j], t1[j]);
+                        }
+                    }
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) o[d][j] += t0[j], o[d][4 + j] += t1[j];
+                    continue;
+                }
                 f16 t;
 #pragma unroll
                 for (int i = 0; i < 16; ++i) t[i] = 0.0f;

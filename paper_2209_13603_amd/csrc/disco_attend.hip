@@ -20,7 +20,7 @@ namespace {
 // keys in `splits` parts.  Parts leave unnormed sums, joined by k_attend_join.
 constexpr int kRows = 32 * kAttendWaves;
 struct Cut {
-    uint32_t rows, row_blocks, items;
+    uint32_t rows, row_blocks, items, run;
     int32_t splits;
     float* part;   // [splits][all rows][dim]
     float* stat;   // [splits][all rows][2]
@@ -44,7 +44,7 @@ __global__ __launch_bounds__(kAttendThreads, (kWorkgroups<T, DP>)) void k_attend
     __shared__ float starts[2][KT];
     lds_t* lds = (lds_t*)smem;
 
-    const uint32_t id = xcd_item(c.items);
+    const uint32_t id = xcd_item(c.run);
     if (id >= c.items) return;
     const int split = (int)(id % c.splits);
     const uint32_t rb = id / c.splits % c.row_blocks;
@@ -150,13 +150,14 @@ __global__ __launch_bounds__(kAttendThreads, (kWorkgroups<T, DP>)) void k_attend
                 s[k][r] = __builtin_amdgcn_exp2f(fmaf(s[k][r], scale2, neg));
                 sum += s[k][r];
             }
-            Tile::values(vt, ln, k, s[k], o);
+            Tile::values(vt, ln, k, s[k], a.dim, lane, o);
         }
         l += sum;
         if (more) store(buf ^ 1);
         __syncthreads();
     }
     l += other_half(l);
+    Tile::settle(o, a.dim, lane);
     const int64_t stat = ((int64_t)b * a.heads + h) * a.queries + i;
     if (c.splits > 1) {
         const int64_t all = (int64_t)a.batch * a.kv_heads * c.rows;
@@ -240,6 +241,7 @@ Cut cut_of(const AttendArgs& a) {
     const int64_t want = blocks > 0 ? (2 * 256 + blocks - 1) / blocks : 1;
     c.splits = (int32_t)std::max<int64_t>(1, std::min<int64_t>({want, tiles / 4, 256}));
     c.items = (uint32_t)(blocks * c.splits);
+    c.run = xcd_run(a, c.items);
     return c;
 }
 
@@ -250,8 +252,8 @@ size_t part_bytes(const AttendArgs& a, const Cut& c) {
 
 template <typename T, int DP>
 void launch(const AttendArgs& a, const Cut& c) {
-    if (c.wide) hipLaunchKernelGGL((k_attend<T, DP, true>), dim3(xcd_grid(c.items)), dim3(kAttendThreads), 0, a.stream, a, c);
-    else hipLaunchKernelGGL((k_attend<T, DP, false>), dim3(xcd_grid(c.items)), dim3(kAttendThreads), 0, a.stream, a, c);
+    if (c.wide) hipLaunchKernelGGL((k_attend<T, DP, true>), dim3(xcd_grid(c.items, c.run)), dim3(kAttendThreads), 0, a.stream, a, c);
+    else hipLaunchKernelGGL((k_attend<T, DP, false>), dim3(xcd_grid(c.items, c.run)), dim3(kAttendThreads), 0, a.stream, a, c);
 }
 
 template <typename T>

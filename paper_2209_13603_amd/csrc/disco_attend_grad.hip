@@ -23,7 +23,7 @@ constexpr int kCols = 32 * kAttendWaves;  // rows (dq) or keys (dk, dv) of a wor
 constexpr int kKeys = 32, kQueries = 32;  // keys, queries of a tile
 
 struct GradCut {
-    uint32_t rows, row_blocks, key_blocks, items_q, items_k;
+    uint32_t rows, row_blocks, key_blocks, items_q, items_k, run_q, run_k;
     int32_t splits_q, splits_k;
     f4* row_c;    // [batch][heads][queries]: -reference, 1 / sum, delta, written with dq for dk and dv
     float* part;  // [splits][...][dim]
@@ -48,7 +48,7 @@ __global__ __launch_bounds__(kAttendThreads, (kWorkgroups<T, DP>)) void k_attend
     __shared__ float starts[2][KT];
     lds_t* lds = (lds_t*)smem;
 
-    const uint32_t id = xcd_item(c.items_q);
+    const uint32_t id = xcd_item(c.run_q);
     if (id >= c.items_q) return;
     const int split = (int)(id % c.splits_q);
     const uint32_t rb = id / c.splits_q % c.row_blocks;
@@ -144,10 +144,11 @@ __global__ __launch_bounds__(kAttendThreads, (kWorkgroups<T, DP>)) void k_attend
         const f16 dp = Tile::scores(vt, ln, 0, gf, a.dim);
 #pragma unroll
         for (int r = 0; r < 16; ++r) s[r] = __builtin_amdgcn_exp2f(fmaf(s[r], scale2, neg)) * (dp[r] - delta);
-        Tile::values(kt, ln, 0, s, dq);
+        Tile::values(kt, ln, 0, s, a.dim, lane, dq);
         if (more) store(buf ^ 1);
         __syncthreads();
     }
+    Tile::settle(dq, a.dim, lane);
     const float f = inv * a.scale;
     if (c.splits_q > 1) {
         const int64_t all = (int64_t)a.batch * a.kv_heads * c.rows;
@@ -170,7 +171,7 @@ __global__ __launch_bounds__(kAttendThreads, (kWorkgroups<T, DP>)) void k_attend
     __shared__ __align__(16) float row_c[2][4][QT];  // GradCut::row_c of the tile's rows
     lds_t* lds = (lds_t*)smem;
 
-    const uint32_t id = xcd_item(c.items_k);
+    const uint32_t id = xcd_item(c.run_k);
     if (id >= c.items_k) return;
     const int split = (int)(id % c.splits_k);
     const uint32_t kb = id / c.splits_k % c.key_blocks;
@@ -270,12 +271,14 @@ __global__ __launch_bounds__(kAttendThreads, (kWorkgroups<T, DP>)) void k_attend
             ds.set(q, f);
         }
         if constexpr (kept) __builtin_amdgcn_sched_barrier(0);
-        Tile::values(gt, ln, 0, p, dv);
+        Tile::values(gt, ln, 0, p, a.dim, lane, dv);
         if constexpr (kept) __builtin_amdgcn_sched_barrier(0);
-        Tile::values(qt, ln, 0, ds, dk);
+        Tile::values(qt, ln, 0, ds, a.dim, lane, dk);
         if (more) store(buf ^ 1);
         __syncthreads();
     }
+    Tile::settle(dk, a.dim, lane);
+    Tile::settle(dv, a.dim, lane);
     if (!live)  // nothing of a key that is taken out
 #pragma unroll
         for (int d = 0; d < DP / 32; ++d)
@@ -328,6 +331,8 @@ GradCut cut_of(const AttendArgs& a) {
     c.splits_k = parts(bk, (a.queries + kQueries - 1) / kQueries * G, 8);
     c.items_q = (uint32_t)(bq * c.splits_q);
     c.items_k = (uint32_t)(bk * c.splits_k);
+    c.run_q = xcd_run(a, c.items_q);
+    c.run_k = xcd_run(a, c.items_k);
     return c;
 }
 
@@ -336,13 +341,13 @@ size_t row_bytes(const AttendArgs& a) { return round256((size_t)a.batch * a.head
 
 template <typename T, int DP>
 void launch_dq(const AttendArgs& a, const GradCut& c) {
-    if (c.wide) hipLaunchKernelGGL((k_attend_dq<T, DP, true>), dim3(xcd_grid(c.items_q)), dim3(kAttendThreads), 0, a.stream, a, c);
-    else hipLaunchKernelGGL((k_attend_dq<T, DP, false>), dim3(xcd_grid(c.items_q)), dim3(kAttendThreads), 0, a.stream, a, c);
+    if (c.wide) hipLaunchKernelGGL((k_attend_dq<T, DP, true>), dim3(xcd_grid(c.items_q, c.run_q)), dim3(kAttendThreads), 0, a.stream, a, c);
+    else hipLaunchKernelGGL((k_attend_dq<T, DP, false>), dim3(xcd_grid(c.items_q, c.run_q)), dim3(kAttendThreads), 0, a.stream, a, c);
 }
 template <typename T, int DP>
 void launch_dkv(const AttendArgs& a, const GradCut& c) {
-    if (c.wide) hipLaunchKernelGGL((k_attend_dkv<T, DP, true>), dim3(xcd_grid(c.items_k)), dim3(kAttendThreads), 0, a.stream, a, c);
-    else hipLaunchKernelGGL((k_attend_dkv<T, DP, false>), dim3(xcd_grid(c.items_k)), dim3(kAttendThreads), 0, a.stream, a, c);
+    if (c.wide) hipLaunchKernelGGL((k_attend_dkv<T, DP, true>), dim3(xcd_grid(c.items_k, c.run_k)), dim3(kAttendThreads), 0, a.stream, a, c);
+    else hipLaunchKernelGGL((k_attend_dkv<T, DP, false>), dim3(xcd_grid(c.items_k, c.run_k)), dim3(kAttendThreads), 0, a.stream, a, c);
 }
 
 template <typename T>

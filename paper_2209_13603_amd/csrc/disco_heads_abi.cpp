@@ -305,18 +305,18 @@ void take_attend(Device* d, const AttendArgs& a, const disco_heads_t* q, const d
 }
 
 // ---- gradient clipping ------------------------------------------------------------
-int64_t check_gradient(const disco_tensor_t& t, const std::string& name) {
-    if (t.dtype != DISCO_FLOAT32 && t.dtype != DISCO_BFLOAT16) refuse(DISCO_ERR_DTYPE, name + " has an unknown dtype");
-    if (t.ndim < 0 || t.ndim > 4) refuse(DISCO_ERR_SHAPE, name + " needs 0 to 4 axes");
+int64_t check_gradient(const disco_tensor_t& t, const char* list, int32_t i) {
+    auto no = [&](disco_status_t status, const char* why) { refuse(status, std::string(list) + "[" + std::to_string(i) + "]" + why); };
+    if (t.dtype != DISCO_FLOAT32 && t.dtype != DISCO_BFLOAT16) no(DISCO_ERR_DTYPE, " has an unknown dtype");
+    if (t.ndim < 0 || t.ndim > 4) no(DISCO_ERR_SHAPE, " needs 0 to 4 axes");
     int64_t n = 1;
-    for (int i = 0; i < t.ndim; ++i) {
-        if (t.shape[i] < 0) refuse(DISCO_ERR_SHAPE, name + " has a negative size");
-        if (t.shape[i] > 0 && n > kMaxOffset / t.shape[i]) refuse(DISCO_ERR_SHAPE, name + " is too large");
-        n *= t.shape[i];
+    for (int k = 0; k < t.ndim; ++k) {
+        if (t.shape[k] < 0) no(DISCO_ERR_SHAPE, " has a negative size");
+        if (t.shape[k] > 0 && n > kMaxOffset / t.shape[k]) no(DISCO_ERR_SHAPE, " is too large");
+        n *= t.shape[k];
     }
-    if (n > 0 && !t.data) refuse(DISCO_ERR_INVALID_ARGUMENT, name + ".data is NULL");
-    if ((uintptr_t)t.data % bytes_of(t.dtype) != 0)
-        refuse(DISCO_ERR_INVALID_ARGUMENT, name + ".data is not aligned to its type");
+    if (n > 0 && !t.data) no(DISCO_ERR_INVALID_ARGUMENT, ".data is NULL");
+    if ((uintptr_t)t.data % bytes_of(t.dtype) != 0) no(DISCO_ERR_INVALID_ARGUMENT, ".data is not aligned to its type");
     return n;
 }
 
@@ -326,15 +326,15 @@ std::vector<ClipTensor> check_gradients(int32_t count, const disco_tensor_t* gra
     std::vector<ClipTensor> v((size_t)count);
     for (int32_t i = 0; i < count; ++i) {
         const disco_tensor_t& g = grads[i];
-        v[i] = ClipTensor{g.data, nullptr, check_gradient(g, "grads[" + std::to_string(i) + "]"), g.dtype == DISCO_BFLOAT16};
+        v[i] = ClipTensor{g.data, nullptr, check_gradient(g, "grads", i), g.dtype == DISCO_BFLOAT16};
         if (!clipped) continue;
         const disco_tensor_t& c = clipped[i];
-        const std::string name = "clipped[" + std::to_string(i) + "]";
-        (void)check_gradient(c, name);
-        if (c.dtype != g.dtype) refuse(DISCO_ERR_DTYPE, name + " has another dtype than its gradient");
+        (void)check_gradient(c, "clipped", i);
+        if (c.dtype != g.dtype)
+            refuse(DISCO_ERR_DTYPE, "clipped[" + std::to_string(i) + "] has another dtype than its gradient");
         bool same = c.ndim == g.ndim;
         for (int a = 0; same && a < g.ndim; ++a) same = c.shape[a] == g.shape[a];
-        if (!same) refuse(DISCO_ERR_SHAPE, name + " has another shape than its gradient");
+        if (!same) refuse(DISCO_ERR_SHAPE, "clipped[" + std::to_string(i) + "] has another shape than its gradient");
         v[i].out = c.data;
     }
     return v;
