@@ -209,7 +209,7 @@ struct TileOf {
     }
     // fp32 heads whose last 32 entries are eight or fewer in use: 16 products of
     // 64 clocks for those would take more time than their multiply-adds on the
-    // vector unit (heads of 36, dk and dv of 4050 queries and 1013 keys: 275 us, 217 so).  The
+    // vector unit (heads of 36, the step of 3 x 4050 queries to 1013 states: 511 us, 482 so).  The
     // first registers of the last accumulator then hold the lane's own sums over
     // the rows that stand in its registers, which settle() joins and puts in place.
     static __device__ __forceinline__ bool tail(int D) { return std::is_same<T, float>::value && D <= DP - 24; }

@@ -189,40 +189,64 @@ __global__ __launch_bounds__(kAttendThreads, (kWorkgroups<T, DP>)) void k_attend
     }
 }
 
-// Joins the parts of each row, in the order of the keys.  One wave a row.
-// grid: ceil(rows of all items / 4).
+// Joins the parts of each row.  A thread holds four entries of a row; where the
+// rows are few, `slices` threads share its parts, and their sums are added in
+// slice order.
+struct Join {
+    int lanes, slices, rows;  // threads of four entries, slices, rows of a workgroup
+};
 template <typename T>
-__global__ __launch_bounds__(kAttendThreads) void k_attend_join(AttendArgs a, Cut c) {
-    const int lane = threadIdx.x % kWave, G = a.heads / a.kv_heads;
-    const int64_t all = (int64_t)a.batch * a.kv_heads * c.rows;
-    const int64_t at = (int64_t)blockIdx.x * kAttendWaves + threadIdx.x / kWave;
-    if (at >= all) return;
-    float m = -INFINITY;
-    for (int s = 0; s < c.splits; ++s) m = fmaxf(m, c.stat[2 * (s * all + at)]);
-    const float ms = m == -INFINITY ? 0.0f : m;
-    float l = 0.0f, o0 = 0.0f, o1 = 0.0f;
-    const bool d0 = lane < a.dim, d1 = lane + 64 < a.dim;
+__global__ __launch_bounds__(kAttendThreads) void k_attend_join(AttendArgs a, Cut c, Join g) {
+    __shared__ f4 part[kAttendThreads];
+    __shared__ float sums[kAttendThreads];
+    const int lane = threadIdx.x % g.lanes, slice = threadIdx.x / g.lanes % g.slices, r = threadIdx.x / (g.lanes * g.slices);
+    const int64_t all = (int64_t)a.batch * a.kv_heads * c.rows, at = (int64_t)blockIdx.x * g.rows + r;
+    const bool live = r < g.rows && at < all;
+    const int d = 4 * lane, n = min(4, a.dim - d);
+    float m = -INFINITY, l = 0.0f;
+    f4 o = {0.0f};
+    if (live) {
+#pragma unroll 8
+        for (int s = 0; s < c.splits; ++s) m = fmaxf(m, c.stat[2 * (s * all + at)]);
+        const float ms = m == -INFINITY ? 0.0f : m;
 #pragma unroll 4
-    for (int s = 0; s < c.splits; ++s) {
-        const float f = __builtin_amdgcn_exp2f(c.stat[2 * (s * all + at)] - ms);
-        const float* p = c.part + (s * all + at) * a.dim;
-        l = fmaf(f, c.stat[2 * (s * all + at) + 1], l);
-        if (d0) o0 = fmaf(f, p[lane], o0);
-        if (d1) o1 = fmaf(f, p[lane + 64], o1);
+        for (int s = slice; s < c.splits; s += g.slices) {
+            const float f = __builtin_amdgcn_exp2f(c.stat[2 * (s * all + at)] - ms);
+            const float* p = c.part + (s * all + at) * a.dim + d;
+            f4 v = {0.0f};
+            if (a.dim % 4 == 0) v = *(const f4*)p;
+            else
+                for (int j = 0; j < n; ++j) v[j] = p[j];
+            l = fmaf(f, c.stat[2 * (s * all + at) + 1], l);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) o[j] = fmaf(f, v[j], o[j]);
+        }
     }
-    const float inv = l == 0.0f ? 0.0f : 1.0f / l;
-    const int64_t row = at % c.rows, bh = at / c.rows, b = bh / a.kv_heads, i = row / G;
-    const int h = (int)(bh % a.kv_heads) * G + (int)(row % G);
-    T* out = (T*)a.out.p + b * a.out.sb + i * a.out.st + h * a.out.sh;
-    o0 *= inv;
-    o1 *= inv;
-    if (d0) out[lane] = (T)o0;
-    if (d1) out[lane + 64] = (T)o1;
-    if (a.low.p) {
-        T* low = (T*)a.low.p + b * a.low.sb + i * a.low.st + h * a.low.sh;
-        if (d0) low[lane] = (T)(o0 - (float)(T)o0);
-        if (d1) low[lane + 64] = (T)(o1 - (float)(T)o1);
+    if (g.slices > 1) {
+        part[threadIdx.x] = o;
+        sums[threadIdx.x] = l;
+        __syncthreads();
+        if (slice == 0)
+            for (int s = 1; s < g.slices; ++s) {
+                o += part[threadIdx.x + s * g.lanes];
+                l += sums[threadIdx.x + s * g.lanes];
+            }
     }
+    if (!live || slice != 0) return;
+    o *= l == 0.0f ? 0.0f : 1.0f / l;
+    const int G = a.heads / a.kv_heads;
+    const uint32_t bh = (uint32_t)(at / c.rows), row = (uint32_t)(at - (int64_t)bh * c.rows);
+    const int64_t b = bh / (uint32_t)a.kv_heads, i = row / (uint32_t)G;
+    const int h = (int)(bh % (uint32_t)a.kv_heads) * G + (int)(row % (uint32_t)G);
+    T* out = (T*)a.out.p + b * a.out.sb + i * a.out.st + h * a.out.sh + d;
+    T* low = a.low.p ? (T*)a.low.p + b * a.low.sb + i * a.low.st + h * a.low.sh + d : nullptr;
+    typedef T T4 __attribute__((ext_vector_type(4)));
+    const T4 v = __builtin_convertvector(o, T4);
+    if (c.wide) *(T4*)out = v;
+    else
+        for (int j = 0; j < n; ++j) out[j] = v[j];
+    if (low)
+        for (int j = 0; j < n; ++j) low[j] = (T)(o[j] - (float)v[j]);
     if (a.stats && lane == 0) {
         float* st = a.stats + 2 * ((b * a.heads + h) * a.queries + i);
         st[0] = m;
@@ -290,9 +314,14 @@ hipError_t launch_attend(const AttendArgs& a, void* ws) {
     if (err != hipSuccess || c.splits == 1) return err;
     const int64_t all = (int64_t)a.batch * a.kv_heads * c.rows;
     tk = timing_begin("attend_join", a.stream);
-    const dim3 grid((unsigned)((all + kAttendWaves - 1) / kAttendWaves));
-    if (a.bf16) hipLaunchKernelGGL(k_attend_join<__bf16>, grid, dim3(kAttendThreads), 0, a.stream, a, c);
-    else hipLaunchKernelGGL(k_attend_join<float>, grid, dim3(kAttendThreads), 0, a.stream, a, c);
+    Join g;
+    g.lanes = (a.dim + 3) / 4;
+    g.slices = 1;
+    while (2 * g.slices <= c.splits && 2 * g.slices * g.lanes <= kAttendThreads && all * g.lanes * g.slices < 65536) g.slices *= 2;
+    g.rows = kAttendThreads / (g.lanes * g.slices);
+    const dim3 grid((unsigned)((all + g.rows - 1) / g.rows));
+    if (a.bf16) hipLaunchKernelGGL(k_attend_join<__bf16>, grid, dim3(kAttendThreads), 0, a.stream, a, c, g);
+    else hipLaunchKernelGGL(k_attend_join<float>, grid, dim3(kAttendThreads), 0, a.stream, a, c, g);
     timing_end(tk, a.stream);
     return hipGetLastError();
 }
