@@ -121,7 +121,7 @@ __global__ __launch_bounds__(kAttendThreads, (kWorkgroups<T, DP>)) void k_attend
 #pragma unroll
                     for (int r = 0; r < 4; ++r) s[k][4 * q + r] = v[r];
                 }
-                s[k] = Tile::scores(kt, ln, k, qf, a.dim, s[k]);
+                s[k] = Tile::scores_from(s[k], kt, ln, k, qf, a.dim);
             }
         }
         float top = s[0][0];

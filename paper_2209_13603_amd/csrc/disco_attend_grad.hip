@@ -139,7 +139,7 @@ __global__ __launch_bounds__(kAttendThreads, (kWorkgroups<T, DP>)) void k_attend
 #pragma unroll
                 for (int r = 0; r < 4; ++r) s[4 * q + r] = v[r];
             }
-            s = Tile::scores(kt, ln, 0, qf, a.dim, s);
+            s = Tile::scores_from(s, kt, ln, 0, qf, a.dim);
         }
         const f16 dp = Tile::scores(vt, ln, 0, gf, a.dim);
 #pragma unroll
@@ -250,8 +250,8 @@ __global__ __launch_bounds__(kAttendThreads, (kWorkgroups<T, DP>)) void k_attend
         f16 s;
 #pragma unroll
         for (int r = 0; r < 16; ++r) s[r] = start;
-        if constexpr (kept) s = Tile::scores_kept(qt, ln, 0, mine, lane, a.dim, s);
-        else s = Tile::scores(qt, ln, 0, kf, a.dim, s);
+        if constexpr (kept) s = Tile::scores_kept(s, qt, ln, 0, mine, lane, a.dim);
+        else s = Tile::scores_from(s, qt, ln, 0, kf, a.dim);
         if constexpr (kept) __builtin_amdgcn_sched_barrier(0);
         const f16 dp = Tile::scores(gt, ln, 0, vf, a.dim);
         if constexpr (kept) __builtin_amdgcn_sched_barrier(0);
