@@ -36,10 +36,12 @@ _DTYPES = {}
 
 
 def _dtype(t):
-    if not _DTYPES:
+    code = _DTYPES.get(t.dtype)
+    if code is None:
         import torch
         _DTYPES.update({torch.float32: DISCO_FLOAT32, torch.bfloat16: DISCO_BFLOAT16})
-    return _DTYPES.get(t.dtype, 99)
+        code = _DTYPES.get(t.dtype, 99)
+    return code
 
 
 def _heads(t, name) -> Heads:
@@ -74,22 +76,30 @@ def _same_device(first, *others):
 class _Call:
     """The stream of one call, and where its outputs and scratch memory come from: torch's allocator,
     on that stream."""
-    __slots__ = ("device", "stream", "handle")
+    __slots__ = ("first", "stream", "handle")
 
     def __init__(self, t, stream):
         import torch
         if not t.is_cuda:
             raise ValueError("tensors must be on a GPU")
-        self.device = t.device
+        self.first = t
         self.stream = stream
         self.handle = torch._C._cuda_getCurrentRawStream(t.get_device()) if stream is None else stream.cuda_stream
+
+    def like(self, t):
+        """A new dense tensor of t's shape and type."""
+        import torch
+        if self.stream is None:
+            return torch.empty_like(t, memory_format=torch.contiguous_format)
+        with torch.cuda.stream(self.stream):
+            return torch.empty_like(t, memory_format=torch.contiguous_format)
 
     def empty(self, shape, dtype):
         import torch
         if self.stream is None:
-            return torch.empty(shape, dtype=dtype, device=self.device)
+            return self.first.new_empty(shape, dtype=dtype)
         with torch.cuda.stream(self.stream):
-            return torch.empty(shape, dtype=dtype, device=self.device)
+            return self.first.new_empty(shape, dtype=dtype)
 
     def workspace(self, name, *args):
         """(tensor to keep until the call is enqueued, address, bytes)"""
@@ -139,7 +149,7 @@ def norm_rotate(x, weight=None, rotation=None, layout="half", positions=None, fi
     """
     call = _Call(x, stream)
     if y is None:
-        y = call.empty(x.shape, x.dtype)
+        y = call.like(x)
     _same_device(x, weight, y)
     hx, hy = _heads(x, "x"), _heads(y, "y")
     tw = _tensor(weight) if weight is not None else None
@@ -154,8 +164,8 @@ def norm_rotate_backward(x, weight, dy, rotation=None, layout="half", positions=
     a weight, not there.  x may be None without the norm.  dx: None, dy itself, or a tensor to write to."""
     call = _Call(dy, stream)
     if want_dx and dx is None:
-        dx = call.empty(dy.shape, dy.dtype)
-    dw = call.empty(weight.shape, weight.dtype) if want_dw and weight is not None else None
+        dx = call.like(dy)
+    dw = call.like(weight) if want_dw and weight is not None else None
     _same_device(dy, x, weight, dx)
     hx = _heads(x, "x") if x is not None else None
     hdy = _heads(dy, "dy")
@@ -193,12 +203,12 @@ def cross_attention(q, k, v, key_bias=None, key_lengths=None, scale=None, return
     import torch
     call = _Call(q, stream)
     if out is None:
-        out = call.empty(q.shape, q.dtype)
+        out = call.like(q)
     if scale == 0.0:
         raise ValueError("scale must not be 0")
     _same_device(q, k, v, out)
     rows = call.empty((q.shape[0], q.shape[2], q.shape[1], 2), torch.float32) if return_stats else None
-    low = call.empty(q.shape, q.dtype) if return_stats and q.dtype == torch.bfloat16 else None
+    low = call.like(q) if return_stats and q.dtype == torch.bfloat16 else None
     hlow = _heads(low, "low") if low is not None else None
     hq, hk = _heads(q, "q"), _heads(k, "k")
     opt = _options(q, k, key_bias, key_lengths, scale)
@@ -216,9 +226,9 @@ def cross_attention_backward(q, k, v, out, stats, dout, key_bias=None, key_lengt
     of one joint buffer."""
     import torch
     call = _Call(q, stream)
-    dq = call.empty(q.shape, q.dtype) if dq is None else dq
-    dk = call.empty(k.shape, k.dtype) if dk is None else dk
-    dv = call.empty(v.shape, v.dtype) if dv is None else dv
+    dq = call.like(q) if dq is None else dq
+    dk = call.like(k) if dk is None else dk
+    dv = call.like(v) if dv is None else dv
     if scale == 0.0:
         raise ValueError("scale must not be 0")
     rows, low = stats

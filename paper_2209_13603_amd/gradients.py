@@ -2,9 +2,11 @@
 ``include/disco.h``) on torch tensors.  Argument marshalling only."""
 from __future__ import annotations
 
+import operator
+
 import numpy as np
 
-from .attention import _Call, _dtype, _same_device
+from .attention import _Call, _dtype
 from .disco import _check, library
 
 # disco_tensor_t
@@ -13,13 +15,14 @@ _TENSOR = np.dtype([("data", "u8"), ("dtype", "i4"), ("ndim", "i4"), ("shape", "
 
 def _array(tensors):
     """The tensors as an array of disco_tensor_t, each as one axis of its entries."""
+    import torch
     a = np.zeros(len(tensors), dtype=_TENSOR)
-    if not all([t.is_contiguous() for t in tensors]):
+    if not all(map(torch.Tensor.is_contiguous, tensors)):
         raise ValueError("gradients must be contiguous")
-    a["data"] = [t.data_ptr() for t in tensors]
-    a["dtype"] = [_dtype(t) for t in tensors]
+    a["data"] = list(map(torch.Tensor.data_ptr, tensors))
+    a["dtype"] = list(map(_dtype, tensors))
     a["ndim"] = 1
-    a["shape"][:, 0] = [t.numel() for t in tensors]
+    a["shape"][:, 0] = list(map(torch.Tensor.numel, tensors))
     return a
 
 
@@ -36,9 +39,11 @@ def clip(grads, max_norm, eps=1e-6, out=None, norm_only=False, stream=None):
     if not grads:
         raise ValueError("no gradients")
     apart = out is not grads
-    if apart and [t.shape for t in out] != [t.shape for t in grads]:
+    shapes = operator.attrgetter("shape")
+    if apart and list(map(shapes, out)) != list(map(shapes, grads)):
         raise ValueError("out must match the gradients one by one")
-    _same_device(*grads, *(out if apart else ()))
+    if len(set(map(torch.Tensor.get_device, grads + out if apart else grads))) != 1:
+        raise ValueError("all tensors must be on %s" % grads[0].device)
     call = _Call(grads[0], stream)
     norm = call.empty((), torch.float32)
     a = _array(grads)
