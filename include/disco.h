@@ -412,7 +412,8 @@ typedef struct {
  * the mean over the head's dim entries.  norm = 0: rotation alone (weight
  * NULL).  weight: NULL (ones), [dim] for all heads, or [heads, dim]; x's type.
  * rotation: NULL for the norm alone.  y has x's sizes and may be x itself (same
- * data and strides), otherwise must not overlap it.  Errors: INVALID_ARGUMENT,
+ * data and strides), otherwise must not overlap it.  batch * tokens * heads < 2^31.
+ * Errors: INVALID_ARGUMENT,
  * SHAPE, DTYPE, DEVICE. */
 disco_status_t disco_norm_rotate(const disco_heads_t* x, int32_t norm, const disco_tensor_t* weight,
                                  double eps, const disco_rotation_t* rotation, disco_heads_t* y,
@@ -452,7 +453,10 @@ typedef struct {
  *          dout . out do not carry out's rounding.
  * The split of a long axis of keys between workgroups depends on the sizes
  * alone, and partial sums are joined in a fixed order.
- * options NULL: defaults.  batch * heads <= 65535 * 8.  Errors:
+ * options NULL: defaults.  batch * heads <= 65535 * 8, tokens * heads < 2^31 (q), batch *
+ * tokens * heads < 2^35.  Rows of whole 16-byte pieces (dim a multiple of 8 in
+ * bf16 and 4 in fp32, strides and addresses likewise) take the fast loads; others
+ * are read entry by entry, about five times slower.  Errors:
  * INVALID_ARGUMENT, SHAPE, DTYPE, OUT_OF_MEMORY, DEVICE. */
 disco_status_t disco_cross_attention(const disco_heads_t* q, const disco_heads_t* k, const disco_heads_t* v,
                                      const disco_attention_t* options, disco_heads_t* out, float* stats,

@@ -125,6 +125,24 @@ def test_against_the_definition(shape, dtype, mask):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("shape", [(2, 1, 4000, 4, 4, 36), (1, 2, 6000, 8, 2, 127), (3, 1, 2500, 2, 1, 1), (1, 5, 3001, 3, 3, 100),
+                                   (2, 1, 9000, 16, 2, 64), (1, 40, 2049, 2, 2, 30)])
+def test_few_rows_against_many_keys(shape, dtype):
+    """The keys in parts, and their join, for every width of a row."""
+    import torch
+    B, Sq, Sk, H, Hk, D = shape
+    g = torch.Generator(device="cuda:0").manual_seed(Sk)
+    mk = lambda *s: torch.randn(s, generator=g, device="cuda:0").to(_dt(dtype))
+    q, k, v, dout = (1.5 * mk(B, Sq, H, D)).to(_dt(dtype)), mk(B, Sk, Hk, D), mk(B, Sk, Hk, D), mk(B, Sq, H, D)
+    bias = torch.randn(B, Sk, generator=g, device="cuda:0")
+    bias[:, 100:700] = -math.inf  # whole tiles, and with them a part of the split, have no key
+    lengths = torch.tensor([Sk] + [130 + 40 * b for b in range(1, B)], dtype=torch.int32, device="cuda:0")
+    want = _exact(q, k, v, dout, bias, lengths, 1 / math.sqrt(D))
+    for name, a, b in zip(("out", "dq", "dk", "dv"), _run(q, k, v, dout, key_bias=bias, key_lengths=lengths), want):
+        _close(name, a, b, TOL[dtype])
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
 def test_rows_without_keys_and_lengths_out_of_range(dtype):
     import torch
     g = torch.Generator(device="cuda:0").manual_seed(1)
