@@ -454,9 +454,9 @@ typedef struct {
  * The split of a long axis of keys between workgroups depends on the sizes
  * alone, and partial sums are joined in a fixed order.
  * options NULL: defaults.  batch * heads <= 65535 * 8, tokens * heads < 2^31 (q), batch *
- * tokens * heads < 2^35.  Rows of whole 16-byte pieces (dim a multiple of 8 in
- * bf16 and 4 in fp32, strides and addresses likewise) take the fast loads; others
- * are read entry by entry, about five times slower.  Errors:
+ * tokens * heads < 2^35.  Rows of whole 16-byte pieces (dim, strides and addresses) go
+ * fastest, rows of whole 8-byte pieces nearly so; others are read entry by entry,
+ * two to five times slower.  Errors:
  * INVALID_ARGUMENT, SHAPE, DTYPE, OUT_OF_MEMORY, DEVICE. */
 disco_status_t disco_cross_attention(const disco_heads_t* q, const disco_heads_t* k, const disco_heads_t* v,
                                      const disco_attention_t* options, disco_heads_t* out, float* stats,

@@ -38,6 +38,8 @@ typedef __bf16 bf4 __attribute__((ext_vector_type(4)));
 typedef short s4 __attribute__((ext_vector_type(4)));
 typedef short s8 __attribute__((ext_vector_type(8)));
 typedef uint32_t u4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u2 __attribute__((ext_vector_type(2)));
+typedef float f2 __attribute__((ext_vector_type(2)));
 typedef __attribute__((address_space(3))) char lds_t;
 
 constexpr int kWave = 64;
@@ -295,12 +297,17 @@ struct TileOf {
     }
 };
 
-// 16 bytes of a row from entry c on, zeros beyond D.  W: in one load.
-template <typename T, bool W>
+// 16 bytes of a row from entry c on, zeros beyond D.  W = 2: in one load, 1: in
+// two, 0: entry by entry.
+template <typename T, int W>
 __device__ __forceinline__ u4 load_chunk(const T* row, int c, int D) {
     constexpr int CH = Mat<T>::CH;
     if (c >= D) return u4{0u, 0u, 0u, 0u};
-    if constexpr (W) return *(const u4*)(row + c);
+    if constexpr (W == 2) return *(const u4*)(row + c);
+    if constexpr (W == 1) {
+        const u2 z = {0u, 0u}, lo = *(const u2*)(row + c), hi = c + CH / 2 < D ? *(const u2*)(row + c + CH / 2) : z;
+        return u4{lo[0], lo[1], hi[0], hi[1]};
+    }
     typename Mat<T>::Frag f;
 #pragma unroll
     for (int j = 0; j < CH; ++j) f[j] = c + j < D ? row[c + j] : (T)0.0f;
@@ -336,29 +343,37 @@ struct Stage {
     static __device__ __forceinline__ bool has(int wave, int u) {
         return Tile::SEGS % kHalves == 0 || seg(wave, u) < Tile::SEGS;
     }
-    // W: 16-byte loads through a buffer over the tile's rows, to which the
-    // entries beyond D and the rows beyond the last are out of range and come
-    // as zeros.  Otherwise entry by entry, the rows beyond the last coming as
+    // W = 2, 1: 16- or 8-byte loads through a buffer over the tile's rows, to
+    // which the entries beyond D and the rows beyond the last are out of range
+    // and come as zeros.  0: entry by entry, the rows beyond the last coming as
     // the last.
-    template <bool W>
+    template <int W>
     __device__ __forceinline__ void load(const Cursor<T>& m, int wave, int lane) {
         const int c = (seg(wave, 0) * 4 + lane % 4) * Mat<T>::CH;
         constexpr int step = kHalves * 4 * Mat<T>::CH;
-        if constexpr (W) {
+        if constexpr (W > 0) {
             const int bytes = ((min(m.left, ROWS) - 1) * (int)m.stride + m.D) * (int)sizeof(T);
             const __amdgpu_buffer_rsrc_t r = __builtin_amdgcn_make_buffer_rsrc(const_cast<T*>(m.p), (short)0, bytes, 0x00020000);
             const int off = (row_of(wave, lane) * (int)m.stride + c) * (int)sizeof(T);
 #pragma unroll
             for (int u = 0; u < N; ++u) {
+                constexpr int half = Mat<T>::CH / 2, beyond = (int)0x80000000;
+                const int at = off + u * step * (int)sizeof(T);
                 const bool in = has(wave, u) && c + u * step < m.D;
-                v[u] = __builtin_bit_cast(u4, __builtin_amdgcn_raw_buffer_load_b128(
-                                                  r, in ? off + u * step * (int)sizeof(T) : (int)0x80000000, 0, 0));
+                if constexpr (W == 2) {
+                    v[u] = __builtin_bit_cast(u4, __builtin_amdgcn_raw_buffer_load_b128(r, in ? at : beyond, 0, 0));
+                } else {
+                    const bool in1 = has(wave, u) && c + u * step + half < m.D;
+                    const auto lo = __builtin_amdgcn_raw_buffer_load_b64(r, in ? at : beyond, 0, 0);
+                    const auto hi = __builtin_amdgcn_raw_buffer_load_b64(r, in1 ? at + 8 : beyond, 0, 0);
+                    v[u] = u4{lo[0], lo[1], hi[0], hi[1]};
+                }
             }
         } else {
             const int r = min(row_of(wave, lane), m.left - 1);
 #pragma unroll
             for (int u = 0; u < N; ++u)
-                if (has(wave, u)) v[u] = load_chunk<T, false>(m.p + r * m.stride, c + u * step, m.D);
+                if (has(wave, u)) v[u] = load_chunk<T, 0>(m.p + r * m.stride, c + u * step, m.D);
         }
     }
     // keep: whether this thread's row counts; zeros otherwise, so that whatever
@@ -378,7 +393,7 @@ struct Stage {
 };
 
 // A lane's column vector as fragments: entries 2 CH s + CH h + j.
-template <typename T, int DP, bool W>
+template <typename T, int DP, int W>
 __device__ __forceinline__ void load_frags(const T* row, int D, bool live, int lane,
                                            typename Mat<T>::Frag (&f)[TileOf<T, DP>::NS]) {
     constexpr int CH = Mat<T>::CH;
@@ -398,14 +413,14 @@ __device__ __forceinline__ void swap_halves(uint32_t& a, uint32_t& b) {
 }
 
 // A lane's column of accumulators o (entry 32 d + 8 (i / 4) + 4 h + i % 4 in
-// register i), times f, to the row's D entries.  W: in 16-byte stores.  bf16
-// lanes first trade groups of four with the lane that holds the other half of
+// register i), times f, to the row's D entries.  W = 2, 1: in 16- or 8-byte stores.
+// For the former, bf16 lanes first trade groups of four with the lane that holds the other half of
 // their row, so that each has eight in a row (stores of 8 bytes: 66 us for the
 // forward pass of 2 x 32768 queries, 8 heads of 64, to 77 keys; so 53 us).  All
 // lanes call it; `live`: whether this one's row exists.
-template <typename T, int DP, bool W>
+template <typename T, int DP, int W>
 __device__ __forceinline__ void store_column(T* row, const f16 (&o)[DP / 32], float f, int D, int lane, bool live) {
-    if constexpr (W && std::is_same<T, __bf16>::value) {
+    if constexpr (W == 2 && std::is_same<T, __bf16>::value) {
 #pragma unroll
         for (int d = 0; d < DP / 32; ++d)
 #pragma unroll
@@ -433,8 +448,13 @@ __device__ __forceinline__ void store_column(T* row, const f16 (&o)[DP / 32], fl
         for (int q = 0; q < 4; ++q) {
             const int c = 32 * d + 8 * q + 4 * (lane / 32);
             const f4 v = {o[d][4 * q] * f, o[d][4 * q + 1] * f, o[d][4 * q + 2] * f, o[d][4 * q + 3] * f};
-            if constexpr (W) {
+            if constexpr (W == 1 && std::is_same<T, __bf16>::value) {
+                if (c < D) *(bf4*)(row + c) = __builtin_convertvector(v, bf4);
+            } else if constexpr (W == 2) {
                 if (c < D) *(f4*)(row + c) = v;
+            } else if constexpr (W == 1) {
+                if (c < D) *(f2*)(row + c) = f2{v[0], v[1]};
+                if (c + 2 < D) *(f2*)(row + c + 2) = f2{v[2], v[3]};
             } else {
 #pragma unroll
                 for (int j = 0; j < 4; ++j)
@@ -450,5 +470,19 @@ inline bool wide_rows(const Heads& t, int dim, int entries, size_t elem) {
     return dim % entries == 0 && (uintptr_t)t.p % (entries * elem) == 0 && t.sb % entries == 0 && t.st % entries == 0 &&
            t.sh % entries == 0 && t.st >= dim && t.st * (int64_t)elem < (int64_t)1 << 24;
 }
+
+// How a call's rows go: 2 in 16-byte pieces, 1 in 8-byte pieces, 0 entry by
+// entry.  The step of 2 x 8192 queries to 2048 keys, 8 heads, bf16: heads of 40
+// (2) 390 us, of 36 (1) 440 us and entry by entry 1017 us, of 37 (0) 709 us.
+inline int row_width(const AttendArgs& a) {
+    const int ch = a.bf16 ? 8 : 4;
+    int w = 2;
+    for (const Heads* t : {&a.q, &a.k, &a.v, &a.out, &a.low, &a.dout, &a.dq, &a.dk, &a.dv})
+        while (w > 0 && !wide_rows(*t, a.dim, w == 2 ? ch : ch / 2, a.bf16 ? 2 : 4)) --w;
+    return w;
+}
+// The width of rows of D partial sums in fp32 for a call of width W.
+template <typename T>
+constexpr int part_width(int w) { return std::is_same<T, __bf16>::value && w > 0 ? 2 : w; }
 
 }  // namespace disco

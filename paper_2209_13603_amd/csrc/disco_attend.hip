@@ -37,7 +37,7 @@ struct Cut {
     int32_t splits;
     float* part;   // [splits][all rows][dim]
     float* stat;   // [splits][all rows][2]
-    bool wide;     // rows of all tensors go by 16 bytes
+    int width;     // see row_width
 };
 
 // Workgroups of a CU that the registers are sized for.
@@ -48,7 +48,7 @@ constexpr int kKeys = std::is_same<T, __bf16>::value ? 64 : 32;  // keys of a ti
 
 // Each wave holds 32 rows; the workgroup's waves share the tiles of keys and
 // values, double-buffered in LDS, the next tile's loads in flight in registers.
-template <typename T, int DP, bool W>
+template <typename T, int DP, int W>
 __global__ __launch_bounds__(kAttendThreads, (kWorkgroups<T, DP>)) void k_attend(AttendArgs a, Cut c) {
     typedef TileOf<T, DP> Tile;
     constexpr int KT = kKeys<T>, NK = KT / 32;
@@ -175,7 +175,7 @@ __global__ __launch_bounds__(kAttendThreads, (kWorkgroups<T, DP>)) void k_attend
     if (c.splits > 1) {
         const int64_t all = (int64_t)a.batch * a.kv_heads * c.rows;
         const int64_t at = split * all + (int64_t)bh * c.rows + row;
-        store_column<float, DP, W>(c.part + at * a.dim, o, 1.0f, a.dim, lane, live);
+        store_column<float, DP, part_width<T>(W)>(c.part + at * a.dim, o, 1.0f, a.dim, lane, live);
         if (live && lane < 32) {
             c.stat[2 * at] = m;
             c.stat[2 * at + 1] = l;
@@ -255,7 +255,7 @@ __global__ __launch_bounds__(kAttendThreads) void k_attend_join(AttendArgs a, Cu
     T* low = a.low.p ? (T*)a.low.p + b * a.low.sb + i * a.low.st + h * a.low.sh + d : nullptr;
     typedef T T4 __attribute__((ext_vector_type(4)));
     const T4 v = __builtin_convertvector(o, T4);
-    if (c.wide) *(T4*)out = v;
+    if (part_width<T>(c.width) == 2) *(T4*)out = v;
     else
         for (int j = 0; j < n; ++j) out[j] = v[j];
     if (low)
@@ -289,8 +289,10 @@ size_t part_bytes(const AttendArgs& a, const Cut& c) {
 
 template <typename T, int DP>
 void launch(const AttendArgs& a, const Cut& c) {
-    if (c.wide) hipLaunchKernelGGL((k_attend<T, DP, true>), dim3(xcd_grid(c.items, c.run)), dim3(kAttendThreads), 0, a.stream, a, c);
-    else hipLaunchKernelGGL((k_attend<T, DP, false>), dim3(xcd_grid(c.items, c.run)), dim3(kAttendThreads), 0, a.stream, a, c);
+    const dim3 grid(xcd_grid(c.items, c.run)), block(kAttendThreads);
+    if (c.width == 2) hipLaunchKernelGGL((k_attend<T, DP, 2>), grid, block, 0, a.stream, a, c);
+    else if (c.width == 1) hipLaunchKernelGGL((k_attend<T, DP, 1>), grid, block, 0, a.stream, a, c);
+    else hipLaunchKernelGGL((k_attend<T, DP, 0>), grid, block, 0, a.stream, a, c);
 }
 
 template <typename T>
@@ -311,10 +313,7 @@ size_t attend_ws_bytes(const AttendArgs& a) {
 
 hipError_t launch_attend(const AttendArgs& a, void* ws) {
     Cut c = cut_of(a);
-    const size_t e = a.bf16 ? 2 : 4;
-    const int ch = a.bf16 ? 8 : 4;
-    c.wide = wide_rows(a.q, a.dim, ch, e) && wide_rows(a.k, a.dim, ch, e) && wide_rows(a.v, a.dim, ch, e) &&
-             wide_rows(a.out, a.dim, ch, e) && wide_rows(a.low, a.dim, ch, e);
+    c.width = row_width(a);
     if (c.splits > 1) {
         c.part = (float*)ws;
         c.stat = (float*)((char*)ws + part_bytes(a, c));

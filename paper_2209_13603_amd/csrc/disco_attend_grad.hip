@@ -39,7 +39,7 @@ struct GradCut {
     int32_t splits_q, splits_k;
     f4* row_c;    // [batch][heads][queries]: -reference, 1 / sum, delta, written with dq for dk and dv
     float* part;  // [splits][...][dim]
-    bool wide;    // rows of all tensors go by 16 bytes
+    int width;    // see row_width
 };
 
 // Workgroups of a CU that the registers are sized for.
@@ -51,7 +51,7 @@ template <typename T, int DP>
 constexpr bool kKeysInLds = DP > (std::is_same<T, float>::value ? 32 : 96);
 
 // dq: each wave holds 32 rows; keys and values come in tiles as in the forward pass.
-template <typename T, int DP, bool W>
+template <typename T, int DP, int W>
 __global__ __launch_bounds__(kAttendThreads, (kWorkgroups<T, DP>)) void k_attend_dq(AttendArgs a, GradCut c) {
     typedef TileOf<T, DP> Tile;
     constexpr int KT = kKeys;
@@ -164,7 +164,7 @@ __global__ __launch_bounds__(kAttendThreads, (kWorkgroups<T, DP>)) void k_attend
     const float f = inv * a.scale;
     if (c.splits_q > 1) {
         const int64_t all = (int64_t)a.batch * a.kv_heads * c.rows;
-        store_column<float, DP, W>(c.part + (split * all + (int64_t)bh * c.rows + row) * a.dim, dq, f, a.dim, lane, live);
+        store_column<float, DP, part_width<T>(W)>(c.part + (split * all + (int64_t)bh * c.rows + row) * a.dim, dq, f, a.dim, lane, live);
     } else {
         store_column<T, DP, W>((T*)a.dq.p + b * a.dq.sb + i * a.dq.st + h * a.dq.sh, dq, f, a.dim, lane, live);
     }
@@ -172,7 +172,7 @@ __global__ __launch_bounds__(kAttendThreads, (kWorkgroups<T, DP>)) void k_attend
 
 // dk, dv: each wave holds 32 keys; queries and output gradients of every head
 // of the group come in tiles.
-template <typename T, int DP, bool W>
+template <typename T, int DP, int W>
 __global__ __launch_bounds__(kAttendThreads, (kWorkgroups<T, DP>)) void k_attend_dkv(AttendArgs a, GradCut c) {
     typedef TileOf<T, DP> Tile;
     constexpr int QT = kQueries;
@@ -299,8 +299,8 @@ __global__ __launch_bounds__(kAttendThreads, (kWorkgroups<T, DP>)) void k_attend
     const bool there = j < a.keys;
     if (c.splits_k > 1) {
         const int64_t all = (int64_t)a.batch * a.kv_heads * a.keys, at = split * 2 * all + (int64_t)bh * a.keys + j;
-        store_column<float, DP, W>(c.part + at * a.dim, dk, a.scale, a.dim, lane, there);
-        store_column<float, DP, W>(c.part + (at + all) * a.dim, dv, 1.0f, a.dim, lane, there);
+        store_column<float, DP, part_width<T>(W)>(c.part + at * a.dim, dk, a.scale, a.dim, lane, there);
+        store_column<float, DP, part_width<T>(W)>(c.part + (at + all) * a.dim, dv, 1.0f, a.dim, lane, there);
     } else {
         store_column<T, DP, W>((T*)a.dk.p + b * a.dk.sb + j * a.dk.st + hk * a.dk.sh, dk, a.scale, a.dim, lane, there);
         store_column<T, DP, W>((T*)a.dv.p + b * a.dv.sb + j * a.dv.st + hk * a.dv.sh, dv, 1.0f, a.dim, lane, there);
@@ -353,13 +353,17 @@ size_t row_bytes(const AttendArgs& a) { return round256((size_t)a.batch * a.head
 
 template <typename T, int DP>
 void launch_dq(const AttendArgs& a, const GradCut& c) {
-    if (c.wide) hipLaunchKernelGGL((k_attend_dq<T, DP, true>), dim3(xcd_grid(c.items_q, c.run_q)), dim3(kAttendThreads), 0, a.stream, a, c);
-    else hipLaunchKernelGGL((k_attend_dq<T, DP, false>), dim3(xcd_grid(c.items_q, c.run_q)), dim3(kAttendThreads), 0, a.stream, a, c);
+    const dim3 grid(xcd_grid(c.items_q, c.run_q)), block(kAttendThreads);
+    if (c.width == 2) hipLaunchKernelGGL((k_attend_dq<T, DP, 2>), grid, block, 0, a.stream, a, c);
+    else if (c.width == 1) hipLaunchKernelGGL((k_attend_dq<T, DP, 1>), grid, block, 0, a.stream, a, c);
+    else hipLaunchKernelGGL((k_attend_dq<T, DP, 0>), grid, block, 0, a.stream, a, c);
 }
 template <typename T, int DP>
 void launch_dkv(const AttendArgs& a, const GradCut& c) {
-    if (c.wide) hipLaunchKernelGGL((k_attend_dkv<T, DP, true>), dim3(xcd_grid(c.items_k, c.run_k)), dim3(kAttendThreads), 0, a.stream, a, c);
-    else hipLaunchKernelGGL((k_attend_dkv<T, DP, false>), dim3(xcd_grid(c.items_k, c.run_k)), dim3(kAttendThreads), 0, a.stream, a, c);
+    const dim3 grid(xcd_grid(c.items_k, c.run_k)), block(kAttendThreads);
+    if (c.width == 2) hipLaunchKernelGGL((k_attend_dkv<T, DP, 2>), grid, block, 0, a.stream, a, c);
+    else if (c.width == 1) hipLaunchKernelGGL((k_attend_dkv<T, DP, 1>), grid, block, 0, a.stream, a, c);
+    else hipLaunchKernelGGL((k_attend_dkv<T, DP, 0>), grid, block, 0, a.stream, a, c);
 }
 
 template <typename T>
@@ -408,11 +412,7 @@ size_t attend_grad_ws_bytes(const AttendArgs& a) {
 
 hipError_t launch_attend_grad(const AttendArgs& a, void* ws) {
     GradCut c = cut_of(a);
-    const size_t e = a.bf16 ? 2 : 4;
-    const int ch = a.bf16 ? 8 : 4;
-    c.wide = true;
-    for (const Heads* t : {&a.q, &a.k, &a.v, &a.out, &a.low, &a.dout, &a.dq, &a.dk, &a.dv})
-        c.wide = c.wide && wide_rows(*t, a.dim, ch, e);
+    c.width = row_width(a);
     c.row_c = (f4*)ws;
     c.part = (float*)((char*)ws + row_bytes(a));
     return a.bf16 ? run<__bf16>(a, c) : run<float>(a, c);
