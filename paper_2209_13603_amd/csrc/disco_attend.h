@@ -27,6 +27,7 @@
 #include <type_traits>
 
 #include "disco_heads.h"
+#include "disco_launch.h"
 
 namespace disco {
 
@@ -43,7 +44,6 @@ typedef float f2 __attribute__((ext_vector_type(2)));
 typedef __attribute__((address_space(3))) char lds_t;
 
 constexpr int kWave = 64;
-constexpr int kAttendThreads = 256;
 constexpr int kAttendWaves = kAttendThreads / kWave;
 // Finite biases stay above -2^100 in units of the scale: a mask of the type's
 // lowest value takes no key out, and must not become -inf on the way.

@@ -204,17 +204,15 @@ __global__ __launch_bounds__(kAttendThreads, (kWorkgroups<T, DP>)) void k_attend
 
 // Joins the parts of each row.  A thread holds four entries of a row; where the
 // rows are few, `slices` threads share its parts, and their sums are added in
-// slice order.
-struct Join {
-    int lanes, slices, rows;  // threads of four entries, slices, rows of a workgroup
-};
+// slice order (see Join).
 template <typename T>
 __global__ __launch_bounds__(kAttendThreads) void k_attend_join(AttendArgs a, Cut c, Join g) {
     __shared__ f4 part[kAttendThreads];
     __shared__ float sums[kAttendThreads];
-    const int lane = threadIdx.x % g.lanes, slice = threadIdx.x / g.lanes % g.slices, r = threadIdx.x / (g.lanes * g.slices);
-    const int64_t all = (int64_t)a.batch * a.kv_heads * c.rows, at = (int64_t)blockIdx.x * g.rows + r;
-    const bool live = r < g.rows && at < all;
+    const int lane = g.lane(threadIdx.x), slice = g.slice(threadIdx.x);
+    const int64_t all = (int64_t)a.batch * a.kv_heads * c.rows, first = (int64_t)blockIdx.x * g.rows, left = all - first;
+    const int64_t at = first + g.row(threadIdx.x);
+    const bool live = g.live(threadIdx.x, left), adds = g.adds(threadIdx.x, left);
     const int d = 4 * lane, n = min(4, a.dim - d);
     float m = -INFINITY, l = 0.0f;
     f4 o = {0.0f};
@@ -239,13 +237,13 @@ __global__ __launch_bounds__(kAttendThreads) void k_attend_join(AttendArgs a, Cu
         part[threadIdx.x] = o;
         sums[threadIdx.x] = l;
         __syncthreads();
-        if (slice == 0)
+        if (adds)
             for (int s = 1; s < g.slices; ++s) {
                 o += part[threadIdx.x + s * g.lanes];
                 l += sums[threadIdx.x + s * g.lanes];
             }
     }
-    if (!live || slice != 0) return;
+    if (!adds) return;
     o *= l == 0.0f ? 0.0f : 1.0f / l;
     const int G = a.heads / a.kv_heads;
     const uint32_t bh = (uint32_t)(at / c.rows), row = (uint32_t)(at - (int64_t)bh * c.rows);
@@ -326,11 +324,7 @@ hipError_t launch_attend(const AttendArgs& a, void* ws) {
     if (err != hipSuccess || c.splits == 1) return err;
     const int64_t all = (int64_t)a.batch * a.kv_heads * c.rows;
     tk = timing_begin("attend_join", a.stream);
-    Join g;
-    g.lanes = (a.dim + 3) / 4;
-    g.slices = 1;
-    while (2 * g.slices <= c.splits && 2 * g.slices * g.lanes <= kAttendThreads && all * g.lanes * g.slices < 65536) g.slices *= 2;
-    g.rows = kAttendThreads / (g.lanes * g.slices);
+    const Join g = join_of(a.dim, c.splits, all);
     const dim3 grid((unsigned)((all + g.rows - 1) / g.rows));
     if (a.bf16) hipLaunchKernelGGL(k_attend_join<__bf16>, grid, dim3(kAttendThreads), 0, a.stream, a, c, g);
     else hipLaunchKernelGGL(k_attend_join<float>, grid, dim3(kAttendThreads), 0, a.stream, a, c, g);
