@@ -45,9 +45,9 @@ typedef __attribute__((address_space(3))) char lds_t;
 
 constexpr int kWave = 64;
 constexpr int kAttendWaves = kAttendThreads / kWave;
-// Finite biases stay above -2^100 in units of the scale: a mask of the type's
-// lowest value takes no key out, and must not become -inf on the way.
-constexpr float kLowestBias = -0x1p+100f;
+// References m of a softmax row beyond this, in units of log 2, are far: see
+// near_reference.
+constexpr float kFarReference = 0x1p+12f;
 
 // Keys of batch item b that its length leaves.
 __device__ __forceinline__ int64_t key_count(const AttendArgs& a, int b) {
@@ -57,10 +57,40 @@ __device__ __forceinline__ int64_t key_count(const AttendArgs& a, int b) {
 }
 
 // What a key's score starts from, in units of the scale (positive here): the
-// product is added onto it in the matrix cores.
-__device__ __forceinline__ float start_of(float bias, float inv_scale) {
+// product is added onto it in the matrix cores.  Finite biases stay within
+// `limit`: a mask of the type's lowest value takes no key out, and must not
+// become -inf on the way.
+__device__ __forceinline__ float start_of(float bias, float inv_scale, float limit) {
     const float t = bias * inv_scale;
-    return t < kLowestBias && bias != -INFINITY ? kLowestBias : t;
+    return fabsf(bias) < INFINITY ? fminf(fmaxf(t, -limit), limit) : t;
+}
+
+// A score's exponent against its row's reference -neg: the product rounded to
+// fp32, as the reference was, so that the largest score's exponent is 0
+// whatever its size, and then the difference, which is exact where it matters.
+__device__ __forceinline__ float exponent(float s, float scale2, float neg) {
+#pragma clang fp contract(off)
+    const float t = s * scale2;
+    return t + neg;
+}
+// The forward pass, which has no instruction to spare, takes one multiply-add
+// s scale2 - m instead where m is near: the product is then exact, and what
+// rounding took from m (half a spacing, 2^-13 below the line) is in every
+// weight of the row and leaves their quotients.  Of a far m, the -1e10 of a mask, it
+// would be an exponent of hundreds: infinite weights or none.  Returns what to
+// add to the products of a lane's column s; a far row's scores become their
+// differences from the reference first.  (32768 queries of 8 heads to
+// 8192 keys: rounded products for every row 690 us, so 671.)
+template <int N>
+__device__ __forceinline__ float near_reference(f16 (&s)[N], float scale2, float neg) {
+    const bool far = fabsf(neg) > kFarReference && fabsf(neg) < INFINITY;
+    if (__any(far)) {
+#pragma unroll
+        for (int k = 0; k < N; ++k)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) s[k][r] = far ? exponent(s[k][r], scale2, neg) / scale2 : s[k][r];
+    }
+    return far ? 0.0f : neg;
 }
 
 // Workgroups go round the XCDs one by one: gives each XCD runs of `run`

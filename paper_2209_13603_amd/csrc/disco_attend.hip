@@ -2,7 +2,8 @@
 //
 // One pass over the keys with the running maximum m and sum l of each row's
 // softmax, in units of log 2: t_ij = scale2 (q_i . k_j + bias_j / scale),
-// p_ij = 2^(t_ij - m_i), o_i = sum_j p_ij v_j / l_i.  The heads that share keys
+// p_ij = 2^(t_ij - m_i), o_i = sum_j p_ij v_j / l_i (m and t rounded alike where they
+// are large: near_reference).  The heads that share keys
 // and values are rows of one tile (row = query * group + head of the group), so
 // that a single query of grouped heads reads them once.
 //
@@ -104,7 +105,7 @@ __global__ __launch_bounds__(kAttendThreads, (kWorkgroups<T, DP>)) void k_attend
         vals.advance(KT);
     };
     auto store = [&](int buf) {
-        const float start = srow < left ? start_of(bias, inv_scale) : -INFINITY;
+        const float start = srow < left ? start_of(bias, inv_scale, a.bias_limit) : -INFINITY;
         const bool keep = start != -INFINITY;
         sk.store(lds + buf * 2 * St::kBytes, wave, lane, keep);
         sv.store(lds + (buf * 2 + 1) * St::kBytes, wave, lane, keep);
@@ -154,7 +155,7 @@ __global__ __launch_bounds__(kAttendThreads, (kWorkgroups<T, DP>)) void k_attend
 #pragma unroll
                 for (int r = 0; r < 16; ++r) o[d][r] *= f;
         }
-        const float neg = m == -INFINITY ? 0.0f : -m;
+        const float neg = near_reference(s, scale2, m == -INFINITY ? 0.0f : -m);
         float sum = 0.0f;  // of the tile, then onto l: a shorter chain of roundings
 #pragma unroll
         for (int k = 0; k < NK; ++k) {

@@ -124,7 +124,7 @@ __global__ __launch_bounds__(kAttendThreads, (kWorkgroups<T, DP>)) void k_attend
         vals.advance(KT);
     };
     auto store = [&](int buf) {
-        const float start = srow < left ? start_of(bias, inv_scale) : -INFINITY;
+        const float start = srow < left ? start_of(bias, inv_scale, a.bias_limit) : -INFINITY;
         const bool keep = start != -INFINITY;
         sk.store(lds + buf * 2 * St::kBytes, wave, lane, keep);
         sv.store(lds + (buf * 2 + 1) * St::kBytes, wave, lane, keep);
@@ -155,7 +155,7 @@ __global__ __launch_bounds__(kAttendThreads, (kWorkgroups<T, DP>)) void k_attend
         }
         const f16 dp = Tile::scores(vt, ln, 0, gf, a.dim);
 #pragma unroll
-        for (int r = 0; r < 16; ++r) s[r] = __builtin_amdgcn_exp2f(fmaf(s[r], scale2, neg)) * (dp[r] - delta);
+        for (int r = 0; r < 16; ++r) s[r] = __builtin_amdgcn_exp2f(exponent(s[r], scale2, neg)) * (dp[r] - delta);
         Tile::values(kt, ln, 0, s, a.dim, lane, dq);
         if (more) store(buf ^ 1);
         __syncthreads();
@@ -191,7 +191,7 @@ __global__ __launch_bounds__(kAttendThreads, (kWorkgroups<T, DP>)) void k_attend
     const int wave = threadIdx.x / kWave, lane = threadIdx.x % kWave, G = a.heads / a.kv_heads;
     const int64_t j = (int64_t)kb * kCols + wave * 32 + lane % 32, n = key_count(a, b);
     const float scale2 = fabsf(a.scale2);
-    const float start = j >= n ? -INFINITY : a.bias ? start_of(a.bias[b * a.bias_sb + j], 1.0f / fabsf(a.scale)) : 0.0f;
+    const float start = j >= n ? -INFINITY : a.bias ? start_of(a.bias[b * a.bias_sb + j], 1.0f / fabsf(a.scale), a.bias_limit) : 0.0f;
     const bool live = start != -INFINITY;
     const int64_t jr = live ? j : 0;
 
@@ -276,7 +276,7 @@ __global__ __launch_bounds__(kAttendThreads, (kWorkgroups<T, DP>)) void k_attend
             f4 e, f;
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
-                e[r] = __builtin_amdgcn_exp2f(fmaf(s[4 * q + r], scale2, neg[r])) * inv[r];
+                e[r] = __builtin_amdgcn_exp2f(exponent(s[4 * q + r], scale2, neg[r])) * inv[r];
                 f[r] = e[r] * (dp[4 * q + r] - delta[r]);
             }
             p.set(q, e);

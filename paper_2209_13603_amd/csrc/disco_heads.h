@@ -50,6 +50,7 @@ struct AttendArgs {
     int64_t queries = 0, keys = 0;
     float scale2 = 0.0f;  // scale / log 2: the scores in units of log 2
     float scale = 0.0f;
+    float bias_limit = 0.0f;  // finite biases stay within it, in units of the scale
     bool bf16 = false;
     hipStream_t stream = nullptr;
 };
