@@ -214,7 +214,7 @@ __global__ __launch_bounds__(kAttendThreads, (kWorkgroups<T, DP>)) void k_attend
     const int t0 = first_tile(steps, split, c.splits_k), t1 = first_tile(steps, split + 1, c.splits_k);
     St sq, sg;
     float rc = 0.0f;  // entry threadIdx.x of the staged tile's row constants
-    int left = 0;  // rows of the staged tile that exist
+    int left = 0;  // rows of the staged tile that exist, QT at most (four entries each are counted in 32 bits)
     const int g0 = tiles > 0 ? t0 / tiles : 0;
     int at = tiles > 0 ? t0 % tiles : 0;  // tile of the next load among its head's
     int64_t head = hk * G + g0;
@@ -224,7 +224,7 @@ __global__ __launch_bounds__(kAttendThreads, (kWorkgroups<T, DP>)) void k_attend
     auto load = [&] {
         sq.template load<W>(qs, wave, lane);
         sg.template load<W>(gs, wave, lane);
-        left = qs.left;
+        left = min(qs.left, QT);
         rc = ((const float*)consts)[min((int)threadIdx.x, 4 * left - 1)];
         if (++at < tiles) {
             qs.advance(QT);
