@@ -381,9 +381,9 @@ typedef struct {
     void* data;           /* device pointer (may be NULL only when the tensor is empty) */
     int32_t dtype;        /* disco_dtype_t */
     int32_t dim;          /* entries of a head, 1..128, contiguous */
-    int32_t heads;
+    int32_t heads;        /* 0..4096 */
     int32_t reserved;     /* 0 */
-    int64_t batch, tokens;
+    int64_t batch, tokens; /* batch 0..65535, batch * tokens < 2^31 */
     int64_t stride_batch, stride_token, stride_head; /* in elements, >= 0; of an output no two rows overlap */
 } disco_heads_t;
 

@@ -27,7 +27,6 @@
 #include <type_traits>
 
 #include "disco_heads.h"
-#include "disco_launch.h"
 
 namespace disco {
 
@@ -96,10 +95,10 @@ __device__ __forceinline__ float near_reference(f16 (&s)[N], float scale2, float
 // Workgroups go round the XCDs one by one: gives each XCD runs of `run`
 // consecutive work items, which share keys, values or queries in its L2.
 __device__ __forceinline__ uint32_t xcd_item(uint32_t run) {
-    const uint32_t k = blockIdx.x / 8;
-    return (k / run * 8 + blockIdx.x % 8) * run + k % run;
+    const uint32_t at = group_index(), k = at / 8;
+    return (k / run * 8 + at % 8) * run + k % run;
 }
-inline unsigned xcd_grid(uint32_t n, uint32_t run) { return ((n + run - 1) / run + 7) / 8 * 8 * run; }
+inline dim3 xcd_grid(uint32_t n, uint32_t run) { return grid_dim(((n + run - 1) / run + 7) / 8 * 8 * run); }
 // One run an XCD where all items cost the same.  With lengths, which the host
 // does not see, whole runs may have nothing to do: eight and more an XCD (3 x
 // 4050 queries of 5 heads, fp32, 1013, 845 and no keys: the step 615 us with one run, 458 us so).

@@ -288,7 +288,7 @@ size_t part_bytes(const AttendArgs& a, const Cut& c) {
 
 template <typename T, int DP>
 void launch(const AttendArgs& a, const Cut& c) {
-    const dim3 grid(xcd_grid(c.items, c.run)), block(kAttendThreads);
+    const dim3 grid = xcd_grid(c.items, c.run), block(kAttendThreads);
     if (c.width == 2) hipLaunchKernelGGL((k_attend<T, DP, 2>), grid, block, 0, a.stream, a, c);
     else if (c.width == 1) hipLaunchKernelGGL((k_attend<T, DP, 1>), grid, block, 0, a.stream, a, c);
     else hipLaunchKernelGGL((k_attend<T, DP, 0>), grid, block, 0, a.stream, a, c);

@@ -353,14 +353,14 @@ size_t row_bytes(const AttendArgs& a) { return round256((size_t)a.batch * a.head
 
 template <typename T, int DP>
 void launch_dq(const AttendArgs& a, const GradCut& c) {
-    const dim3 grid(xcd_grid(c.items_q, c.run_q)), block(kAttendThreads);
+    const dim3 grid = xcd_grid(c.items_q, c.run_q), block(kAttendThreads);
     if (c.width == 2) hipLaunchKernelGGL((k_attend_dq<T, DP, 2>), grid, block, 0, a.stream, a, c);
     else if (c.width == 1) hipLaunchKernelGGL((k_attend_dq<T, DP, 1>), grid, block, 0, a.stream, a, c);
     else hipLaunchKernelGGL((k_attend_dq<T, DP, 0>), grid, block, 0, a.stream, a, c);
 }
 template <typename T, int DP>
 void launch_dkv(const AttendArgs& a, const GradCut& c) {
-    const dim3 grid(xcd_grid(c.items_k, c.run_k)), block(kAttendThreads);
+    const dim3 grid = xcd_grid(c.items_k, c.run_k), block(kAttendThreads);
     if (c.width == 2) hipLaunchKernelGGL((k_attend_dkv<T, DP, 2>), grid, block, 0, a.stream, a, c);
     else if (c.width == 1) hipLaunchKernelGGL((k_attend_dkv<T, DP, 1>), grid, block, 0, a.stream, a, c);
     else hipLaunchKernelGGL((k_attend_dkv<T, DP, 0>), grid, block, 0, a.stream, a, c);

@@ -6,6 +6,7 @@
 #include <cstdint>
 
 #include "disco.h"
+#include "disco_launch.h"
 
 namespace disco {
 
@@ -16,6 +17,13 @@ struct Heads {
 };
 
 constexpr int kMaxHeadDim = 128;
+
+inline dim3 grid_dim(uint32_t groups) {
+    const Grid g = grid_of(groups);
+    return dim3(g.x, g.y);
+}
+// The workgroup's place in a grid of grid_dim.
+__device__ __forceinline__ uint32_t group_index() { return blockIdx.y * gridDim.x + blockIdx.x; }
 
 // ---- head norm and rotation (disco_rotate.hip) ------------------------------
 struct RotateArgs {

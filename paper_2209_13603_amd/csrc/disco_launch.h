@@ -7,6 +7,17 @@ namespace disco {
 
 constexpr int kAttendThreads = 256;
 
+// The workgroups of a launch as rows of a grid: HIP takes fewer than 2^32
+// threads along an axis.  Whole rows of a multiple of eight keep the workgroups'
+// turn over the XCDs; the last row's surplus has no work.
+struct Grid {
+    uint32_t x, y;
+};
+constexpr uint32_t kGridRow = 1u << 21;  // times 1024 threads at most
+constexpr Grid grid_of(uint32_t groups) {
+    return groups <= kGridRow ? Grid{groups, 1} : Grid{kGridRow, (groups - 1) / kGridRow + 1};
+}
+
 // Joining the parts of attention rows: `lanes` threads hold four entries each
 // of a row, `slices` such groups share its parts, `rows` rows go to a workgroup.
 struct Join {

@@ -157,7 +157,7 @@ __device__ __forceinline__ T* row_at(const Heads& t, const Place& p) {
 template <typename T, int V, bool INTER>
 __global__ __launch_bounds__(kThreads) void k_rotate(RotateArgs a, Shape sh) {
     const int item = threadIdx.x % sh.lanes, slot = threadIdx.x / sh.lanes;
-    const uint32_t row = blockIdx.x * (uint32_t)sh.slots + slot;
+    const uint32_t row = group_index() * (uint32_t)sh.slots + slot;
     if (row >= sh.rows) return;  // whole rows: the sums below stay within one
     const Item it = item_of<V, INTER>(item, sh, a.rotary, a.dim);
     const Place p = place_of(a, sh, row);
@@ -318,8 +318,9 @@ Shape shape_of(const RotateArgs& a, int v, bool per_head, int blocks) {
     return s;
 }
 
-// Workgroups of the gradient when it sums dw: each leaves one partial row.
-constexpr int kGradBlocks = 1024;
+// Workgroups of the gradient when it sums dw, each of which leaves one partial
+// row, and otherwise (as many as one axis of a grid takes).
+constexpr int kGradBlocks = 1024, kGradRowBlocks = kGridRow;
 
 // Calls f with the kernels' types for the storage type, width and layout.
 template <typename F>
@@ -346,7 +347,7 @@ hipError_t launch_rotate(const RotateArgs& a) {
     const Shape s = shape_of(a, v, false, 0);
     const int tk = timing_begin("norm_rotate", a.stream);
     const hipError_t e = dispatch(a, v, [&](auto t, auto vv, auto inter) {
-        hipLaunchKernelGGL((k_rotate<decltype(t), decltype(vv)::value, decltype(inter)::value>), dim3((unsigned)s.gx),
+        hipLaunchKernelGGL((k_rotate<decltype(t), decltype(vv)::value, decltype(inter)::value>), grid_dim(s.gx),
                            dim3(kThreads), 0, a.stream, a, s);
         return hipGetLastError();
     });
@@ -358,7 +359,7 @@ size_t rotate_grad_ws_bytes(const RotateArgs& a) { return (size_t)(kGradBlocks +
 
 hipError_t launch_rotate_grad(const RotateArgs& a, float* ws) {
     const int v = width(a);
-    const Shape s = shape_of(a, v, a.weight && a.weight_sh != 0 && a.dweight, a.dweight ? kGradBlocks : 0);
+    const Shape s = shape_of(a, v, a.weight && a.weight_sh != 0 && a.dweight, a.dweight ? kGradBlocks : kGradRowBlocks);
     int tk = timing_begin("norm_rotate_grad", a.stream);
     hipError_t e = dispatch(a, v, [&](auto t, auto vv, auto inter) {
         hipLaunchKernelGGL((k_rotate_grad<decltype(t), decltype(vv)::value, decltype(inter)::value>),

@@ -21,7 +21,7 @@ def walker(tmp_path_factory):
     return exe
 
 
-@pytest.mark.parametrize("what", ["join"])
+@pytest.mark.parametrize("what", ["join", "grid"])
 def test_maps(walker, what):
     r = subprocess.run([walker, what], capture_output=True, text=True, timeout=300)
     assert r.returncode == 0, r.stdout

@@ -36,9 +36,24 @@ static void join() {
             }
 }
 
+// Every workgroup of a launch has a place, no axis has 2^32 threads or 2^16 rows.
+static void grid() {
+    for (uint64_t groups : {uint64_t(1), uint64_t(7), uint64_t(2048), uint64_t(1) << 21, (uint64_t(1) << 21) + 1, uint64_t(1) << 24,
+                            // rows of 2^31 / 4 (norm and rotation, 64 lanes a row), of 2^35 / 128 and 2^19 pairs of item and head
+                            // (attention), rounded up to eight runs
+                            (uint64_t(1) << 29) + 1, (uint64_t(1) << 28) + (uint64_t(1) << 19) + 4096, uint64_t(0x7fffffff)}) {
+        const Grid g = grid_of((uint32_t)groups);
+        const uint64_t all = uint64_t(g.x) * g.y;
+        const bool good = uint64_t(g.x) * 1024 < (uint64_t(1) << 32) && g.y <= 65535 && all >= groups && all - groups < kGridRow &&
+                          all < (uint64_t(1) << 32) && (g.y == 1 || g.x % 8 == 0);
+        if (!good && failures++ < 10) std::printf("grid: %llu groups as %u x %u\n", (unsigned long long)groups, g.x, g.y);
+    }
+}
+
 int main(int argc, char** argv) {
     const char* what = argc > 1 ? argv[1] : "";
     if (!std::strcmp(what, "join")) join();
+    else if (!std::strcmp(what, "grid")) grid();
     else return 2;
     std::printf("%s: %d failures\n", what, failures);
     return failures != 0;
