@@ -171,14 +171,55 @@ void check_same(const disco_heads_t* a, const char* na, const disco_heads_t* b, 
         refuse(DISCO_ERR_SHAPE, std::string(na) + " and " + nb + " have different sizes");
 }
 
-// Whether two tensors may share memory.  Parts of one joint buffer, which
-// interleave token by token, are told apart by their place within a token.
+// An axis that two tensors step along alike.
+struct Axis {
+    int64_t stride, na, nb;
+};
+
+// Whether some a0 + sum ia stride + ea, ea < dim_a, is some b0 + sum ib stride +
+// eb, eb < dim_b, for d = b0 - a0: by falling stride each axis steps over all
+// that the ones after it span, so that only two of its differences ia - ib can
+// bring d within reach of those.
+bool meets(const Axis* ax, int n, int64_t d, int64_t dim_a, int64_t dim_b) {
+    if (n == 0) return d > -dim_b && d < dim_a;
+    const int64_t s = ax->stride, k = d >= 0 ? d / s : -((-d + s - 1) / s);
+    for (int64_t i : {k, k + 1})
+        if (i > -ax->nb && i < ax->na && meets(ax + 1, n - 1, d - i * s, dim_a, dim_b)) return true;
+    return false;
+}
+
+// Whether two tensors may share memory: exactly where they have the same
+// strides along nested axes, as the parts of one joint buffer do in any order of
+// its axes.  With other strides, tensors whose tokens lie equally far apart
+// are told apart by their place within a token, all others by the memory from
+// their first to their last entry.
 bool may_overlap(const disco_heads_t& a, const disco_heads_t& b) {
     if (empty(a) || empty(b)) return false;
     const int64_t ea = (int64_t)bytes_of(a.dtype), eb = (int64_t)bytes_of(b.dtype);
     const uintptr_t a0 = (uintptr_t)a.data, b0 = (uintptr_t)b.data;
     const uintptr_t a1 = a0 + (uintptr_t)(extent(a) * ea), b1 = b0 + (uintptr_t)(extent(b) * eb);
     if (a1 <= b0 || b1 <= a0) return false;
+
+    Axis ax[3];
+    int n = 0;
+    bool alike = ea == eb;
+    const int64_t at[3][4] = {{a.stride_batch, a.batch, b.stride_batch, b.batch},
+                              {a.stride_token, a.tokens, b.stride_token, b.tokens},
+                              {a.stride_head, a.heads, b.stride_head, b.heads}};
+    for (const auto& x : at) {
+        const int64_t na = x[0] == 0 ? 1 : x[1], nb = x[2] == 0 ? 1 : x[3];
+        if (na > 1 && nb > 1 && x[0] != x[2]) alike = false;
+        if (na > 1 || nb > 1) ax[n++] = Axis{na > 1 ? x[0] : x[2], na, nb};
+    }
+    std::sort(ax, ax + n, [](const Axis& p, const Axis& q) { return p.stride > q.stride; });
+    int64_t span_a = a.dim, span_b = b.dim;
+    for (int i = n - 1; i >= 0 && alike; --i) {
+        alike = ax[i].stride >= std::max(span_a, span_b);
+        span_a += ax[i].stride * (ax[i].na - 1);
+        span_b += ax[i].stride * (ax[i].nb - 1);
+    }
+    if (alike) return meets(ax, n, ((int64_t)b0 - (int64_t)a0) / ea, a.dim, b.dim);
+
     const int64_t step = a.stride_token * ea;
     if (step > 0 && step == b.stride_token * eb && (a.batch == 1 || a.stride_batch % a.stride_token == 0) &&
         (b.batch == 1 || b.stride_batch % b.stride_token == 0)) {
