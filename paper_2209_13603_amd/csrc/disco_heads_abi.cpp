@@ -230,9 +230,11 @@ bool may_overlap(const disco_heads_t& a, const disco_heads_t& b) {
     return true;
 }
 
+// Of tensors of one size: whether each entry of one lies where the other's does
+// (the stride of a single entry leads nowhere).
 bool same_place(const disco_heads_t& a, const disco_heads_t& b) {
-    return a.data == b.data && a.stride_batch == b.stride_batch && a.stride_token == b.stride_token &&
-           a.stride_head == b.stride_head;
+    return a.data == b.data && (a.batch <= 1 || a.stride_batch == b.stride_batch) &&
+           (a.tokens <= 1 || a.stride_token == b.stride_token) && (a.heads <= 1 || a.stride_head == b.stride_head);
 }
 
 void check_apart(const disco_heads_t* out, const char* no, const disco_heads_t* in, const char* ni) {

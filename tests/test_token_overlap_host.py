@@ -102,3 +102,15 @@ def test_parts_of_a_projection_with_fewer_key_heads():
     args = lambda dv: (t["q"], t["k"], t["v"], None, out, 0x90000000, None, dout, t["dq"], t["dk"], dv, None, 0, None)
     assert call(*args(t["dv"])) == disco.DISCO_ERR_DEVICE
     assert call(*args(heads((B, S, 2, D), (S * token, token, D), at["dv"] - 1))) == disco.DISCO_ERR_INVALID_ARGUMENT
+
+
+@pytest.mark.parametrize("shape", [(1, 5, 3, 8), (2, 1, 3, 8), (2, 5, 1, 8)])
+def test_in_place_whatever_the_stride_of_a_single_entry(shape):
+    strides = [shape[1] * shape[2] * shape[3], shape[2] * shape[3], shape[3]]
+    axis = shape.index(1)
+    other = list(strides)
+    other[axis] = 1000
+    x, y = heads(shape, strides, 0), heads(shape, other, 0)
+    assert not refused(x, y)
+    call = disco.library().disco_norm_rotate_backward
+    assert call(None, 0, None, 0.0, None, x, y, None, None, 0, None) == disco.DISCO_ERR_DEVICE
