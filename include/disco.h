@@ -376,7 +376,9 @@ disco_status_t disco_psi_entries(int nlat_in, int nlon_in, int nlat_out, int nlo
  * sums), one type for the tensors of a call; tables, biases and statistics
  * are fp32.  Scratch memory: `workspace` of at least the bytes that the
  * ..._workspace call names (256-byte aligned, on the same device, the caller's
- * until the work is complete), or NULL for the stream-ordered pool. */
+ * until the work is complete), or NULL for the stream-ordered pool.  What a call
+ * writes, the workspace with it, lies apart from all else that it is given, but
+ * where a call allows the same place: INVALID_ARGUMENT otherwise. */
 typedef struct {
     void* data;           /* device pointer (may be NULL only when the tensor is empty) */
     int32_t dtype;        /* disco_dtype_t */

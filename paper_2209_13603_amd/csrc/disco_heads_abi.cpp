@@ -8,6 +8,7 @@
 #include <cmath>
 #include <cstring>
 #include <exception>
+#include <initializer_list>
 #include <new>
 #include <string>
 #include <utility>
@@ -171,60 +172,78 @@ void check_same(const disco_heads_t* a, const char* na, const disco_heads_t* b, 
         refuse(DISCO_ERR_SHAPE, std::string(na) + " and " + nb + " have different sizes");
 }
 
-// An axis that two tensors step along alike.
+// The memory of an argument: rows of `width` bytes, n[i] of them `stride[i]` bytes
+// apart along batch, token and head; one row for a dense argument.
+struct Place {
+    const char* name;
+    uintptr_t p;
+    int64_t width, stride[3], n[3];
+    bool none() const { return p == 0 || width == 0 || n[0] == 0 || n[1] == 0 || n[2] == 0; }
+    uintptr_t end() const {
+        uintptr_t e = p + (uintptr_t)width;
+        for (int i = 0; i < 3; ++i) e += (uintptr_t)(stride[i] * (n[i] - 1));
+        return e;
+    }
+};
+Place place(const char* name, const disco_heads_t* t) {
+    if (!t) return Place{name, 0, 0, {0, 0, 0}, {1, 1, 1}};
+    const int64_t e = (int64_t)bytes_of(t->dtype);
+    return Place{name, (uintptr_t)t->data, t->dim * e, {t->stride_batch * e, t->stride_token * e, t->stride_head * e},
+                 {t->batch, t->tokens, t->heads}};
+}
+Place place(const char* name, const void* p, int64_t bytes) { return Place{name, (uintptr_t)p, p ? bytes : 0, {0, 0, 0}, {1, 1, 1}}; }
+
+// An axis that two places step along alike, with what the axes after it span.
 struct Axis {
-    int64_t stride, na, nb;
+    int64_t stride, na, nb, span_a, span_b;
 };
 
-// Whether some a0 + sum ia stride + ea, ea < dim_a, is some b0 + sum ib stride +
-// eb, eb < dim_b, for d = b0 - a0: by falling stride each axis steps over all
-// that the ones after it span, so that only two of its differences ia - ib can
-// bring d within reach of those.
-bool meets(const Axis* ax, int n, int64_t d, int64_t dim_a, int64_t dim_b) {
-    if (n == 0) return d > -dim_b && d < dim_a;
-    const int64_t s = ax->stride, k = d >= 0 ? d / s : -((-d + s - 1) / s);
-    for (int64_t i : {k, k + 1})
-        if (i > -ax->nb && i < ax->na && meets(ax + 1, n - 1, d - i * s, dim_a, dim_b)) return true;
+// Whether some ia stride + ea along the axes is some ib stride + eb + d, ea < wa and eb
+// < wb: along each axis few differences ia - ib bring d within reach of what the
+// axes after it span, and where more than a few do, b covers rows of a.
+bool meets(const Axis* ax, int n, int64_t d, int64_t wa, int64_t wb) {
+    if (n == 0) return d > -wb && d < wa;
+    auto below = [](int64_t x, int64_t s) { return x >= 0 ? x / s : -((-x + s - 1) / s); };
+    const int64_t s = ax->stride;
+    const int64_t lo = std::max(1 - ax->nb, below(d - ax->span_a, s)), hi = std::min(ax->na - 1, below(d + ax->span_b, s) + 1);
+    if (hi - lo > 4) return true;
+    for (int64_t i = lo; i <= hi; ++i)
+        if (meets(ax + 1, n - 1, d - i * s, wa, wb)) return true;
     return false;
 }
 
-// Whether two tensors may share memory: exactly where they have the same
+// Whether two places may share memory: exactly where they have the same
 // strides along nested axes, as the parts of one joint buffer do in any order of
-// its axes.  With other strides, tensors whose tokens lie equally far apart
-// are told apart by their place within a token, all others by the memory from
-// their first to their last entry.
-bool may_overlap(const disco_heads_t& a, const disco_heads_t& b) {
-    if (empty(a) || empty(b)) return false;
-    const int64_t ea = (int64_t)bytes_of(a.dtype), eb = (int64_t)bytes_of(b.dtype);
-    const uintptr_t a0 = (uintptr_t)a.data, b0 = (uintptr_t)b.data;
-    const uintptr_t a1 = a0 + (uintptr_t)(extent(a) * ea), b1 = b0 + (uintptr_t)(extent(b) * eb);
-    if (a1 <= b0 || b1 <= a0) return false;
-
+// its axes, or where one of them is a single row.  With other strides, tensors whose
+// tokens lie equally far apart are told apart by their place within a token,
+// all others by the memory from their first to their last byte.
+bool may_overlap(const Place& a, const Place& b) {
+    if (a.none() || b.none() || a.end() <= b.p || b.end() <= a.p) return false;
     Axis ax[3];
     int n = 0;
-    bool alike = ea == eb;
-    const int64_t at[3][4] = {{a.stride_batch, a.batch, b.stride_batch, b.batch},
-                              {a.stride_token, a.tokens, b.stride_token, b.tokens},
-                              {a.stride_head, a.heads, b.stride_head, b.heads}};
-    for (const auto& x : at) {
-        const int64_t na = x[0] == 0 ? 1 : x[1], nb = x[2] == 0 ? 1 : x[3];
-        if (na > 1 && nb > 1 && x[0] != x[2]) alike = false;
-        if (na > 1 || nb > 1) ax[n++] = Axis{na > 1 ? x[0] : x[2], na, nb};
+    bool alike = true, single_a = true, single_b = true;
+    for (int i = 0; i < 3; ++i) {
+        const int64_t na = a.stride[i] == 0 ? 1 : a.n[i], nb = b.stride[i] == 0 ? 1 : b.n[i];
+        if (na > 1 && nb > 1 && a.stride[i] != b.stride[i]) alike = false;
+        if (na > 1 || nb > 1) ax[n++] = Axis{na > 1 ? a.stride[i] : b.stride[i], na, nb, 0, 0};
+        single_a = single_a && na == 1;
+        single_b = single_b && nb == 1;
     }
     std::sort(ax, ax + n, [](const Axis& p, const Axis& q) { return p.stride > q.stride; });
-    int64_t span_a = a.dim, span_b = b.dim;
+    int64_t span_a = a.width, span_b = b.width;
     for (int i = n - 1; i >= 0 && alike; --i) {
-        alike = ax[i].stride >= std::max(span_a, span_b);
+        alike = (single_a || ax[i].stride >= span_a) && (single_b || ax[i].stride >= span_b);
+        ax[i].span_a = span_a;
+        ax[i].span_b = span_b;
         span_a += ax[i].stride * (ax[i].na - 1);
         span_b += ax[i].stride * (ax[i].nb - 1);
     }
-    if (alike) return meets(ax, n, ((int64_t)b0 - (int64_t)a0) / ea, a.dim, b.dim);
+    if (alike) return meets(ax, n, (int64_t)b.p - (int64_t)a.p, a.width, b.width);
 
-    const int64_t step = a.stride_token * ea;
-    if (step > 0 && step == b.stride_token * eb && (a.batch == 1 || a.stride_batch % a.stride_token == 0) &&
-        (b.batch == 1 || b.stride_batch % b.stride_token == 0)) {
-        const int64_t wa = ((a.heads - 1) * a.stride_head + a.dim) * ea, wb = ((b.heads - 1) * b.stride_head + b.dim) * eb;
-        const int64_t d = (int64_t)((a0 >= b0 ? (a0 - b0) % (uintptr_t)step : (step - (b0 - a0) % (uintptr_t)step) % step));
+    const int64_t step = a.stride[1];
+    if (step > 0 && step == b.stride[1] && (a.n[0] == 1 || a.stride[0] % step == 0) && (b.n[0] == 1 || b.stride[0] % step == 0)) {
+        const int64_t wa = (a.n[2] - 1) * a.stride[2] + a.width, wb = (b.n[2] - 1) * b.stride[2] + b.width;
+        const int64_t d = a.p >= b.p ? (int64_t)((a.p - b.p) % (uintptr_t)step) : (step - (int64_t)((b.p - a.p) % (uintptr_t)step)) % step;
         if (d >= wb && d + wa <= step) return false;
     }
     return true;
@@ -237,8 +256,15 @@ bool same_place(const disco_heads_t& a, const disco_heads_t& b) {
            (a.tokens <= 1 || a.stride_token == b.stride_token) && (a.heads <= 1 || a.stride_head == b.stride_head);
 }
 
-void check_apart(const disco_heads_t* out, const char* no, const disco_heads_t* in, const char* ni) {
-    if (may_overlap(*out, *in)) refuse(DISCO_ERR_INVALID_ARGUMENT, std::string(no) + " overlaps " + ni);
+// Everything that a call writes lies apart from all else that it reads and writes.
+void check_apart(std::initializer_list<Place> written, std::initializer_list<Place> read) {
+    for (const Place* w = written.begin(); w != written.end(); ++w) {
+        auto check = [&](const Place& o) {
+            if (may_overlap(*w, o)) refuse(DISCO_ERR_INVALID_ARGUMENT, std::string(w->name) + " overlaps " + o.name);
+        };
+        for (const Place& r : read) check(r);
+        for (const Place* o = written.begin(); o != w; ++o) check(*o);
+    }
 }
 
 Heads heads_of(const disco_heads_t* t) { return Heads{t->data, t->stride_batch, t->stride_token, t->stride_head}; }
@@ -277,7 +303,7 @@ void check_rotate(const disco_heads_t* x, int32_t norm, const disco_tensor_t* w,
     if (r->rows > 0 && (!r->cosines || !r->sines)) refuse(DISCO_ERR_INVALID_ARGUMENT, "rotation tables are NULL");
     if (!r->positions && !empty(*x) && (r->first_position > r->rows || x->tokens > r->rows - r->first_position))
         refuse(DISCO_ERR_SHAPE, "the rotation tables end before the last token");
-    if (r->position_stride_batch > kMaxOffset)
+    if (r->position_stride_batch > kMaxOffset / std::max<int64_t>(x->batch, 1))
         refuse(DISCO_ERR_INVALID_ARGUMENT, "position stride out of range");
     a->rotary = r->rotary_dim;
     a->interleaved = r->layout == DISCO_ROTARY_INTERLEAVED;
@@ -287,6 +313,15 @@ void check_rotate(const disco_heads_t* x, int32_t norm, const disco_tensor_t* w,
     a->positions = r->positions;
     a->pos_sb = r->position_stride_batch;
     a->pos0 = r->first_position;
+}
+
+// The small arguments as places.
+Place weight_place(const RotateArgs& a, const char* name, const void* p) {
+    return place(name, p, (a.weight_sh ? a.heads : 1) * a.dim * (int64_t)(a.bf16 ? 2 : 4));
+}
+Place table_place(const RotateArgs& a, const char* name, const float* p) { return place(name, p, std::min(a.rows, kMaxOffset) * (a.rotary / 2) * (int64_t)sizeof(float)); }
+Place position_place(const RotateArgs& a) {
+    return place("positions", a.positions, ((a.batch - 1) * a.pos_sb + a.tokens) * (int64_t)sizeof(int32_t));
 }
 
 void take_rotation(Device* d, const RotateArgs& a) {
@@ -332,11 +367,19 @@ void check_attend(const disco_heads_t* q, const disco_heads_t* k, const disco_he
     a->k = heads_of(k);
     if (v) a->v = heads_of(v);
     if (!o) return;
-    if (o->bias_stride_batch < 0 || o->bias_stride_batch > kMaxOffset)
+    if (o->bias_stride_batch < 0 || o->bias_stride_batch > kMaxOffset / std::max<int64_t>(q->batch, 1))
         refuse(DISCO_ERR_INVALID_ARGUMENT, "bias stride out of range");
     a->bias = o->key_bias;
     a->bias_sb = o->bias_stride_batch;
     a->lengths = o->key_lengths;
+}
+
+Place bias_place(const AttendArgs& a) {
+    return place("key_bias", a.bias, a.keys > 0 ? ((a.batch - 1) * a.bias_sb + a.keys) * (int64_t)sizeof(float) : 0);
+}
+Place lengths_place(const AttendArgs& a) { return place("key_lengths", a.lengths, a.batch * (int64_t)sizeof(int32_t)); }
+Place stats_place(const AttendArgs& a) {
+    return place("stats", a.stats, (int64_t)a.batch * a.heads * a.queries * 2 * (int64_t)sizeof(float));
 }
 
 void take_attend(Device* d, const AttendArgs& a, const disco_heads_t* q, const disco_heads_t* k) {
@@ -424,8 +467,9 @@ disco_status_t disco_norm_rotate(const disco_heads_t* x, int32_t norm, const dis
         check_same(x, "x", y, "y");
         RotateArgs a;
         check_rotate(x, norm, weight, eps, rotation, &a);
-        if (!same_place(*x, *y)) check_apart(y, "y", x, "x");
         if (empty(*x)) return;
+        check_apart({place("y", y)}, {place("x", same_place(*x, *y) ? nullptr : x), weight_place(a, "weight", a.weight),
+                                      table_place(a, "cosines", a.cosines), table_place(a, "sines", a.sines), position_place(a)});
         a.x = heads_of(x);
         a.y = heads_of(y);
         a.stream = stream;
@@ -480,20 +524,14 @@ disco_status_t disco_norm_rotate_backward(const disco_heads_t* x, int32_t norm, 
         if (dweight) {
             if (!dweight->data) refuse(DISCO_ERR_INVALID_ARGUMENT, "dweight.data is NULL");
             a.dweight = dweight->data;
-            const disco_heads_t row{dweight->data, dweight->dtype, dy->dim, weight->ndim == 2 ? dy->heads : 1, 0, 1, 1,
-                                    0, 0, dy->dim};
-            if (x) check_apart(&row, "dweight", x, "x");
-            check_apart(&row, "dweight", dy, "dy");
-            if (dx) check_apart(&row, "dweight", dx, "dx");
-            disco_heads_t wt = row;
-            wt.data = weight->data;
-            check_apart(&row, "dweight", &wt, "weight");
-        }
-        if (dx) {
-            if (!same_place(*dx, *dy)) check_apart(dx, "dx", dy, "dy");
-            if (x) check_apart(dx, "dx", x, "x");
         }
         if (!a.dweight && (!dx || empty(*dy))) return;
+        const size_t need = a.dweight ? rotate_grad_ws_bytes(a) : 0;
+        const Place dw = weight_place(a, "dweight", a.dweight), in_x = place("x", x), in_dy = place("dy", dy),
+                    wt = weight_place(a, "weight", a.weight), c = table_place(a, "cosines", a.cosines),
+                    sn = table_place(a, "sines", a.sines), pos = position_place(a), ws_in = place("the workspace", workspace, (int64_t)need);
+        check_apart({dw, ws_in}, {in_x, in_dy, wt, c, sn, pos});
+        if (dx) check_apart({place("dx", dx)}, {in_x, same_place(*dx, *dy) ? Place{} : in_dy, wt, c, sn, pos, dw, ws_in});
         a.dy = heads_of(dy);
         if (x) a.x = heads_of(x);
         if (dx) a.dx = heads_of(dx);
@@ -506,7 +544,6 @@ disco_status_t disco_norm_rotate_backward(const disco_heads_t* x, int32_t norm, 
         }
         d.take(a.dweight, "dweight");
         take_rotation(&d, a);
-        const size_t need = a.dweight ? rotate_grad_ws_bytes(a) : 0;
         if (need && workspace) d.take(workspace, "workspace");
         d.enter();
         Workspace ws(workspace, workspace_bytes, need, stream);
@@ -535,27 +572,24 @@ disco_status_t disco_cross_attention(const disco_heads_t* q, const disco_heads_t
         check_attend(q, k, v, options, &a);
         check_output(out, "out");
         check_same(q, "q", out, "out");
-        for (auto& t : {std::make_pair(q, "q"), std::make_pair(k, "k"), std::make_pair(v, "v")})
-            check_apart(out, "out", t.first, t.second);
         if (low) {
             if (!a.bf16) refuse(DISCO_ERR_DTYPE, "low is for bf16");
             check_output(low, "low");
             check_same(q, "q", low, "low");
-            for (auto& t : {std::make_pair(q, "q"), std::make_pair(k, "k"), std::make_pair(v, "v"),
-                            std::make_pair((const disco_heads_t*)out, "out")})
-                check_apart(low, "low", t.first, t.second);
             a.low = heads_of(low);
         }
         if (empty(*q)) return;
         a.out = heads_of(out);
         a.stats = stats;
         a.stream = stream;
+        const size_t need = attend_ws_bytes(a);
+        check_apart({place("out", out), place("low", low), stats_place(a), place("the workspace", workspace, (int64_t)need)},
+                    {place("q", q), place("k", k), place("v", v), bias_place(a), lengths_place(a)});
         Device d;
         take_attend(&d, a, q, k);
         d.take(out->data, "out");
         d.take(a.low.p, "low");
         d.take(stats, "stats");
-        const size_t need = attend_ws_bytes(a);
         if (need && workspace) d.take(workspace, "workspace");
         d.enter();
         Workspace ws(workspace, workspace_bytes, need, stream);
@@ -585,13 +619,9 @@ disco_status_t disco_cross_attention_backward(const disco_heads_t* q, const disc
             a.low = heads_of(low);
         }
         const std::pair<disco_heads_t*, const char*> outs[] = {{dq, "dq"}, {dk, "dk"}, {dv, "dv"}};
-        const std::pair<const disco_heads_t*, const char*> ins[] = {{q, "q"}, {k, "k"}, {v, "v"}, {out, "out"}, {dout, "dout"}};
         for (int i = 0; i < 3; ++i) {
             check_output(outs[i].first, outs[i].second);
             check_same(outs[i].first, outs[i].second, i == 0 ? q : k, i == 0 ? "q" : "k");
-            for (const auto& in : ins) check_apart(outs[i].first, outs[i].second, in.first, in.second);
-            if (low) check_apart(outs[i].first, outs[i].second, low, "low");
-            for (int j = 0; j < i; ++j) check_apart(outs[i].first, outs[i].second, outs[j].first, outs[j].second);
         }
         if (empty(*q) && empty(*k)) return;
         if (!empty(*q) && !stats) refuse(DISCO_ERR_INVALID_ARGUMENT, "stats is NULL");
@@ -602,6 +632,10 @@ disco_status_t disco_cross_attention_backward(const disco_heads_t* q, const disc
         a.dv = heads_of(dv);
         a.stats = const_cast<float*>(stats);
         a.stream = stream;
+        const size_t need = attend_grad_ws_bytes(a);
+        check_apart({place("dq", dq), place("dk", dk), place("dv", dv), place("the workspace", workspace, (int64_t)need)},
+                    {place("q", q), place("k", k), place("v", v), place("out", out), place("low", low), place("dout", dout),
+                     stats_place(a), bias_place(a), lengths_place(a)});
         Device d;
         take_attend(&d, a, q, k);
         if (!empty(*q)) {
@@ -615,7 +649,6 @@ disco_status_t disco_cross_attention_backward(const disco_heads_t* q, const disc
             d.take(dk->data, "dk");
             d.take(dv->data, "dv");
         }
-        const size_t need = attend_grad_ws_bytes(a);
         if (need && workspace) d.take(workspace, "workspace");
         d.enter();
         Workspace ws(workspace, workspace_bytes, need, stream);
@@ -642,19 +675,20 @@ disco_status_t disco_gradient_clip(int32_t count, const disco_tensor_t* grads, d
         if (clipped && !(max_norm >= 0.0)) refuse(DISCO_ERR_INVALID_ARGUMENT, "max_norm must be >= 0");
         if (!(eps >= 0.0) || !std::isfinite(eps)) refuse(DISCO_ERR_INVALID_ARGUMENT, "eps must be >= 0 and finite");
         check_ranges(t);
-        const uintptr_t n0 = (uintptr_t)norm;
+        const size_t need = clip_ws_bytes(t.data(), (int)t.size());
+        const Place n0 = place("norm", norm, sizeof(float)), w0 = place("the workspace", workspace, (int64_t)need);
+        check_apart({n0, w0}, {});
+        for (const ClipTensor& x : t) {
+            const int64_t len = x.n * (x.bf16 ? 2 : 4);
+            check_apart({n0, w0}, {place("a gradient", x.g, len), place("a clipped gradient", x.out, len)});
+        }
         Device d;
         d.take(norm, "norm");
         for (const ClipTensor& x : t) {
             if (x.n == 0) continue;
-            const uintptr_t len = (uintptr_t)x.n * (x.bf16 ? 2 : 4);
-            for (const void* p : {x.g, (const void*)x.out})
-                if (p && n0 + sizeof(float) > (uintptr_t)p && n0 < (uintptr_t)p + len)
-                    refuse(DISCO_ERR_INVALID_ARGUMENT, "norm overlaps a gradient");
             d.take(x.g, "a gradient");
             if (x.out && x.out != x.g) d.take(x.out, "a clipped gradient");
         }
-        const size_t need = clip_ws_bytes(t.data(), (int)t.size());
         if (need && workspace) d.take(workspace, "workspace");
         d.enter();
         Workspace ws(workspace, workspace_bytes, need, stream);

@@ -114,3 +114,131 @@ def test_in_place_whatever_the_stride_of_a_single_entry(shape):
     assert not refused(x, y)
     call = disco.library().disco_norm_rotate_backward
     assert call(None, 0, None, 0.0, None, x, y, None, None, 0, None) == disco.DISCO_ERR_DEVICE
+
+
+# ---- outputs beside tables, masks, statistics and scratch memory ------------------------------------------------------
+INVALID, DEVICE = disco.DISCO_ERR_INVALID_ARGUMENT, disco.DISCO_ERR_DEVICE
+FAR = 0x80000000
+
+
+def weight(address, n=8):
+    return disco.Tensor(address, disco.DISCO_FLOAT32, 1, (ctypes.c_int64 * 4)(n, 0, 0, 0))
+
+
+def dense(n, shape=(2, 5, 3, 8), data=None):
+    B, S, H, D = shape
+    h = heads(shape, (S * H * D, H * D, D), n * 100000)
+    if data is not None:
+        h.data = data
+    return h
+
+
+# y spans 960 bytes; a table of 6 rows of 2, positions [2, 5], a weight of 8
+@pytest.mark.parametrize("what,size", [("weight", 32), ("cosines", 48), ("sines", 48), ("positions", 40)])
+@pytest.mark.parametrize("back", [False, True])
+def test_norm_rotate_refuses_outputs_over_its_small_arguments(what, size, back):
+    x, y = dense(1), dense(2)
+    for at, status in ((y.data, INVALID), (y.data + 956, INVALID), (y.data - size + 4, INVALID), (y.data + 960, DEVICE),
+                       (y.data - size, DEVICE)):
+        a = {"weight": FAR, "cosines": FAR + 4096, "sines": FAR + 8192, "positions": FAR + 16384}
+        a[what] = at
+        rot = disco.RotationArgs(4, 0, a["cosines"], a["sines"], 6, a["positions"], 5, 0)
+        lib = disco.library()
+        got = lib.disco_norm_rotate_backward(x, 1, weight(a["weight"]), 0.0, rot, dense(3), y, None, None, 0, None) if back else \
+            lib.disco_norm_rotate(x, 1, weight(a["weight"]), 0.0, rot, y, None)
+        assert got == status, (what, hex(at))
+
+
+@pytest.mark.parametrize("what,size", [("cosines", 48), ("sines", 48), ("positions", 40)])
+def test_the_weights_gradient_lies_apart_from_tables(what, size):
+    a = {"cosines": FAR + 4096, "sines": FAR + 8192, "positions": FAR + 16384}
+    for at, status in ((FAR + 256, INVALID), (FAR + 256 + 28, INVALID), (FAR + 256 + 32, DEVICE)):
+        a[what] = at
+        rot = disco.RotationArgs(4, 0, a["cosines"], a["sines"], 6, a["positions"], 5, 0)
+        assert disco.library().disco_norm_rotate_backward(dense(1), 1, weight(FAR), 0.0, rot, dense(3), None, weight(FAR + 256),
+                                                          None, 0, None) == status
+
+
+def test_a_small_argument_between_the_rows_of_an_output():
+    """Gaps that hold it are no overlap: after each token, and between batch items."""
+    for shape, strides, gap, n in (((2, 5, 3, 8), (200, 40, 8), 24, 10), ((2, 5, 3, 8), (500, 24, 8), 120, 300)):
+        y = heads(shape, strides, 0)
+        base = disco.RotationArgs(4, 0, FAR, FAR + 4096, 6, None, 0, 0)
+        for off, status in ((gap, DEVICE), (gap - 1, INVALID), (gap + 81 if n > 10 else gap + 9, INVALID)):
+            rot = disco.RotationArgs(4, 0, BASE + 4 * off, FAR + 4096, n // 2, None, 0, 0)
+            assert disco.library().disco_norm_rotate(dense(5), 0, None, 0.0, rot, y, None) == status, (strides, off)
+        assert disco.library().disco_norm_rotate(dense(5), 0, None, 0.0, base, y, None) == DEVICE
+
+
+# batch 2, 5 queries, 7 keys, 3 heads of 8, fp32: stats 2 * 3 * 5 * 2 floats, bias [2, 7], lengths [2]
+@pytest.mark.parametrize("what,size", [("bias", 56), ("lengths", 8)])
+@pytest.mark.parametrize("back", [False, True])
+def test_attention_refuses_outputs_over_its_masks(what, size, back):
+    for n, out_bytes in ((4, 960),) if not back else ((6, 960), (7, 1344), (8, 1344)):
+        at0 = BASE + 400000 * n
+        for at, status in ((at0, INVALID), (at0 + out_bytes - 4, INVALID), (at0 - size + 4, INVALID), (at0 + out_bytes, DEVICE)):
+            a = {"bias": FAR, "lengths": FAR + 4096, what: at}
+            opt = disco.AttentionArgs(0.0, a["bias"], 7, a["lengths"])
+            assert attend(opt, back) == status, (what, n, hex(at))
+
+
+def attend(opt=None, back=False, stats=FAR + 65536, workspace=None, nbytes=0):
+    lib = disco.library()
+    q, out = dense(1), dense(4)
+    k, v = dense(2, (2, 7, 3, 8)), dense(3, (2, 7, 3, 8))
+    if not back:
+        return lib.disco_cross_attention(q, k, v, opt, out, stats, None, workspace, nbytes, None)
+    return lib.disco_cross_attention_backward(q, k, v, opt, out, stats, None, dense(5), dense(6), dense(7, (2, 7, 3, 8)),
+                                              dense(8, (2, 7, 3, 8)), workspace, nbytes, None)
+
+
+def test_statistics_lie_apart():
+    opt = disco.AttentionArgs(0.0, FAR, 7, FAR + 4096)
+    for n, size in ((1, 960), (2, 1344), (3, 1344), (4, 960)):
+        at = BASE + 400000 * n
+        assert attend(opt, stats=at) == INVALID and attend(opt, stats=at + size - 4) == INVALID
+        assert attend(opt, stats=at + size) == DEVICE
+    assert attend(opt, stats=FAR) == INVALID and attend(opt, stats=FAR + 4096) == INVALID
+    for n, size in ((6, 960), (7, 1344), (8, 1344)):
+        at = BASE + 400000 * n
+        assert attend(opt, True, stats=at) == INVALID and attend(opt, True, stats=at + size) == DEVICE
+
+
+def test_the_workspace_lies_apart():
+    lib, n = disco.library(), ctypes.c_size_t()
+    # (the backward call's; the forward call of these sizes needs none)
+    assert lib.disco_cross_attention_workspace(dense(1), dense(2, (2, 7, 3, 8)), 1, n) == 0 and n.value > 0
+    opt = disco.AttentionArgs(0.0, FAR, 7, FAR + 4096)
+    size = 1 << 20
+    for i in range(1, 9):
+        at = (BASE + 400000 * i) // 256 * 256
+        assert attend(opt, True, workspace=at, nbytes=size) == INVALID, i
+    for at in (FAR, FAR + 4096, FAR + 65536):
+        assert attend(opt, True, workspace=at, nbytes=size) == INVALID
+    assert attend(opt, True, workspace=FAR + (1 << 20), nbytes=size) == DEVICE
+    # one query, keys in parts
+    q, k, v, out = (dense(i, s) for i, s in ((1, (1, 1, 1, 8)), (2, (1, 4000, 1, 8)), (3, (1, 4000, 1, 8)), (4, (1, 1, 1, 8))))
+    assert lib.disco_cross_attention_workspace(q, k, 0, n) == 0 and n.value > 0
+    for t in (q, k, v, out):
+        assert lib.disco_cross_attention(q, k, v, None, out, None, None, t.data // 256 * 256, size, None) == INVALID
+    assert lib.disco_cross_attention(q, k, v, None, out, None, None, FAR, size, None) == DEVICE
+    # the weight's gradient
+    x, dy, dx = dense(1), dense(2), dense(3)
+    assert lib.disco_norm_rotate_workspace(dy, weight(FAR), n) == 0 and n.value > 0
+    run = lambda ws: lib.disco_norm_rotate_backward(x, 1, weight(FAR + 4096), 0.0, None, dy, dx, weight(FAR), ws, 1 << 30, None)
+    for at in (x.data, dy.data, dx.data, FAR, FAR + 4096):
+        assert run(at // 256 * 256) == INVALID
+    assert run(FAR + (1 << 28)) == DEVICE
+
+
+def test_clipping_keeps_its_workspace_apart():
+    lib, n = disco.library(), ctypes.c_size_t()
+    grads, outs = ((disco.Tensor * 1)(weight(at, 100000)) for at in (FAR, FAR + (1 << 22)))
+    g, o = ctypes.addressof(grads), ctypes.addressof(outs)
+    assert lib.disco_gradient_clip_workspace(1, g, n) == 0 and n.value > 0
+    norm = FAR + (1 << 24)
+    run = lambda ws, clipped=o: lib.disco_gradient_clip(1, g, clipped, 1.0, 0.0, norm, ws, 1 << 20, None)
+    for at in (FAR, FAR + 4 * 100000 // 256 * 256, FAR + (1 << 22), norm):
+        assert run(at) == INVALID
+    assert run(FAR, None) == INVALID and run(FAR + (1 << 22), None) == DEVICE
+    assert run(FAR + (1 << 25)) == DEVICE
