@@ -482,8 +482,9 @@ disco_status_t disco_cross_attention_workspace(const disco_heads_t* q, const dis
  *   clipped = g * min(1, max_norm / (norm + eps)),
  * grads[count] of any shapes (ndim 0..4), each fp32 or bf16; clipped[i] of grads[i]'s type and
  * shape, the same memory (in place) or apart from all of them; clipped NULL: the norm alone.  norm: one
- * device float.  The squares are summed in 64 bits in an order that depends on
- * the sizes alone; nothing is read back to the host.  A norm that is not finite propagates as the formula has it. */
+ * device float (infinity beyond fp32).  The squares are summed in 64 bits in an
+ * order that depends on the sizes alone, and the factor is theirs before any rounding
+ * to fp32; nothing is read back to the host.  A norm that is not finite propagates as the formula has it. */
 disco_status_t disco_gradient_clip(int32_t count, const disco_tensor_t* grads, disco_tensor_t* clipped,
                                    double max_norm, double eps, float* norm, void* workspace,
                                    size_t workspace_bytes, hipStream_t stream);

@@ -7,7 +7,8 @@
 // third launch and no atomic is needed, and every run gives the same bits) and
 // scale their part.  Small sets take one launch of one workgroup.  Squares
 // are added in 64 bits: an fp64 multiply-add a value is still far below the
-// memory's time, and no fp32 gradient over- or underflows.  Bound by the
+// memory's time, and no fp32 gradient over- or underflows; the factor is taken
+// in 64 bits too, since the norm of finite gradients may pass fp32.  Bound by the
 // memory: two reads and a write of every value, the second read from the
 // caches where the set fits them.  60 tensors of fp32 and bf16, 1.26 GB: 186 us
 // (6.8 TB/s) and 500 us (5.0 TB/s).
@@ -109,18 +110,24 @@ __device__ __forceinline__ double squares(const T* p, int64_t lo, int64_t hi) {
     return s;
 }
 
+// The factor in two: what is below the normal values of fp32 keeps its bits.
+struct Factor {
+    float first, second;
+    __device__ __forceinline__ bool one() const { return first == 1.0f && second == 1.0f; }
+};
+
 template <typename T, int THREADS>
-__device__ __forceinline__ void scale(const T* p, T* q, int64_t lo, int64_t hi, float c) {
+__device__ __forceinline__ void scale(const T* p, T* q, int64_t lo, int64_t hi, Factor c) {
     walk<T, THREADS, false>(
         p, q, lo, hi,
         [&](int64_t i, auto v) {
             typedef decltype(v) V;
             V r;
 #pragma unroll
-            for (int j = 0; j < Wide<T>::n; ++j) r[j] = (T)((float)v[j] * c);
+            for (int j = 0; j < Wide<T>::n; ++j) r[j] = (T)((float)v[j] * c.first * c.second);
             *(V*)(q + i) = r;
         },
-        [&](int64_t i) { q[i] = (T)((float)p[i] * c); });
+        [&](int64_t i) { q[i] = (T)((float)p[i] * c.first * c.second); });
 }
 
 // Sum over the workgroup, the same value in every thread.
@@ -135,11 +142,12 @@ __device__ __forceinline__ double block_sum(double v) {
     return s;
 }
 
-__device__ __forceinline__ float factor(double total, float max_norm, float eps, float* norm) {
-    const float n = (float)sqrt(total);
-    if (norm && threadIdx.x == 0) *norm = n;
-    const float c = max_norm / (n + eps);
-    return c > 1.0f ? 1.0f : c;  // NaN stays
+__device__ __forceinline__ Factor factor(double total, double max_norm, double eps, float* norm) {
+    const double n = sqrt(total);
+    if (norm && threadIdx.x == 0) *norm = (float)n;
+    const double q = max_norm / (n + eps), c = q > 1.0 ? 1.0 : q;  // NaN stays
+    const float first = c < 0x1p-126 ? 0x1p-126f : 1.0f;
+    return Factor{first, (float)(c / first)};
 }
 
 // Calls f(tensor, lo, hi) on this workgroup's pieces: every gridDim.x-th, so
@@ -169,26 +177,26 @@ __global__ __launch_bounds__(kThreads) void k_clip_squares(ClipSet s, double* __
 
 // norm is written by the launch that is given it.
 __global__ __launch_bounds__(kThreads) void k_clip_scale(ClipSet s, const double* __restrict__ partial, int n_partial,
-                                                         float max_norm, float eps, float* __restrict__ norm) {
+                                                         double max_norm, double eps, float* __restrict__ norm) {
     double v = 0.0;
     for (int i = threadIdx.x; i < n_partial; i += kThreads) v += partial[i];
-    const float c = factor(block_sum<kThreads>(v), max_norm, eps, blockIdx.x == 0 ? norm : nullptr);
+    const Factor c = factor(block_sum<kThreads>(v), max_norm, eps, blockIdx.x == 0 ? norm : nullptr);
     pieces_of(s, [&](int t, int64_t lo, int64_t hi) {
-        if (!s.out[t] || (c == 1.0f && s.out[t] == s.g[t])) return;
+        if (!s.out[t] || (c.one() && s.out[t] == s.g[t])) return;
         if (s.bf16[t]) scale<__bf16, kThreads>((const __bf16*)s.g[t], (__bf16*)s.out[t], lo, hi, c);
         else scale<float, kThreads>((const float*)s.g[t], (float*)s.out[t], lo, hi, c);
     });
 }
 
-__global__ __launch_bounds__(kSmallThreads) void k_clip_small(ClipSet s, float max_norm, float eps,
+__global__ __launch_bounds__(kSmallThreads) void k_clip_small(ClipSet s, double max_norm, double eps,
                                                               float* __restrict__ norm) {
     double v = 0.0;
     for (int t = 0; t < s.count; ++t)
         v += s.bf16[t] ? squares<__bf16, kSmallThreads, false>((const __bf16*)s.g[t], 0, s.n[t])
                        : squares<float, kSmallThreads, false>((const float*)s.g[t], 0, s.n[t]);
-    const float c = factor(block_sum<kSmallThreads>(v), max_norm, eps, norm);
+    const Factor c = factor(block_sum<kSmallThreads>(v), max_norm, eps, norm);
     for (int t = 0; t < s.count; ++t) {
-        if (!s.out[t] || (c == 1.0f && s.out[t] == s.g[t])) continue;
+        if (!s.out[t] || (c.one() && s.out[t] == s.g[t])) continue;
         if (s.bf16[t]) scale<__bf16, kSmallThreads>((const __bf16*)s.g[t], (__bf16*)s.out[t], 0, s.n[t], c);
         else scale<float, kSmallThreads>((const float*)s.g[t], (float*)s.out[t], 0, s.n[t], c);
     }
@@ -237,7 +245,7 @@ size_t clip_ws_bytes(const ClipTensor* t, int n) {
     return blocks * sizeof(double);
 }
 
-hipError_t launch_clip(const ClipTensor* t, int n, float max_norm, float eps, float* norm, void* ws,
+hipError_t launch_clip(const ClipTensor* t, int n, double max_norm, double eps, float* norm, void* ws,
                        hipStream_t stream) {
     ClipSet s;
     int64_t total;

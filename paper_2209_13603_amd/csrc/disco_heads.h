@@ -75,7 +75,7 @@ struct ClipTensor {
     bool bf16;
 };
 size_t clip_ws_bytes(const ClipTensor* t, int n);
-hipError_t launch_clip(const ClipTensor* t, int n, float max_norm, float eps, float* norm, void* ws,
+hipError_t launch_clip(const ClipTensor* t, int n, double max_norm, double eps, float* norm, void* ws,
                        hipStream_t stream);
 
 }  // namespace disco

@@ -692,7 +692,7 @@ disco_status_t disco_gradient_clip(int32_t count, const disco_tensor_t* grads, d
         if (need && workspace) d.take(workspace, "workspace");
         d.enter();
         Workspace ws(workspace, workspace_bytes, need, stream);
-        check_hip(launch_clip(t.data(), (int)t.size(), (float)max_norm, (float)eps, norm, ws.p, stream), "kernel launch");
+        check_hip(launch_clip(t.data(), (int)t.size(), max_norm, eps, norm, ws.p, stream), "kernel launch");
     });
 }
 
