@@ -110,6 +110,24 @@ __device__ __forceinline__ int first_tile(int tiles, int part, int parts) {
     return q * part + min(part, r);
 }
 
+template <int N>
+__device__ __forceinline__ void clear(f16 (&o)[N]) {
+#pragma unroll
+    for (int d = 0; d < N; ++d)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) o[d][r] = 0.0f;
+}
+
+// (Selects: a branch behind the loop has cost registers in it, fp32 heads of 36
+// 100 -> 125 us.)
+template <int N>
+__device__ __forceinline__ void clear_if(bool yes, f16 (&o)[N]) {
+#pragma unroll
+    for (int d = 0; d < N; ++d)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) o[d][r] = yes ? 0.0f : o[d][r];
+}
+
 __device__ __forceinline__ float other_half(float v) { return __shfl_xor(v, 32); }
 
 template <int N, typename F>

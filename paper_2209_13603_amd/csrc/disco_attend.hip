@@ -79,15 +79,13 @@ __global__ __launch_bounds__(kAttendThreads, (kWorkgroups<T, DP>)) void k_attend
     const typename Tile::Lane ln = Tile::lane_of(lane);
 
     f16 o[DP / 32];
-#pragma unroll
-    for (int d = 0; d < DP / 32; ++d)
-#pragma unroll
-        for (int r = 0; r < 16; ++r) o[d][r] = 0.0f;
+    clear(o);
     float m = -INFINITY, l = 0.0f;
 
     St sk, sv;
     float bias = 0.0f;  // of the staged row
     int left = 0;       // rows of the staged tile that exist
+    uint64_t any = 0;   // whose staged keys were left, once at least
     const int64_t key0 = (int64_t)t0 * KT;
     Cursor<T> keys{(const T*)a.k.p + b * a.k.sb + hk * a.k.sh + key0 * a.k.st, a.k.st, (int)(n - key0), a.dim};
     Cursor<T> vals{(const T*)a.v.p + b * a.v.sb + hk * a.v.sh + key0 * a.v.st, a.v.st, (int)(n - key0), a.dim};
@@ -107,6 +105,7 @@ __global__ __launch_bounds__(kAttendThreads, (kWorkgroups<T, DP>)) void k_attend
     auto store = [&](int buf) {
         const float start = srow < left ? start_of(bias, inv_scale, a.bias_limit) : -INFINITY;
         const bool keep = start != -INFINITY;
+        any |= __ballot(keep);
         sk.store(lds + buf * 2 * St::kBytes, wave, lane, keep);
         sv.store(lds + (buf * 2 + 1) * St::kBytes, wave, lane, keep);
         if (lane % 4 == 0) starts[buf][srow] = start;  // (two waves to a row: the same value)
@@ -172,6 +171,12 @@ __global__ __launch_bounds__(kAttendThreads, (kWorkgroups<T, DP>)) void k_attend
     }
     l += other_half(l);
     Tile::settle(o, a.dim, lane);
+    // No key left here: zeros, whatever the queries hold (NaN times the zeros that
+    // stand for the keys is NaN).
+    const bool none = a.bias && !__syncthreads_or(any != 0);
+    m = none ? -INFINITY : m;
+    l = none ? 0.0f : l;
+    clear_if(none, o);
     const int64_t stat = ((int64_t)b * a.heads + h) * a.queries + i;
     if (c.splits > 1) {
         const int64_t all = (int64_t)a.batch * a.kv_heads * c.rows;

@@ -99,14 +99,12 @@ __global__ __launch_bounds__(kAttendThreads, (kWorkgroups<T, DP>)) void k_attend
     const typename Tile::Lane ln = Tile::lane_of(lane);
 
     f16 dq[DP / 32];
-#pragma unroll
-    for (int d = 0; d < DP / 32; ++d)
-#pragma unroll
-        for (int r = 0; r < 16; ++r) dq[d][r] = 0.0f;
+    clear(dq);
 
     St sk, sv;
     float bias = 0.0f;  // of the staged row
     int left = 0;       // rows of the staged tile that exist
+    uint64_t any = 0;   // whose staged keys were left, once at least
     const int64_t key0 = (int64_t)t0 * KT;
     Cursor<T> keys{(const T*)a.k.p + b * a.k.sb + hk * a.k.sh + key0 * a.k.st, a.k.st, (int)(n - key0), a.dim};
     Cursor<T> vals{(const T*)a.v.p + b * a.v.sb + hk * a.v.sh + key0 * a.v.st, a.v.st, (int)(n - key0), a.dim};
@@ -126,6 +124,7 @@ __global__ __launch_bounds__(kAttendThreads, (kWorkgroups<T, DP>)) void k_attend
     auto store = [&](int buf) {
         const float start = srow < left ? start_of(bias, inv_scale, a.bias_limit) : -INFINITY;
         const bool keep = start != -INFINITY;
+        any |= __ballot(keep);
         sk.store(lds + buf * 2 * St::kBytes, wave, lane, keep);
         sv.store(lds + (buf * 2 + 1) * St::kBytes, wave, lane, keep);
         if (lane % 4 == 0) starts[buf][srow] = start;  // (two waves to a row: the same value)
@@ -161,6 +160,7 @@ __global__ __launch_bounds__(kAttendThreads, (kWorkgroups<T, DP>)) void k_attend
         __syncthreads();
     }
     Tile::settle(dq, a.dim, lane);
+    clear_if(a.bias && !__syncthreads_or(any != 0), dq);  // as in the forward pass
     const float f = inv * a.scale;
     if (c.splits_q > 1) {
         const int64_t all = (int64_t)a.batch * a.kv_heads * c.rows;
@@ -204,10 +204,8 @@ __global__ __launch_bounds__(kAttendThreads, (kWorkgroups<T, DP>)) void k_attend
     if constexpr (kept) Tile::keep(mine, lane, kf);
     const typename Tile::Lane ln = Tile::lane_of(lane);
     f16 dk[DP / 32], dv[DP / 32];
-#pragma unroll
-    for (int d = 0; d < DP / 32; ++d)
-#pragma unroll
-        for (int r = 0; r < 16; ++r) dk[d][r] = dv[d][r] = 0.0f;
+    clear(dk);
+    clear(dv);
 
     // The tiles of the group's heads one after the other.
     const int tiles = (int)((a.queries + QT - 1) / QT), steps = (int64_t)kb * kCols < n ? tiles * G : 0;
@@ -291,11 +289,8 @@ __global__ __launch_bounds__(kAttendThreads, (kWorkgroups<T, DP>)) void k_attend
     }
     Tile::settle(dk, a.dim, lane);
     Tile::settle(dv, a.dim, lane);
-    if (!live)  // nothing of a key that is taken out
-#pragma unroll
-        for (int d = 0; d < DP / 32; ++d)
-#pragma unroll
-            for (int r = 0; r < 16; ++r) dk[d][r] = dv[d][r] = 0.0f;
+    clear_if(!live, dk);  // nothing of a key that is taken out
+    clear_if(!live, dv);
     const bool there = j < a.keys;
     if (c.splits_k > 1) {
         const int64_t all = (int64_t)a.batch * a.kv_heads * a.keys, at = split * 2 * all + (int64_t)bh * a.keys + j;
