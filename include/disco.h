@@ -432,7 +432,7 @@ disco_status_t disco_norm_rotate_backward(const disco_heads_t* x, int32_t norm, 
 disco_status_t disco_norm_rotate_workspace(const disco_heads_t* x, const disco_tensor_t* weight, size_t* bytes);
 
 typedef struct {
-    double scale;                /* of the scores; 0 selects 1 / sqrt(dim) */
+    double scale;                /* of the scores, |scale| from 2^-126 to 2^127; 0 selects 1 / sqrt(dim) */
     const float* key_bias;       /* NULL, or [batch][keys]: added to the scores of a key, e.g. the logarithm
                                     of its quadrature weight; -inf takes the key out */
     int64_t bias_stride_batch;   /* elements between batch items of key_bias; 0: the same for all */

@@ -5,6 +5,7 @@
 #include <rocprofiler-sdk-roctx/roctx.h>
 
 #include <algorithm>
+#include <cfloat>
 #include <cmath>
 #include <cstring>
 #include <exception>
@@ -351,7 +352,9 @@ void check_attend(const disco_heads_t* q, const disco_heads_t* k, const disco_he
         q->batch * q->tokens * q->heads >= kMaxRows * 16 || k->batch * k->tokens * k->heads >= kMaxRows * 16)
         refuse(DISCO_ERR_SHAPE, "batch * tokens * heads out of range");
     const double scale = o && o->scale != 0.0 ? o->scale : 1.0 / std::sqrt((double)q->dim);
-    if (!std::isfinite(scale)) refuse(DISCO_ERR_INVALID_ARGUMENT, "scale must be finite");
+    // (the kernels take it, its product with 1 / log 2 and its reciprocal in fp32)
+    if (!(std::fabs(scale) >= FLT_MIN) || !(std::fabs(scale) * 1.4426950408889634074 <= FLT_MAX))
+        refuse(DISCO_ERR_INVALID_ARGUMENT, "scale must be a normal number of fp32, at most 2^127");
     a->batch = (int32_t)q->batch;
     a->heads = q->heads;
     a->kv_heads = k->heads;
