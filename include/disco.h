@@ -445,7 +445,7 @@ typedef struct {
  * q, out [batch][queries][heads][dim]; k, v [batch][keys][kv_heads][dim], heads a
  * multiple of kv_heads, h' = h / (heads / kv_heads).  A query that no key is
  * left for gives zeros.  What k and v hold at keys taken out (infinities and
- * NaN too) reaches no output.  Finite biases beyond 2^100 |scale| (2^125 at
+ * NaN too) reaches no output.  Finite biases beyond 2^126 |scale| (about 2^125 at
  * most) on either side count as that; NaN and +inf give NaN.  For the backward call:
  *   stats  NULL, or [batch][heads][queries][2] floats: a reference near the
  *          row's largest score in units of log 2 (-inf: no key) and the sum of

@@ -363,8 +363,8 @@ void check_attend(const disco_heads_t* q, const disco_heads_t* k, const disco_he
     a->keys = k->tokens;
     a->scale = (float)scale;
     a->scale2 = (float)(scale * 1.4426950408889634074);
-    // (in units of log 2 too such a bias is finite)
-    a->bias_limit = (float)std::min(0x1p+100, 0x1p+126 / std::fabs(scale * 1.4426950408889634074));
+    // (with a product added and in units of log 2 too such a bias is finite)
+    a->bias_limit = (float)std::min(0x1p+126, 0x1p+126 / std::fabs(scale * 1.4426950408889634074));
     a->bf16 = q->dtype == DISCO_BFLOAT16;
     a->q = heads_of(q);
     a->k = heads_of(k);

@@ -203,3 +203,19 @@ def test_lowest_biases_at_scales_out_of_the_ordinary(queries, scale, dtype):
     want = _weighted(q, k, v, dout, torch.zeros(1, 2, queries, 3000), scale)
     for name, a, b in zip(("out", "dq", "dk", "dv"), _run(q, k, v, dout, key_bias=bias, scale=scale), want):
         _close(name, a, b, TOL[dtype])
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("queries", [1, 40])
+@pytest.mark.parametrize("low,high", [(-1e33, -1e31), (-1e36, -1e35), (1e31, 1e33), (1e35, 1e36)])
+def test_the_larger_of_two_large_biases(low, high, queries, dtype):
+    """Keys of one mask below keys of another, with no other key left: the larger bias takes all."""
+    import torch
+    q, k, v, dout = _make(1, queries, 3000, 2, 1, 64, dtype, 10)
+    bias = torch.full((3000,), low, device="cuda:0")
+    bias[1500:] = high
+    logits = torch.full((1, 2, queries, 3000), -math.inf)
+    logits[..., 1500:] = 0.0
+    want = _weighted(q, k, v, dout, logits, 1 / 8)
+    for name, a, b in zip(("out", "dq", "dk", "dv"), _run(q, k, v, dout, key_bias=bias), want):
+        _close(name, a, b, TOL[dtype])
