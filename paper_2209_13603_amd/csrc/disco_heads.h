@@ -38,7 +38,7 @@ struct RotateArgs {
     int64_t pos_sb = 0, pos0 = 0;
     int32_t batch = 0, heads = 0, dim = 0, rotary = 0;
     int64_t tokens = 0;
-    float eps = 0.0f;
+    float eps = 0.0f, eps_up = 0.0f;  // eps_up: 2^192 eps
     bool norm = false, interleaved = false, bf16 = false;
     hipStream_t stream = nullptr;
 };

@@ -292,6 +292,7 @@ void check_rotate(const disco_heads_t* x, int32_t norm, const disco_tensor_t* w,
     a->dim = x->dim;
     a->tokens = x->tokens;
     a->eps = (float)eps;
+    a->eps_up = eps > 0.0 ? std::max((float)(eps * 0x1p+192), FLT_MIN) : 0.0f;
     a->norm = norm != 0;
     a->bf16 = x->dtype == DISCO_BFLOAT16;
     if (!r || r->rotary_dim == 0) return;

@@ -14,7 +14,8 @@
 // the same 2 V to a lane; the lanes of a row, a power of two of them, share the
 // sums of squares by shuffles.  Rows of all heads of all tokens follow each
 // other over the lanes; angles and weight come from the caches (together 14 of
-// 58 us).  Statistics and sums are fp32; y, dx and dw are rounded once.
+// 58 us).  Statistics and sums are fp32, of rows brought into its range where their
+// squares leave it; y, dx and dw are rounded once.
 // Measured, 4 x 32768 tokens, 8 heads of 64, bf16: forward 62 us (268 MB, 4.3
 // TB/s; two heads a thread took 3 % off, four 5 % on), gradients 95 us (403 MB, 4.2 TB/s) and 7 us
 // for the weight's.
@@ -129,6 +130,15 @@ __device__ __forceinline__ bool load_angles(const RotateArgs& a, int64_t b, int6
     return true;
 }
 
+// What a row is multiplied by so that its squares stay in the range of fp32, ss
+// being their sum: 1 but for rows of entries around 1e15 and above, or 1e-12 and
+// below beside an eps as small.
+__device__ __forceinline__ float row_scale(float ss, float inv_d, float eps) {
+    return ss > 0x1p+100f ? 0x1p-96f : fmaf(ss, inv_d, eps) < 0x1p-80f ? 0x1p+96f : 1.0f;
+}
+// eps beside the squares of a row that was multiplied by f.
+__device__ __forceinline__ float scaled_eps(const RotateArgs& a, float f) { return f > 1.0f ? a.eps_up : a.eps * f * f; }
+
 // Token and head of a row.
 struct Place {
     int64_t b, tok;
@@ -174,10 +184,22 @@ __global__ __launch_bounds__(kThreads) void k_rotate(RotateArgs a, Shape sh) {
         if (it.has_b) load<T, V>(wp + it.b, w + V);
     }
     if (a.norm) {
-        float ss = 0.0f;
+        const float inv_d = 1.0f / (float)a.dim;
+        auto squares = [&] {
+            float ss = 0.0f;
 #pragma unroll
-        for (int i = 0; i < 2 * V; ++i) ss = fmaf(e[i], e[i], ss);
-        r *= rsqrtf(fmaf(lane_sum(ss, sh.lanes), 1.0f / (float)a.dim, a.eps));
+            for (int i = 0; i < 2 * V; ++i) ss = fmaf(e[i], e[i], ss);
+            return lane_sum(ss, sh.lanes);
+        };
+        float ss = squares(), eps = a.eps;
+        const float f = row_scale(ss, inv_d, eps);
+        if (__any(f != 1.0f)) {
+#pragma unroll
+            for (int i = 0; i < 2 * V; ++i) e[i] *= f;
+            ss = squares();
+            eps = scaled_eps(a, f);
+        }
+        r *= rsqrtf(fmaf(ss, inv_d, eps));
     }
 #pragma unroll
     for (int i = 0; i < 2 * V; ++i) e[i] = e[i] * r * w[i];
@@ -221,18 +243,36 @@ __global__ __launch_bounds__(kThreads) void k_rotate_grad(RotateArgs a, Shape sh
         if (a.weight && a.weight_sh && !sh.per_head) load_weight(p.h);
         if (it.rot) turn<V, INTER>(g, c, s, -1.0f);
         if (a.norm) {
-            float ss = 0.0f, tx = 0.0f;
+            float ss, tx, eps = a.eps;
+            auto sums = [&] {
+                ss = tx = 0.0f;
 #pragma unroll
-            for (int i = 0; i < 2 * V; ++i) {
-                ss = fmaf(e[i], e[i], ss);
-                tx = fmaf(w[i] * g[i], e[i], tx);
+                for (int i = 0; i < 2 * V; ++i) {
+                    ss = fmaf(e[i], e[i], ss);
+                    tx = fmaf(w[i] * g[i], e[i], tx);
+                }
+                ss = lane_sum(ss, sh.lanes);
+                tx = lane_sum(tx, sh.lanes);
+            };
+            sums();
+            const float f = row_scale(ss, inv_d, eps);
+            const bool any = __any(f != 1.0f);
+            if (any) {
+#pragma unroll
+                for (int i = 0; i < 2 * V; ++i) e[i] *= f;
+                sums();
+                eps = scaled_eps(a, f);
             }
-            const float r = poison * rsqrtf(fmaf(lane_sum(ss, sh.lanes), inv_d, a.eps));
-            const float m = r * r * lane_sum(tx, sh.lanes) * inv_d;  // mean(t n) r
+            const float r = poison * rsqrtf(fmaf(ss, inv_d, eps));
+            const float m = r * r * tx * inv_d;  // mean(t n) r
 #pragma unroll
             for (int i = 0; i < 2 * V; ++i) {
                 dw[i] = fmaf(g[i] * r, e[i], dw[i]);
                 g[i] = r * fmaf(-m, e[i], w[i] * g[i]);
+            }
+            if (any) {
+#pragma unroll
+                for (int i = 0; i < 2 * V; ++i) g[i] *= f;
             }
         } else {
 #pragma unroll
