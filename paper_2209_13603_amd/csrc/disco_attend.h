@@ -154,8 +154,14 @@ struct Mat<__bf16> {
     static __device__ __forceinline__ f16 scores(Frag a, Frag b, f16 c) {
         return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
     }
-    // P as the values' operand.  Rounded to nearest: an error of 2^-9 in the mean
-    // of each term, as large as that of the result's own rounding.
+    // P as the values' operand, and in the gradients P and dS: rounded to nearest,
+    // which the bf16 instructions need (fp32 ones run at an eighth of the rate).
+    // Each term carries a rounding of 2^-8 at most, as the result does: outputs are
+    // 2.1e-3 to 2.5e-3 from the definition in 64 bits, where a single rounding
+    // leaves 1.7e-3.  In two bf16 parts each they would leave that too, for 43 % more
+    // time forward (32768 x 8192, heads of 64: 670 -> 960 us; heads of 128 300 ->
+    // 393) and 24 % for dq (413 -> 512).  Sums, softmax statistics and the row sums of the
+    // gradients stay in fp32, and fp32 calls round nothing on the way.
     struct Probs {
         bf8 v[2];
         __device__ __forceinline__ Probs() {}
@@ -520,7 +526,7 @@ inline bool wide_rows(const Heads& t, int dim, int entries, size_t elem) {
 
 // How a call's rows go: 2 in 16-byte pieces, 1 in 8-byte pieces, 0 entry by
 // entry.  The step of 2 x 8192 queries to 2048 keys, 8 heads, bf16: heads of 40
-// (2) 390 us, of 36 (1) 440 us and entry by entry 1017 us, of 37 (0) 709 us.
+// (2) 384 us, of 36 (1) 387 us and entry by entry 775 us, of 37 (0) 725 us.
 inline int row_width(const AttendArgs& a) {
     const int ch = a.bf16 ? 8 : 4;
     int w = 2;

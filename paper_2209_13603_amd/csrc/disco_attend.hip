@@ -7,14 +7,15 @@
 // and values are rows of one tile (row = query * group + head of the group), so
 // that a single query of grouped heads reads them once.
 //
-// Bound.  Many rows: the matrix products and the softmax's vector instructions
-// share the issue of a SIMD and fill it (counters of the 32768 x 8192 case,
-// heads of 64: products 38 % of the cycles, vector 62 %; moving the row sums
-// onto the matrix cores only moved the time, 675 -> 710 us).  Measured: 32768 queries,
-// 8192 keys, 8 heads of 64, 668 us (824 TFLOP/s); 2 x 8192 queries, 2048 keys,
-// 16 heads of 128, 300 us (916 TFLOP/s).  Few rows: reading the keys and values
-// once; 4 queries of 16 heads on 4 against 131072 keys of 128, 1.07 GB, 194 us (5.5
-// TB/s).  fp32 (4050 x 1013, 15 heads of 36): 100 us.
+// Bound.  Heads of 64, many rows: the matrix products and the softmax's vector
+// instructions share the issue of a SIMD and fill it (counters of the 32768 x 8192
+// case: products 37 % of the cycles, vector 62 %; moving the row sums onto the
+// matrix cores only moved the time, 675 -> 710 us).  Heads of 128: 40 and 40 %, the rest waits
+// at the tiles' barriers with two workgroups a CU.  Measured: 32768 queries, 8192
+// keys, 8 heads of 64, 682 us (806 TFLOP/s); 2 x 8192 queries, 2048 keys, 16
+// heads of 128, 301 us (914 TFLOP/s).  Few rows: reading the keys and values once; 4
+// queries of 16 heads on 4 against 131072 keys of 128, 1.07 GB, 194 us a call
+// (5.5 TB/s).  fp32 (4050 x 1013, 15 heads of 36): 99 us.
 //
 // Where the rows leave CUs without two workgroups, the keys go to parts (at
 // least four tiles each) whose unnormed sums k_attend_join adds in their order.

@@ -12,13 +12,14 @@
 // dq and dk had errors of up to 2.4e-3, before any other rounding, where their
 // own is 1.7e-3.
 //
-// Bound: products and vector instructions share the issue of a SIMD.  2 x 8192
-// queries, 2048 keys, 16 heads on 4, of 128, bf16: dq 400 us (three products, 1030
-// TFLOP/s), dk and dv 545 us (four, 1010 TFLOP/s, 41 and 26 % of the cycles; the
-// sums of dk and dv take half the registers, so the key fragments stay in LDS:
-// 950 us in one workgroup a CU, 545 in two).  2 x 32768 queries, 77 keys, 8
-// heads of 64: 93 and 47 us, the rows' memory (0.34 GB for dq) in short workgroups.
-// fp32 (4050 x 1013, 15 heads of 36): 135 and 177 us.
+// Bound.  2 x 8192 queries, 2048 keys, 16 heads on 4, of 128, bf16: dq 416 us (three
+// products, 991 TFLOP/s; products 45 % and vector instructions 40 % of the
+// cycles, which they share), dk and dv 558 us (four, 985 TFLOP/s; 42 and 29 %: the sums of
+// dk and dv take half the registers, so the key fragments stay in LDS, 950 us in one
+// workgroup a CU, 545 in two, and a tile's parts run one after the other between
+// fences).  2 x 32768 queries, 77 keys, 8 heads of 64: 93 and 50 us, the rows' memory
+// (0.34 GB for dq) in short workgroups.  fp32 (4050 x 1013, 15 heads of 36): 132
+// and 178 us, products 39 and 33 %: workgroups of unequal lengths.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>

@@ -10,8 +10,8 @@
 // memory's time, and no fp32 gradient over- or underflows; the factor is taken
 // in 64 bits too, since the norm of finite gradients may pass fp32.  Bound by the
 // memory: two reads and a write of every value, the second read from the
-// caches where the set fits them.  60 tensors of fp32 and bf16, 1.26 GB: 186 us
-// (6.8 TB/s) and 500 us (5.0 TB/s).
+// caches where the set fits them.  60 tensors of fp32 and bf16, 1.26 GB: 184 us
+// (6.8 TB/s) and 503 us (5.0 TB/s).
 //
 // The tensors' addresses and sizes travel in the kernel arguments, up to
 // kMaxTensors of them a launch: nothing is uploaded, kept or looked up.
