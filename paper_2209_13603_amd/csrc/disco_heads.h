@@ -25,6 +25,27 @@ inline dim3 grid_dim(uint32_t groups) {
 // The workgroup's place in a grid of grid_dim.
 __device__ __forceinline__ uint32_t group_index() { return blockIdx.y * gridDim.x + blockIdx.x; }
 
+// Division of n < 2^31 by a fixed d: (mulhi(n, m) + n) >> s with s = ceil(log2 d),
+// m = floor(2^32 (2^s - d) / d) + 1 (Granlund and Montgomery, Division by invariant
+// integers using multiplication, 1994).
+struct Divisor {
+    uint32_t d, m, s;
+    __device__ __forceinline__ uint32_t quotient(uint32_t n) const { return (__umulhi(n, m) + n) >> s; }
+};
+inline Divisor divisor(uint32_t d) {
+    Divisor r{d, 0, 0};
+    while (((uint64_t)1 << r.s) < d) ++r.s;
+    r.m = (uint32_t)((((uint64_t)1 << 32) * (((uint64_t)1 << r.s) - d)) / d + 1);
+    return r;
+}
+
+// What a row is multiplied by so that its squares stay in the range of fp32, ss
+// being their sum: 1 but for rows of entries around 1e15 and above, or 1e-12 and
+// below beside an eps as small.
+__device__ __forceinline__ float row_scale(float ss, float inv_d, float eps) {
+    return ss > 0x1p+100f ? 0x1p-96f : fmaf(ss, inv_d, eps) < 0x1p-80f ? 0x1p+96f : 1.0f;
+}
+
 // ---- head norm and rotation (disco_rotate.hip) ------------------------------
 struct RotateArgs {
     Heads x, y, dy, dx;
