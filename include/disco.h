@@ -490,6 +490,107 @@ disco_status_t disco_gradient_clip(int32_t count, const disco_tensor_t* grads, d
                                    size_t workspace_bytes, hipStream_t stream);
 disco_status_t disco_gradient_clip_workspace(int32_t count, const disco_tensor_t* grads, size_t* bytes);
 
+/* ---- Blocks around attention: residual sums, dropout, recurrence in time --
+ *
+ * Around each attention a network keeps a residual stream of channel tensors
+ * [batch][tokens][channels], given with their strides; along the time steps
+ * of its fields it carries a state.  Devices, types, workspaces and what a call
+ * writes as above; sums, norms and states are fp32. */
+typedef struct {
+    void* data;           /* device pointer (may be NULL only when the tensor is empty) */
+    int32_t dtype;        /* disco_dtype_t */
+    int32_t reserved;     /* 0 */
+    int64_t batch, tokens, channels;     /* batch * tokens < 2^31; channels contiguous */
+    int64_t stride_batch, stride_token;  /* in elements, >= 0; of an output no two rows overlap */
+} disco_rows_t;
+
+/* Dropout by a counter-based generator: an entry stays, times 1 / (1 - p), with
+ * probability 1 - p, and is 0 otherwise, whatever it holds.  p is taken to the nearest multiple of
+ * 2^-16, in the factor too.  Entry c of row r (of all batch items' tokens) stays
+ * where half c % 8 (low halves first) of the four words of Philox4x32-10 at the counter (c / 8, r, low and
+ * high word of offset), key seed (low word first), is at least 65536 p: the mask
+ * depends on seed, offset and place alone, not on strides or on how the
+ * work is cut, and is stored nowhere. */
+typedef struct {
+    double p;                /* 0..1 */
+    uint64_t seed;
+    uint64_t offset;         /* another for each call that must draw anew */
+    const uint64_t* counter; /* NULL, or one device word that the kernels add to offset, so that a replayed
+                                graph draws anew once the program has raised it */
+} disco_dropout_t;
+
+/* y = dropout of x.  Its gradient is the same call on dy.  y has x's sizes and type and may be
+ * x itself.  Fewer than 2^31 chunks of eight entries of a row.  Errors: INVALID_ARGUMENT, SHAPE, DTYPE, DEVICE. */
+disco_status_t disco_dropout(const disco_rows_t* x, const disco_dropout_t* dropout, disco_rows_t* y, hipStream_t stream);
+
+typedef struct {
+    double scale;                      /* of the residual x */
+    double eps;
+    int32_t post_norm;                 /* 1: the block's output f is normed */
+    int32_t reserved;                  /* 0 */
+    const disco_tensor_t* post_weight; /* NULL (ones), [channels] or [batch, channels]; x's type; so are the others */
+    const disco_tensor_t* gate;
+    const disco_tensor_t* next_weight;
+    const disco_dropout_t* dropout;    /* NULL: none */
+} disco_residual_t;
+
+/* Residual sum of a block with the norm after it, its gate and dropout, and the
+ * norm before the next block, in one pass:
+ *   h = scale x + gate * dropout(post_weight * f / rms(f)),   y = next_weight * h / rms(h),
+ *   rms(v) = sqrt(mean(v^2) + eps) over the row's channels (f itself without post_norm).
+ * x NULL: no residual.  h or y may be NULL; each may be x or f itself (not both the
+ * same).  y is taken from h before its rounding.  channels 1..8192.  options
+ * NULL: scale 1, eps 1e-6 and nothing else.  Errors: INVALID_ARGUMENT, SHAPE, DTYPE, DEVICE. */
+disco_status_t disco_residual_norm(const disco_rows_t* x, const disco_rows_t* f, const disco_residual_t* options,
+                                   disco_rows_t* h, disco_rows_t* y, hipStream_t stream);
+
+/* Gradients of disco_residual_norm for dh and dy (either may be NULL: zeros) from
+ * its inputs: dx, df (each may be x, f, dh or dy itself, not both the same) and the
+ * gradients of the weights (their shapes and types); any may be NULL.  Sums over
+ * rows run in a fixed order. */
+disco_status_t disco_residual_norm_backward(const disco_rows_t* x, const disco_rows_t* f, const disco_residual_t* options,
+                                            const disco_rows_t* dh, const disco_rows_t* dy, disco_rows_t* dx,
+                                            disco_rows_t* df, disco_tensor_t* dpost_weight, disco_tensor_t* dgate,
+                                            disco_tensor_t* dnext_weight, void* workspace, size_t workspace_bytes,
+                                            hipStream_t stream);
+disco_status_t disco_residual_norm_workspace(const disco_rows_t* f, const disco_residual_t* options, size_t* bytes);
+
+enum { DISCO_GAIN_MEAN = 0, DISCO_GAIN_POWER = 1, DISCO_GAIN_ONE = 2 };
+typedef struct {
+    int32_t gain;            /* c of x: 1 - a (the state stays a mean), sqrt(1 - a^2) (its variance stays) or 1 */
+    int32_t reserved;        /* 0 */
+    const int32_t* lengths;  /* NULL, or [batch]: steps at and beyond it are not the item's (values outside
+                                0..tokens are taken as the nearer of the two) */
+} disco_recurrence_t;
+
+/* Gated linear recurrence along the tokens, for every channel by itself:
+ *   h_t = a_t h_(t-1) + c_t x_t,  a = sigmoid(gate),   y_t = h_t, or h_t sigmoid(out_gate_t),
+ * x, gate, out_gate (or NULL) and y of one size and type; y may be any of the inputs itself.
+ * state: h before the first token, [batch][channels] floats, or NULL (zeros); last:
+ * NULL, or h behind the last one, the same size; may be state itself, so that
+ * calls of one token or more go on where the last one ended.  Steps beyond an item's length leave its state as it
+ * is and give zeros; what the inputs hold there (NaN too) reaches no output.
+ * A gate of -inf starts anew from x, one of +inf holds the state, where x and h are finite.
+ * carries: NULL, or [batch][(tokens + 15) / 16][channels] floats, the states before
+ * every 16th token, which the backward call reads.  How the work is cut depends on
+ * the sizes alone, and parts are joined in a fixed order.  batch * channels < 2^31,
+ * channels up to 2^24.  options NULL: gain MEAN, no lengths.  Errors: INVALID_ARGUMENT,
+ * SHAPE, DTYPE, OUT_OF_MEMORY, DEVICE. */
+disco_status_t disco_gated_recurrence(const disco_rows_t* x, const disco_rows_t* gate, const disco_rows_t* out_gate,
+                                      const disco_recurrence_t* options, const float* state, disco_rows_t* y, float* last,
+                                      float* carries, void* workspace, size_t workspace_bytes, hipStream_t stream);
+
+/* Gradients of disco_gated_recurrence for dy and dlast (of `last`; NULL: zeros) from its
+ * inputs and carries: dx, dgate, dout_gate (x's sizes; each may be any of the inputs
+ * itself) and dstate (of `state`; may be dlast itself); any may be NULL. */
+disco_status_t disco_gated_recurrence_backward(const disco_rows_t* x, const disco_rows_t* gate, const disco_rows_t* out_gate,
+                                               const disco_recurrence_t* options, const float* carries,
+                                               const disco_rows_t* dy, const float* dlast, disco_rows_t* dx,
+                                               disco_rows_t* dgate, disco_rows_t* dout_gate, float* dstate,
+                                               void* workspace, size_t workspace_bytes, hipStream_t stream);
+/* Scratch bytes of either call.  Host only. */
+disco_status_t disco_gated_recurrence_workspace(const disco_rows_t* x, size_t* bytes);
+
 /* Kernel timing for measurement tools.  While enabled (on != 0), every
  * kernel the library launches from this process is bracketed by HIP events
  * recorded on the call's stream; disco_kernel_timing_read waits for the

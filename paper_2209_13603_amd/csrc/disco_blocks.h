@@ -1,0 +1,151 @@
+// disco_blocks.h -- arguments and launchers of the residual sum with its norms,
+// of dropout and of the gated recurrence, and the device parts that they share.
+#pragma once
+#include <hip/hip_runtime.h>
+
+#include <cstdint>
+
+#include "disco_heads.h"
+
+namespace disco {
+
+// A channel tensor [batch][tokens][channels] as the kernels see it.
+struct Rows {
+    void* p = nullptr;
+    int64_t sb = 0, st = 0;  // strides in elements
+};
+
+constexpr int kMaxNormChannels = 8192;  // of a row that is normed
+constexpr int kChunk = 8;                // entries of a row that a thread holds together
+
+// ---- dropout (disco_dropout.hip) ---------------------------------------------
+struct DropArgs {
+    uint32_t out = 0;  // an entry whose 16 bits lie below falls out; 65536: all
+    float factor = 1.0f;
+    uint32_t key0 = 0, key1 = 0;
+    uint64_t offset = 0;
+    const uint64_t* counter = nullptr;  // added to the offset
+};
+struct DropoutArgs {
+    Rows x, y;
+    DropArgs drop;
+    uint32_t batch = 0;
+    int64_t tokens = 0, channels = 0;
+    bool bf16 = false;
+    hipStream_t stream = nullptr;
+};
+hipError_t launch_dropout(const DropoutArgs& a);
+
+// ---- residual sum with its norms (disco_residual.hip) -------------------------
+struct ResidualArgs {
+    Rows x, f, h, y, dh, dy, dx, df;
+    // x's type; elements between batch items, 0 where all share one
+    const void *post_w = nullptr, *gate = nullptr, *next_w = nullptr;
+    int64_t post_sb = 0, gate_sb = 0, next_sb = 0;
+    void *dpost = nullptr, *dgate = nullptr, *dnext = nullptr;
+    DropArgs drop;
+    bool dropped = false, post = false, bf16 = false;
+    uint32_t batch = 0;
+    int64_t tokens = 0;
+    int32_t channels = 0;
+    float scale = 1.0f, eps = 0.0f, eps_up = 0.0f;  // eps_up: 2^192 eps
+    hipStream_t stream = nullptr;
+};
+hipError_t launch_residual(const ResidualArgs& a);
+size_t residual_grad_ws_bytes(const ResidualArgs& a);
+hipError_t launch_residual_grad(const ResidualArgs& a, float* ws);
+
+// ---- gated recurrence (disco_recur.hip, disco_recur_grad.hip) -----------------
+constexpr int kRun = 16;  // steps between two states that a forward call keeps for its gradients
+enum { kGainMean = 0, kGainPower = 1, kGainOne = 2 };
+struct RecurArgs {
+    Rows x, g, z, y;  // z: the output gate, or none
+    Rows dy, dx, dg, dz;
+    const int32_t* lengths = nullptr;
+    const float* state = nullptr;  // [batch][channels], or zeros
+    float* last = nullptr;         // [batch][channels]
+    float* carries = nullptr;      // [batch][runs][channels]: the state before each run
+    const float* dlast = nullptr;  // [batch][channels]
+    float* dstate = nullptr;       // [batch][channels]
+    uint32_t batch = 0;
+    int64_t steps = 0, channels = 0;
+    int gain = 0;
+    bool bf16 = false;
+    hipStream_t stream = nullptr;
+};
+size_t recur_ws_bytes(const RecurArgs& a);  // of either direction
+hipError_t launch_recur(const RecurArgs& a, float* ws);
+hipError_t launch_recur_grad(const RecurArgs& a, float* ws);
+
+// ---- device parts --------------------------------------------------------------
+// Philox4x32-10 (Salmon, Moraes, Dror, Shaw: Parallel random numbers: as easy as
+// 1, 2, 3; 2011): four words from a counter of four and a key of two.
+struct Words {
+    uint32_t w[4];
+};
+__device__ __forceinline__ Words philox(uint32_t a, uint32_t b, uint32_t c, uint32_t d, uint32_t k0, uint32_t k1) {
+#pragma unroll
+    for (int i = 0; i < 10; ++i) {
+        const uint64_t p = (uint64_t)a * 0xD2511F53u, q = (uint64_t)c * 0xCD9E8D57u;
+        a = (uint32_t)(q >> 32) ^ b ^ k0;
+        b = (uint32_t)q;
+        c = (uint32_t)(p >> 32) ^ d ^ k1;
+        d = (uint32_t)p;
+        k0 += 0x9E3779B9u;
+        k1 += 0xBB67AE85u;
+    }
+    return Words{{a, b, c, d}};
+}
+__device__ __forceinline__ uint64_t drop_offset(const DropArgs& d) { return d.offset + (d.counter ? *d.counter : 0); }
+// Which of the entries 8 chunk .. 8 chunk + 7 of a row stay, a bit each: 16 bits of
+// the generator an entry, so that one block of it serves a chunk of either type.
+__device__ __forceinline__ uint32_t kept(const DropArgs& d, uint64_t offset, uint32_t row, uint32_t chunk) {
+    const Words r = philox(chunk, row, (uint32_t)offset, (uint32_t)(offset >> 32), d.key0, d.key1);
+    uint32_t bits = 0;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        bits |= ((r.w[j] & 0xffffu) >= d.out ? 1u : 0u) << (2 * j);
+        bits |= ((r.w[j] >> 16) >= d.out ? 1u : 0u) << (2 * j + 1);
+    }
+    return bits;
+}
+
+// Eight entries of a row as they lie in memory.
+template <typename T>
+struct Raw {
+    T v[kChunk];
+};
+// Entries c .. c + 7 of a row of n, W at a time (n and the address are multiples
+// of W entries); `other` beyond n.
+template <typename T, int W>
+__device__ __forceinline__ Raw<T> load_raw(const T* row, int64_t c, int64_t n, float other = 0.0f) {
+    typedef T V __attribute__((ext_vector_type(W)));
+    Raw<T> r;
+#pragma unroll
+    for (int i = 0; i < kChunk; i += W) {
+        V v = (V)(T)other;
+        if (c + i < n) v = *(const V*)(row + c + i);
+#pragma unroll
+        for (int j = 0; j < W; ++j) r.v[i + j] = v[j];
+    }
+    return r;
+}
+template <typename T, int W>
+__device__ __forceinline__ void store_row(T* row, int64_t c, int64_t n, const float (&e)[kChunk]) {
+    typedef float F __attribute__((ext_vector_type(W)));
+    typedef T V __attribute__((ext_vector_type(W)));
+#pragma unroll
+    for (int i = 0; i < kChunk; i += W) {
+        F f;
+#pragma unroll
+        for (int j = 0; j < W; ++j) f[j] = e[i + j];
+        if (c + i < n) *(V*)(row + c + i) = __builtin_convertvector(f, V);
+    }
+}
+
+// Host: whether rows of a tensor are read or written w entries at a time.
+inline bool rows_fit(const Rows& t, int w, size_t elem) {
+    return !t.p || ((uintptr_t)t.p % (w * elem) == 0 && t.sb % w == 0 && t.st % w == 0);
+}
+
+}  // namespace disco

@@ -1,0 +1,72 @@
+// disco_dropout.hip -- dropout by a counter-based generator.
+//
+//   y = x factor where an entry's 16 bits are at least `out`, 0 elsewhere,
+//   factor = 65536 / (65536 - out),
+//
+// the bits of entry c of row r being half c % 8 of Philox4x32-10 at the counter
+// (c / 8, r, offset): the mask is a function of seed, offset and place, is never
+// stored, and the gradient is the same call on dy.  Sixteen bits an entry instead
+// of 32 halve the generator's work; the factor is that of the probability as it is
+// taken, so the expectation stays exact.
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+#include <cstdint>
+
+#include "disco_blocks.h"
+#include "disco_internal.h"
+
+namespace disco {
+
+namespace {
+
+constexpr int kThreads = 256;
+
+struct Shape {
+    Divisor chunks, tokens;  // of a row; rows of a batch item
+    uint32_t all;            // chunks of all rows
+};
+
+template <typename T, int W>
+__global__ __launch_bounds__(kThreads) void k_dropout(DropoutArgs a, Shape s) {
+    const uint32_t i = group_index() * kThreads + threadIdx.x;
+    if (i >= s.all) return;
+    const uint32_t row = s.chunks.quotient(i), chunk = i - row * s.chunks.d;
+    const uint32_t b = s.tokens.quotient(row), tok = row - b * s.tokens.d;
+    const int64_t c = (int64_t)chunk * kChunk;
+    const Raw<T> x = load_raw<T, W>((const T*)a.x.p + b * a.x.sb + tok * a.x.st, c, a.channels);
+    const uint32_t keep = kept(a.drop, drop_offset(a.drop), row, chunk);
+    float e[kChunk];
+#pragma unroll
+    for (int j = 0; j < kChunk; ++j) e[j] = keep >> j & 1 ? (float)x.v[j] * a.drop.factor : 0.0f;
+    store_row<T, W>((T*)a.y.p + b * a.y.sb + tok * a.y.st, c, a.channels, e);
+}
+
+template <typename T, int W>
+hipError_t launch(const DropoutArgs& a, const Shape& s) {
+    hipLaunchKernelGGL((k_dropout<T, W>), grid_dim((s.all + kThreads - 1) / kThreads), dim3(kThreads), 0, a.stream, a, s);
+    return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_dropout(const DropoutArgs& a) {
+    const int64_t chunks = (a.channels + kChunk - 1) / kChunk;
+    Shape s;
+    s.chunks = divisor((uint32_t)chunks);
+    s.tokens = divisor((uint32_t)a.tokens);
+    s.all = (uint32_t)(chunks * a.batch * a.tokens);
+    const size_t e = a.bf16 ? 2 : 4;
+    int w = a.bf16 ? 8 : 4;
+    while (w > 1 && (a.channels % w || !rows_fit(a.x, w, e) || !rows_fit(a.y, w, e))) w /= 2;
+    const int tk = timing_begin("dropout", a.stream);
+    hipError_t err;
+    if (a.bf16)
+        err = w == 8 ? launch<__bf16, 8>(a, s) : w == 4 ? launch<__bf16, 4>(a, s) : w == 2 ? launch<__bf16, 2>(a, s) : launch<__bf16, 1>(a, s);
+    else
+        err = w == 4 ? launch<float, 4>(a, s) : w == 2 ? launch<float, 2>(a, s) : launch<float, 1>(a, s);
+    timing_end(tk, a.stream);
+    return err;
+}
+
+}  // namespace disco

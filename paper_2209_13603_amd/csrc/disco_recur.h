@@ -1,0 +1,377 @@
+// disco_recur.h -- parts shared by the kernels of the gated recurrence and of its
+// gradients.
+//
+//   h_t = a_t h_(t-1) + c_t x_t,  a = sigmoid(g),  c = 1 - a (mean), sqrt(1 - a^2)
+//   (power) or 1 (one).
+//
+// A gate is held as q: |q| is the smaller of a and 1 - a, its sign bit is set where
+// that is a.  A state multiplied by an a near 1 is taken as h - (1 - a) h, so
+// that 1 - a keeps all its bits however long the memory is.
+//
+// A thread holds a run of 16 steps of V channels.  The map of states over some steps
+// is h -> A h + B, and a run's is joined with the others' without knowing the state
+// before it.  A is held as a gate is: over a long memory the products that
+// round near 1 alike would drift (gates of 12, 40000 steps: 6e-5; so 1e-7).
+#pragma once
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+#include <cstdint>
+#include <type_traits>
+
+#include "disco_blocks.h"
+
+namespace disco {
+
+constexpr int kRecurThreads = 256;
+constexpr int kRecurBlock = 64;  // channels of a workgroup that scans along time
+constexpr int kMaxSplits = 64;
+
+constexpr int kRecurChannels = 2;  // of a thread
+
+// How a call is cut.  scan: workgroups of 64 channels whose threads hold
+// consecutive runs and join their maps, `splits` of them share the time axis;
+// otherwise a thread walks all runs of its V channels by itself.
+struct RecurCut {
+    uint32_t columns;   // groups of V channels
+    uint32_t blocks;    // of 64 channels (scan)
+    uint32_t groups;    // workgroups
+    int32_t splits, tiles;  // tiles of all runs; a split takes every tiles / splits
+    Divisor by_columns;
+    float* maps;   // [splits][batch][channels][2]
+    float* entry;  // [batch][channels]: the state that the call is given, which its result may overwrite
+};
+
+__device__ __forceinline__ float gate_of(float g) {
+    const float e = __builtin_amdgcn_exp2f(-1.44269504f * fabsf(g));
+    const float q = e * __builtin_amdgcn_rcpf(1.0f + e);
+    return __uint_as_float(__float_as_uint(q) | (__float_as_uint(g) & 0x80000000u));
+}
+__device__ __forceinline__ bool closed(float q) { return __float_as_int(q) < 0; }  // a is the smaller
+__device__ __forceinline__ float decay(float h, float q) {
+    const float s = fabsf(q);
+    return closed(q) ? s * h : fmaf(-s, h, h);
+}
+// A product A of a's step by step, and 1 - A as a sum of what each step takes.
+struct Product {
+    float a = 1.0f, rest = 0.0f;
+    __device__ __forceinline__ void take(float q) {
+        const float s = fabsf(q), u = s * a, v = fmaf(-s, a, a);
+        a = closed(q) ? u : v;
+        rest += closed(q) ? v : u;
+    }
+    __device__ __forceinline__ float gate() const { return a < 0.5f ? -a : rest; }
+};
+// The product of two such.
+__device__ __forceinline__ float joined(float p, float q) {
+    const float s = fabsf(p), r = fabsf(q);
+    if (!closed(p) && !closed(q)) {
+        const float rest = fmaf(r, 1.0f - s, s);
+        return rest <= 0.5f ? rest : rest - 1.0f;
+    }
+    return -((closed(p) ? s : 1.0f - s) * (closed(q) ? r : 1.0f - r));
+}
+template <int GAIN>
+__device__ __forceinline__ float gain_of(float q) {
+    const float s = fabsf(q);
+    if (GAIN == kGainMean) return closed(q) ? 1.0f - s : s;
+    if (GAIN == kGainPower) return __builtin_amdgcn_sqrtf(closed(q) ? fmaf(-s, s, 1.0f) : s * (2.0f - s));
+    return 1.0f;
+}
+template <int GAIN>
+__device__ __forceinline__ float advance(float h, float q, float x) {
+    if (GAIN == kGainMean) {  // the one of h and x that weighs more, and the other's share
+        const float s = fabsf(q), p = closed(q) ? x : h, o = closed(q) ? h : x;
+        return fmaf(s, o, fmaf(-s, p, p));
+    }
+    if (GAIN == kGainPower) return fmaf(gain_of<GAIN>(q), x, decay(h, q));
+    return decay(h, q) + x;
+}
+__device__ __forceinline__ float sigmoid(float z) {
+    const float q = gate_of(z), s = fabsf(q);
+    return closed(q) ? s : 1.0f - s;
+}
+
+// V entries of V neighbouring channels.
+template <typename T, int V>
+struct Part {
+    T v[V];
+};
+// Channels c .. c + V - 1 of a row of n, in one load where WIDE.
+template <typename T, int V, bool WIDE>
+__device__ __forceinline__ Part<T, V> load_part(const T* p, int64_t c, int64_t n) {
+    typedef T Vec __attribute__((ext_vector_type(V)));
+    Part<T, V> r;
+    if constexpr (WIDE) {
+        const Vec v = *(const Vec*)p;
+#pragma unroll
+        for (int j = 0; j < V; ++j) r.v[j] = v[j];
+    } else {
+#pragma unroll
+        for (int j = 0; j < V; ++j) r.v[j] = c + j < n ? p[j] : (T)0.0f;
+    }
+    return r;
+}
+template <typename T, int V, bool WIDE>
+__device__ __forceinline__ void store_part(T* p, int64_t c, int64_t n, const float (&e)[V]) {
+    typedef T Vec __attribute__((ext_vector_type(V)));
+    if constexpr (WIDE) {
+        Vec v;
+#pragma unroll
+        for (int j = 0; j < V; ++j) v[j] = (T)e[j];
+        *(Vec*)p = v;
+    } else {
+#pragma unroll
+        for (int j = 0; j < V; ++j)
+            if (c + j < n) p[j] = (T)e[j];
+    }
+}
+
+// The run of a thread: 16 steps from s0 on, of which the item has `left`.  Loads
+// stop at the item's last step (an item without any reads its first, which memory
+// has), so that they need no branches; what lies beyond is then taken
+// out, in the few runs that have such steps.
+struct Run {
+    int64_t first;  // step that the loads begin at
+    int left;       // steps of the run that the item has
+    int steps;      // steps of the run that the tensors have
+    __device__ __forceinline__ Run(const RecurArgs& a, int64_t s0, int64_t count) {
+        const int64_t n = count - s0, m = a.steps - s0;
+        left = n < 0 ? 0 : n > kRun ? kRun : (int)n;
+        steps = m < 0 ? 0 : m > kRun ? kRun : (int)m;
+        first = left > 0 ? s0 : count > 0 ? count - 1 : 0;
+    }
+    __device__ __forceinline__ bool whole() const { return __all(left == kRun); }
+    template <typename T, int V, bool WIDE>
+    __device__ __forceinline__ void load(const T* p, int64_t st, int64_t c, int64_t n, Part<T, V> (&v)[kRun]) const {
+        p += first * st;
+        if (whole()) {
+#pragma unroll
+            for (int i = 0; i < kRun; ++i, p += st) v[i] = load_part<T, V, WIDE>(p, c, n);
+        } else {
+#pragma unroll
+            for (int i = 0; i < kRun; ++i) {
+                v[i] = load_part<T, V, WIDE>(p, c, n);
+                p += i + 1 < left ? st : 0;
+            }
+#pragma unroll
+            for (int i = 0; i < kRun; ++i)
+#pragma unroll
+                for (int j = 0; j < V; ++j) v[i].v[j] = i < left ? v[i].v[j] : (T)0.0f;
+        }
+    }
+};
+
+// The gates of steps that the item has not: they leave a state as it is.
+template <int V>
+__device__ __forceinline__ void take_out(const Run& r, float (&q)[kRun][V]) {
+    if (r.whole()) return;
+#pragma unroll
+    for (int i = 0; i < kRun; ++i)
+#pragma unroll
+        for (int j = 0; j < V; ++j) q[i][j] = i < r.left ? q[i][j] : 0.0f;
+}
+
+// Where a thread works: its channels, and the runs it takes.
+template <int V, bool SCAN>
+struct Lane {
+    static constexpr int kLanes = kRecurBlock / V;                      // threads of a step (scan)
+    static constexpr int kSlots = SCAN ? kRecurThreads / kLanes : 1;    // runs of a tile
+    static constexpr int kInWave = 64 / kLanes;                         // of them in a wave
+    static constexpr int kWaves = kRecurThreads / 64;
+    uint32_t b;
+    int64_t c;       // first channel
+    int slot, split;
+    bool live;       // has channels
+    int64_t count;   // steps of this item
+    int t0, t1;      // tiles
+    __device__ __forceinline__ Lane(const RecurArgs& a, const RecurCut& cut, int first_split = 0) {
+        if constexpr (SCAN) {
+            uint32_t id = group_index();
+            const uint32_t block = id % cut.blocks;
+            id /= cut.blocks;
+            b = id % a.batch;
+            split = first_split + (int)(id / a.batch);
+            slot = threadIdx.x / kLanes;
+            const uint32_t column = block * kLanes + threadIdx.x % kLanes;
+            live = column < cut.columns && split < cut.splits;
+            c = (int64_t)column * V;
+            t0 = (int)((int64_t)cut.tiles * split / cut.splits);
+            t1 = split < cut.splits ? (int)((int64_t)cut.tiles * (split + 1) / cut.splits) : t0;
+        } else {
+            const uint32_t id = group_index() * kRecurThreads + threadIdx.x;
+            live = id < cut.columns * a.batch;
+            b = cut.by_columns.quotient(live ? id : 0);
+            c = (int64_t)((live ? id : 0) - b * cut.columns) * V;
+            slot = split = 0;
+            t0 = 0;
+            t1 = live ? cut.tiles : 0;
+        }
+        if (!live) b = 0, c = 0;
+        count = a.steps;
+        if (a.lengths) {
+            const int64_t n = a.lengths[b];
+            count = n < 0 ? 0 : n < count ? n : count;
+        }
+    }
+    template <typename T>
+    __device__ __forceinline__ T* at(const Rows& r) const {
+        return (T*)r.p + b * r.sb + c;
+    }
+    // The place of this thread's channels in a [batch][channels] array.
+    __device__ __forceinline__ int64_t state_at(const RecurArgs& a) const { return (int64_t)b * a.channels + c; }
+};
+
+// fp32 values of a thread's channels (never wide: channels may be odd).
+template <int V>
+__device__ __forceinline__ void load_state(const float* p, int64_t at, int64_t c, int64_t n, bool live, float (&h)[V]) {
+#pragma unroll
+    for (int j = 0; j < V; ++j) h[j] = p && live && c + j < n ? p[at + j] : 0.0f;
+}
+template <int V>
+__device__ __forceinline__ void store_state(float* p, int64_t at, int64_t c, int64_t n, bool live, const float (&h)[V]) {
+#pragma unroll
+    for (int j = 0; j < V; ++j)
+        if (live && c + j < n) p[at + j] = h[j];
+}
+
+// Joins the maps of a workgroup's runs: gives each thread the state before
+// its own (after its own, looking backwards) from that before the tile, `h`, and leaves in h the
+// state behind the tile.  One barrier a tile; the buffers take turns.
+template <int V, bool SCAN, bool BACK>
+struct JoinMaps {
+    typedef Lane<V, SCAN> L;
+    __device__ __forceinline__ static void run(float (&A)[V], float (&B)[V], float (&h)[V], float (&mine)[V],
+                                               float (*maps)[L::kWaves][L::kLanes][2 * V], int turn) {
+        const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, col = threadIdx.x % L::kLanes;
+        const int at = lane / L::kLanes;  // place in the wave
+        const int order = BACK ? L::kInWave - 1 - at : at;
+#pragma unroll
+        for (int d = 1; d < L::kInWave; d *= 2) {
+#pragma unroll
+            for (int j = 0; j < V; ++j) {
+                const int from = BACK ? lane + d * L::kLanes : lane - d * L::kLanes;
+                const float a = __shfl(A[j], from), b = __shfl(B[j], from);
+                if (order >= d) {
+                    B[j] += decay(b, A[j]);
+                    A[j] = joined(A[j], a);
+                }
+            }
+        }
+        if (order == L::kInWave - 1) {
+#pragma unroll
+            for (int j = 0; j < V; ++j) {
+                maps[turn][wave][col][j] = A[j];
+                maps[turn][wave][col][V + j] = B[j];
+            }
+        }
+        // of the runs before this one in the wave
+        float ea[V], eb[V];
+#pragma unroll
+        for (int j = 0; j < V; ++j) {
+            const int from = BACK ? lane + L::kLanes : lane - L::kLanes;
+            const float a = __shfl(A[j], from), b = __shfl(B[j], from);
+            ea[j] = order ? a : 0.0f;
+            eb[j] = order ? b : 0.0f;
+        }
+        __syncthreads();
+#pragma unroll
+        for (int k = 0; k < L::kWaves; ++k) {
+            const int w = BACK ? L::kWaves - 1 - k : k;
+#pragma unroll
+            for (int j = 0; j < V; ++j) {
+                if (w == wave) mine[j] = decay(h[j], ea[j]) + eb[j];
+                h[j] = decay(h[j], maps[turn][w][col][j]) + maps[turn][w][col][V + j];
+            }
+        }
+    }
+};
+
+// Where a call has splits, the first kernel keeps the given state for the second.
+template <int V, bool SCAN>
+__device__ __forceinline__ void keep_entry(const Lane<V, SCAN>& ln, const RecurArgs& a, const RecurCut& cut, const float* given) {
+    float h[V];
+    load_state(given, ln.state_at(a), ln.c, a.channels, ln.live, h);
+    store_state(cut.entry, ln.state_at(a), ln.c, a.channels, ln.live, h);
+}
+
+// The state before split `split` (behind it, looking backwards) from that at the
+// ends of the series.
+template <int V, bool BACK>
+__device__ __forceinline__ void through_splits(const RecurArgs& a, const RecurCut& cut, int split, int64_t at, int64_t c,
+                                               bool live, float (&h)[V]) {
+    const int64_t all = (int64_t)a.batch * a.channels;
+    const int n = BACK ? cut.splits - 1 - split : split;
+#pragma unroll 4
+    for (int i = 0; i < n; ++i) {
+        const int s = BACK ? cut.splits - 1 - i : i;
+#pragma unroll
+        for (int j = 0; j < V; ++j)
+            if (live && c + j < a.channels) {
+                const float* m = cut.maps + 2 * (s * all + at + j);
+                h[j] = decay(h[j], m[0]) + m[1];
+            }
+    }
+}
+
+inline bool recur_wide(const RecurArgs& a) {
+    constexpr int v = kRecurChannels;
+    const size_t e = a.bf16 ? 2 : 4;
+    if (a.channels % v) return false;
+    for (const Rows* t : {&a.x, &a.g, &a.z, &a.y, &a.dy, &a.dx, &a.dg, &a.dz})
+        if (!rows_fit(*t, v, e)) return false;
+    return true;
+}
+
+// Whether threads walk alone: where there are enough of them, or few steps.
+constexpr uint32_t kWalkThreads = 65536;
+inline bool walks(const RecurArgs& a) {
+    constexpr int v = kRecurChannels;
+    return a.steps <= 2 * kRun || (uint64_t)a.batch * ((a.channels + v - 1) / v) >= kWalkThreads;
+}
+constexpr uint32_t kScanGroups = 1024;  // workgroups that fill the card
+inline RecurCut recur_cut(const RecurArgs& a) {
+    constexpr int v = kRecurChannels;
+    RecurCut c{};
+    c.columns = (uint32_t)((a.channels + v - 1) / v);
+    c.by_columns = divisor(c.columns);
+    const int64_t runs = (a.steps + kRun - 1) / kRun;
+    c.splits = 1;
+    if (walks(a)) {
+        c.tiles = (int32_t)runs;
+        c.groups = (uint32_t)(((uint64_t)c.columns * a.batch + kRecurThreads - 1) / kRecurThreads);
+        return c;
+    }
+    const int slots = kRecurThreads * v / kRecurBlock;
+    c.tiles = (int32_t)((runs + slots - 1) / slots);
+    c.blocks = (uint32_t)((a.channels + kRecurBlock - 1) / kRecurBlock);
+    const uint64_t base = (uint64_t)c.blocks * a.batch;
+    c.splits = (int32_t)std::max<uint64_t>(1, std::min<uint64_t>({kScanGroups / base, (uint64_t)c.tiles / 2, kMaxSplits}));
+    c.groups = (uint32_t)(base * c.splits);
+    return c;
+}
+
+// Calls f with the storage type, whether loads are wide, and whether there is an
+// output gate.
+template <typename F>
+hipError_t recur_dispatch(const RecurArgs& a, F&& f) {
+    auto gated = [&](auto t, auto wide) {
+        return a.z.p ? f(t, wide, std::true_type{}) : f(t, wide, std::false_type{});
+    };
+    auto type = [&](auto t) { return recur_wide(a) ? gated(t, std::true_type{}) : gated(t, std::false_type{}); };
+    return a.bf16 ? type(__bf16{}) : type(float{});
+}
+
+inline void recur_ws(RecurCut* cut, const RecurArgs& a, float* ws) {
+    cut->maps = ws;
+    cut->entry = ws ? ws + (int64_t)cut->splits * a.batch * a.channels * 2 : nullptr;
+}
+
+template <typename F>
+hipError_t by_gain(int gain, F&& f) {
+    if (gain == kGainMean) return f(std::integral_constant<int, kGainMean>{});
+    if (gain == kGainPower) return f(std::integral_constant<int, kGainPower>{});
+    return f(std::integral_constant<int, kGainOne>{});
+}
+
+}  // namespace disco

@@ -61,7 +61,9 @@ EXPORTS = ("disco_plan_create", "disco_plan_destroy", "disco_plan_query", "disco
            "disco_status_string", "disco_last_error", "disco_debug_bounds_violations",
            "disco_norm_rotate", "disco_norm_rotate_backward", "disco_norm_rotate_workspace",
            "disco_cross_attention", "disco_cross_attention_backward", "disco_cross_attention_workspace",
-           "disco_gradient_clip", "disco_gradient_clip_workspace")
+           "disco_gradient_clip", "disco_gradient_clip_workspace", "disco_dropout", "disco_residual_norm",
+           "disco_residual_norm_backward", "disco_residual_norm_workspace", "disco_gated_recurrence",
+           "disco_gated_recurrence_backward", "disco_gated_recurrence_workspace")
 
 
 def debug_bounds_violations() -> int:
@@ -107,6 +109,32 @@ class AttentionArgs(ctypes.Structure):
     """disco_attention_t."""
     _fields_ = [("scale", ctypes.c_double), ("key_bias", ctypes.c_void_p), ("bias_stride_batch", ctypes.c_int64),
                 ("key_lengths", ctypes.c_void_p)]
+
+
+class Rows(ctypes.Structure):
+    """disco_rows_t: a channel tensor [batch, tokens, channels] with its strides."""
+    _fields_ = [("data", ctypes.c_void_p), ("dtype", ctypes.c_int32), ("reserved", ctypes.c_int32),
+                ("batch", ctypes.c_int64), ("tokens", ctypes.c_int64), ("channels", ctypes.c_int64),
+                ("stride_batch", ctypes.c_int64), ("stride_token", ctypes.c_int64)]
+
+
+class DropoutArgs(ctypes.Structure):
+    """disco_dropout_t."""
+    _fields_ = [("p", ctypes.c_double), ("seed", ctypes.c_uint64), ("offset", ctypes.c_uint64),
+                ("counter", ctypes.c_void_p)]
+
+
+class ResidualArgs(ctypes.Structure):
+    """disco_residual_t."""
+    _fields_ = [("scale", ctypes.c_double), ("eps", ctypes.c_double), ("post_norm", ctypes.c_int32),
+                ("reserved", ctypes.c_int32), ("post_weight", ctypes.POINTER(Tensor)),
+                ("gate", ctypes.POINTER(Tensor)), ("next_weight", ctypes.POINTER(Tensor)),
+                ("dropout", ctypes.POINTER(DropoutArgs))]
+
+
+class RecurrenceArgs(ctypes.Structure):
+    """disco_recurrence_t."""
+    _fields_ = [("gain", ctypes.c_int32), ("reserved", ctypes.c_int32), ("lengths", ctypes.c_void_p)]
 
 
 class PlanInfo(ctypes.Structure):
@@ -196,7 +224,7 @@ def library(path: str = None) -> ctypes.CDLL:
     lib.disco_last_error.argtypes = []
     lib.disco_last_error.restype = ctypes.c_char_p
     V, Z, I32, S = ctypes.c_void_p, ctypes.c_size_t, ctypes.c_int32, P(ctypes.c_size_t)
-    H, T, R, A = P(Heads), P(Tensor), P(RotationArgs), P(AttentionArgs)
+    H, T, R, A, W = P(Heads), P(Tensor), P(RotationArgs), P(AttentionArgs), P(Rows)
     token_calls = {
         "disco_norm_rotate": [H, I32, T, ctypes.c_double, R, H, V],
         "disco_norm_rotate_backward": [H, I32, T, ctypes.c_double, R, H, H, T, V, Z, V],
@@ -207,6 +235,13 @@ def library(path: str = None) -> ctypes.CDLL:
         # the tensor arrays of many gradients come as addresses
         "disco_gradient_clip": [I32, V, V, ctypes.c_double, ctypes.c_double, V, V, Z, V],
         "disco_gradient_clip_workspace": [I32, V, S],
+        "disco_dropout": [W, P(DropoutArgs), W, V],
+        "disco_residual_norm": [W, W, P(ResidualArgs), W, W, V],
+        "disco_residual_norm_backward": [W, W, P(ResidualArgs), W, W, W, W, T, T, T, V, Z, V],
+        "disco_residual_norm_workspace": [W, P(ResidualArgs), S],
+        "disco_gated_recurrence": [W, W, W, P(RecurrenceArgs), V, W, V, V, V, Z, V],
+        "disco_gated_recurrence_backward": [W, W, W, P(RecurrenceArgs), V, W, V, W, W, W, V, V, Z, V],
+        "disco_gated_recurrence_workspace": [W, S],
     }
     for name, args in token_calls.items():
         getattr(lib, name).argtypes = args
