@@ -97,17 +97,14 @@ __device__ __forceinline__ Words philox(uint32_t a, uint32_t b, uint32_t c, uint
     return Words{{a, b, c, d}};
 }
 __device__ __forceinline__ uint64_t drop_offset(const DropArgs& d) { return d.offset + (d.counter ? *d.counter : 0); }
-// Which of the entries 8 chunk .. 8 chunk + 7 of a row stay, a bit each: 16 bits of
-// the generator an entry, so that one block of it serves a chunk of either type.
-__device__ __forceinline__ uint32_t kept(const DropArgs& d, uint64_t offset, uint32_t row, uint32_t chunk) {
-    const Words r = philox(chunk, row, (uint32_t)offset, (uint32_t)(offset >> 32), d.key0, d.key1);
-    uint32_t bits = 0;
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-        bits |= ((r.w[j] & 0xffffu) >= d.out ? 1u : 0u) << (2 * j);
-        bits |= ((r.w[j] >> 16) >= d.out ? 1u : 0u) << (2 * j + 1);
-    }
-    return bits;
+// The 16 bits of the entries 8 chunk .. 8 chunk + 7 of a row: one block of the
+// generator serves a chunk of either type.
+__device__ __forceinline__ Words drop_words(const DropArgs& d, uint64_t offset, uint32_t row, uint32_t chunk) {
+    return philox(chunk, row, (uint32_t)offset, (uint32_t)(offset >> 32), d.key0, d.key1);
+}
+// Whether entry i of the chunk stays.
+__device__ __forceinline__ bool stays(const Words& r, int i, uint32_t out) {
+    return (i % 2 ? r.w[i / 2] >> 16 : r.w[i / 2] & 0xffffu) >= out;
 }
 
 // Eight entries of a row as they lie in memory.
@@ -115,23 +112,37 @@ template <typename T>
 struct Raw {
     T v[kChunk];
 };
-// Entries c .. c + 7 of a row of n, W at a time (n and the address are multiples
-// of W entries); `other` beyond n.
+// Keeps the eight entries as they lie: without it what a loop does not change is
+// converted before it, into twice the registers.
+template <typename T>
+__device__ __forceinline__ void stay_raw(Raw<T>& r) {
+    if constexpr (sizeof(T) == 2) {
+        struct Words4 {
+            uint32_t w[4];
+        };
+        Words4 u = __builtin_bit_cast(Words4, r);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) asm("" : "+v"(u.w[i]));
+        r = __builtin_bit_cast(Raw<T>, u);
+    }
+}
+// The first eight entries at p, of which `left` are there (perhaps none), W at a time: left and
+// the address are multiples of W entries.  Zeros beyond.
 template <typename T, int W>
-__device__ __forceinline__ Raw<T> load_raw(const T* row, int64_t c, int64_t n, float other = 0.0f) {
+__device__ __forceinline__ Raw<T> load_raw(const T* p, int left) {
     typedef T V __attribute__((ext_vector_type(W)));
     Raw<T> r;
 #pragma unroll
     for (int i = 0; i < kChunk; i += W) {
-        V v = (V)(T)other;
-        if (c + i < n) v = *(const V*)(row + c + i);
+        V v = (V)(T)0.0f;
+        if (i < left) v = *(const V*)(p + i);
 #pragma unroll
         for (int j = 0; j < W; ++j) r.v[i + j] = v[j];
     }
     return r;
 }
 template <typename T, int W>
-__device__ __forceinline__ void store_row(T* row, int64_t c, int64_t n, const float (&e)[kChunk]) {
+__device__ __forceinline__ void store_raw(T* p, int left, const float (&e)[kChunk]) {
     typedef float F __attribute__((ext_vector_type(W)));
     typedef T V __attribute__((ext_vector_type(W)));
 #pragma unroll
@@ -139,8 +150,32 @@ __device__ __forceinline__ void store_row(T* row, int64_t c, int64_t n, const fl
         F f;
 #pragma unroll
         for (int j = 0; j < W; ++j) f[j] = e[i + j];
-        if (c + i < n) *(V*)(row + c + i) = __builtin_convertvector(f, V);
+        if (i < left) *(V*)(p + i) = __builtin_convertvector(f, V);
     }
+}
+
+// Sum over the 2^k neighbouring lanes of a row, in each of them: exchanges within
+// quads, eights, sixteens and the wave's halves on the vector unit (through LDS, as
+// shuffles go, a row's three sums took longer than its loads).
+template <int CTRL>
+__device__ __forceinline__ float dpp_add(float v) {
+    return v + __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), CTRL, 0xf, 0xf, false));
+}
+__device__ __forceinline__ float lanes_sum(float v, int lanes) {
+    asm("" : "+s"(lanes));  // (compared here: kept over a loop the conditions spill)
+    if (lanes >= 2) v = dpp_add<0xB1>(v);    // lane ^ 1
+    if (lanes >= 4) v = dpp_add<0x4E>(v);    // lane ^ 2
+    if (lanes >= 8) v = dpp_add<0x141>(v);   // mirrored within eight
+    if (lanes >= 16) v = dpp_add<0x140>(v);  // mirrored within sixteen
+    if (lanes >= 32) {
+        const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+        v = __uint_as_float(r[0]) + __uint_as_float(r[1]);
+    }
+    if (lanes >= 64) {
+        const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+        v = __uint_as_float(r[0]) + __uint_as_float(r[1]);
+    }
+    return v;
 }
 
 // Host: whether rows of a tensor are read or written w entries at a time.

@@ -34,12 +34,13 @@ __global__ __launch_bounds__(kThreads) void k_dropout(DropoutArgs a, Shape s) {
     const uint32_t row = s.chunks.quotient(i), chunk = i - row * s.chunks.d;
     const uint32_t b = s.tokens.quotient(row), tok = row - b * s.tokens.d;
     const int64_t c = (int64_t)chunk * kChunk;
-    const Raw<T> x = load_raw<T, W>((const T*)a.x.p + b * a.x.sb + tok * a.x.st, c, a.channels);
-    const uint32_t keep = kept(a.drop, drop_offset(a.drop), row, chunk);
+    const int left = (int)min((int64_t)kChunk, a.channels - c);
+    const Raw<T> x = load_raw<T, W>((const T*)a.x.p + b * a.x.sb + tok * a.x.st + c, left);
+    const Words r = drop_words(a.drop, drop_offset(a.drop), row, chunk);
     float e[kChunk];
 #pragma unroll
-    for (int j = 0; j < kChunk; ++j) e[j] = keep >> j & 1 ? (float)x.v[j] * a.drop.factor : 0.0f;
-    store_row<T, W>((T*)a.y.p + b * a.y.sb + tok * a.y.st, c, a.channels, e);
+    for (int j = 0; j < kChunk; ++j) e[j] = stays(r, j, a.drop.out) ? (float)x.v[j] * a.drop.factor : 0.0f;
+    store_raw<T, W>((T*)a.y.p + b * a.y.sb + tok * a.y.st + c, left, e);
 }
 
 template <typename T, int W>

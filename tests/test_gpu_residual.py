@@ -166,6 +166,13 @@ def test_rows_whose_squares_leave_fp32(factor):
     assert rel(y, want[1]) <= 2e-6
 
 
+def test_weights_without_an_eps():
+    """Slots of a workgroup that have no row bring nothing to the sums."""
+    for shape in ((1, 1, 40), (1, 7, 96), (3, 5, 24)):
+        x, f, dh, dy, w = _inputs(*shape, "fp32")
+        _all(x, f, dh, dy, dict(post_norm=True, eps=0.0, **w), "fp32")
+
+
 def test_what_is_not_finite_stays_in_its_row():
     import torch
     from paper_2209_13603_amd import blocks
