@@ -107,38 +107,66 @@ __device__ __forceinline__ bool stays(const Words& r, int i, uint32_t out) {
     return (i % 2 ? r.w[i / 2] >> 16 : r.w[i / 2] & 0xffffu) >= out;
 }
 
-// Eight entries of a row as they lie in memory.
+// Eight entries of a row as they lie in memory: bf16 two in a register (as single
+// values, once branches meet, they take one each).
 template <typename T>
-struct Raw {
-    T v[kChunk];
-};
-// Keeps the eight entries as they lie: without it what a loop does not change is
-// converted before it, into twice the registers.
-template <typename T>
-__device__ __forceinline__ void stay_raw(Raw<T>& r) {
-    if constexpr (sizeof(T) == 2) {
-        struct Words4 {
-            uint32_t w[4];
-        };
-        Words4 u = __builtin_bit_cast(Words4, r);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) asm("" : "+v"(u.w[i]));
-        r = __builtin_bit_cast(Raw<T>, u);
+struct Raw;
+template <>
+struct Raw<__bf16> {
+    uint32_t w[kChunk / 2];
+    __device__ __forceinline__ float at(int i) const {
+        return __uint_as_float(i % 2 ? w[i / 2] & 0xffff0000u : w[i / 2] << 16);
     }
-}
+    __device__ __forceinline__ void fill(float v) {
+#pragma unroll
+        for (int i = 0; i < kChunk / 2; ++i) w[i] = (__float_as_uint(v) >> 16) * 0x10001u;
+    }
+    // A new value to the compiler: without it what a loop does not change is
+    // converted before it, into twice the registers.
+    __device__ __forceinline__ void anew() {
+#pragma unroll
+        for (int i = 0; i < kChunk / 2; ++i) asm("" : "+v"(w[i]));
+    }
+    // Entries i .. i + W - 1
+    template <int W>
+    __device__ __forceinline__ void load(int i, const __bf16* p) {
+        if constexpr (W == 1) {
+            const uint32_t v = *(const uint16_t*)p;
+            w[i / 2] = i % 2 ? (w[i / 2] & 0xffffu) | v << 16 : (w[i / 2] & 0xffff0000u) | v;
+        } else {
+            typedef uint32_t U __attribute__((ext_vector_type(W / 2)));
+            const U v = *(const U*)p;
+#pragma unroll
+            for (int j = 0; j < W / 2; ++j) w[i / 2 + j] = v[j];
+        }
+    }
+};
+template <>
+struct Raw<float> {
+    float w[kChunk];
+    __device__ __forceinline__ float at(int i) const { return w[i]; }
+    __device__ __forceinline__ void fill(float v) {
+#pragma unroll
+        for (int i = 0; i < kChunk; ++i) w[i] = v;
+    }
+    __device__ __forceinline__ void anew() {}
+    template <int W>
+    __device__ __forceinline__ void load(int i, const float* p) {
+        typedef float U __attribute__((ext_vector_type(W)));
+        const U v = *(const U*)p;
+#pragma unroll
+        for (int j = 0; j < W; ++j) w[i + j] = v[j];
+    }
+};
 // The first eight entries at p, of which `left` are there (perhaps none), W at a time: left and
 // the address are multiples of W entries.  Zeros beyond.
 template <typename T, int W>
 __device__ __forceinline__ Raw<T> load_raw(const T* p, int left) {
-    typedef T V __attribute__((ext_vector_type(W)));
     Raw<T> r;
+    r.fill(0.0f);
 #pragma unroll
-    for (int i = 0; i < kChunk; i += W) {
-        V v = (V)(T)0.0f;
-        if (i < left) v = *(const V*)(p + i);
-#pragma unroll
-        for (int j = 0; j < W; ++j) r.v[i + j] = v[j];
-    }
+    for (int i = 0; i < kChunk; i += W)
+        if (i < left) r.template load<W>(i, p + i);
     return r;
 }
 template <typename T, int W>

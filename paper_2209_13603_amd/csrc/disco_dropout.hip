@@ -39,7 +39,7 @@ __global__ __launch_bounds__(kThreads) void k_dropout(DropoutArgs a, Shape s) {
     const Words r = drop_words(a.drop, drop_offset(a.drop), row, chunk);
     float e[kChunk];
 #pragma unroll
-    for (int j = 0; j < kChunk; ++j) e[j] = stays(r, j, a.drop.out) ? (float)x.v[j] * a.drop.factor : 0.0f;
+    for (int j = 0; j < kChunk; ++j) e[j] = stays(r, j, a.drop.out) ? x.at(j) * a.drop.factor : 0.0f;
     store_raw<T, W>((T*)a.y.p + b * a.y.sb + tok * a.y.st + c, left, e);
 }
 

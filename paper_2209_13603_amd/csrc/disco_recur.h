@@ -23,11 +23,12 @@
 
 namespace disco {
 
-constexpr int kRecurThreads = 256;
+constexpr int kWalkBlock = 256;  // threads of a workgroup whose threads walk alone
+constexpr int kScanBlock = 512;  // of one that scans
 constexpr int kRecurBlock = 64;  // channels of a workgroup that scans along time
 constexpr int kMaxSplits = 64;
 
-constexpr int kRecurChannels = 2;  // of a thread
+constexpr int kRecurChannels = 2;  // of a thread: see Part
 
 // How a call is cut.  scan: workgroups of 64 channels whose threads hold
 // consecutive runs and join their maps, `splits` of them share the time axis;
@@ -60,6 +61,7 @@ struct Product {
         a = closed(q) ? u : v;
         rest += closed(q) ? v : u;
     }
+    // As a gate.
     __device__ __forceinline__ float gate() const { return a < 0.5f ? -a : rest; }
 };
 // The product of two such.
@@ -92,23 +94,41 @@ __device__ __forceinline__ float sigmoid(float z) {
     return closed(q) ? s : 1.0f - s;
 }
 
-// V entries of V neighbouring channels.
-template <typename T, int V>
-struct Part {
-    T v[V];
+// Two neighbouring channels as they lie: bf16 in one register (as single values, once
+// branches meet, they take one each).
+template <typename T>
+struct Part;
+template <>
+struct Part<__bf16> {
+    uint32_t u;
+    __device__ __forceinline__ float at(int j) const { return __uint_as_float(j ? u & 0xffff0000u : u << 16); }
+    __device__ __forceinline__ void clear_unless(bool in) { u = in ? u : 0u; }
+    // A new value to the compiler: what is converted is then converted again, instead of kept.
+    __device__ __forceinline__ void anew() { asm("" : "+v"(u)); }
 };
-// Channels c .. c + V - 1 of a row of n, in one load where WIDE.
-template <typename T, int V, bool WIDE>
-__device__ __forceinline__ Part<T, V> load_part(const T* p, int64_t c, int64_t n) {
-    typedef T Vec __attribute__((ext_vector_type(V)));
-    Part<T, V> r;
-    if constexpr (WIDE) {
-        const Vec v = *(const Vec*)p;
-#pragma unroll
-        for (int j = 0; j < V; ++j) r.v[j] = v[j];
+template <>
+struct Part<float> {
+    float v[2];
+    __device__ __forceinline__ float at(int j) const { return v[j]; }
+    __device__ __forceinline__ void clear_unless(bool in) { v[0] = in ? v[0] : 0.0f, v[1] = in ? v[1] : 0.0f; }
+    __device__ __forceinline__ void anew() {}
+};
+// Channels c, c + 1 of a row of n, in one load where WIDE.
+template <typename T, bool WIDE>
+__device__ __forceinline__ Part<T> load_part(const T* p, int64_t c, int64_t n) {
+    Part<T> r;
+    if constexpr (WIDE && sizeof(T) == 2) {
+        r.u = *(const uint32_t*)p;
+    } else if constexpr (WIDE) {
+        const float2 v = *(const float2*)p;
+        r.v[0] = v.x, r.v[1] = v.y;
+    } else if constexpr (sizeof(T) == 2) {
+        const uint16_t* q = (const uint16_t*)p;
+        r.u = c < n ? q[0] : 0u;
+        if (c + 1 < n) r.u |= (uint32_t)q[1] << 16;
     } else {
-#pragma unroll
-        for (int j = 0; j < V; ++j) r.v[j] = c + j < n ? p[j] : (T)0.0f;
+        r.v[0] = c < n ? p[0] : 0.0f;
+        r.v[1] = c + 1 < n ? p[1] : 0.0f;
     }
     return r;
 }
@@ -127,58 +147,96 @@ __device__ __forceinline__ void store_part(T* p, int64_t c, int64_t n, const flo
     }
 }
 
-// The run of a thread: 16 steps from s0 on, of which the item has `left`.  Loads
-// stop at the item's last step (an item without any reads its first, which memory
-// has), so that they need no branches; what lies beyond is then taken
-// out, in the few runs that have such steps.
+// The gates as new values: what is derived from them is then derived again, instead
+// of kept from one pass over a run to the next (conditions too, in scalar registers).
+template <int N, int V>
+__device__ __forceinline__ void anew(float (&q)[N][V]) {
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+#pragma unroll
+        for (int j = 0; j < V; ++j) asm("" : "+v"(q[i][j]));
+}
+
+// The next step's place.  (A new value each time: sums of the first place and multiples
+// of the stride, made ahead, take two registers a step.)
+template <typename T>
+__device__ __forceinline__ void move(T*& p, int64_t by) {
+    p += by;
+    asm("" : "+v"(p));
+}
+
+// The run of a thread: 16 steps from s0 on, of which the item has `left` and the
+// tensors `steps`.  Whole runs go without conditions; of the others a wave takes
+// the groups of four steps in which one of its threads has any.  Their loads stop at the item's last
+// step (an item without any reads its first, which memory has); what lies beyond is
+// taken out.
+constexpr int kGroup = 4;
 struct Run {
     int64_t first;  // step that the loads begin at
-    int left;       // steps of the run that the item has
-    int steps;      // steps of the run that the tensors have
+    int left, steps;
+    bool whole;     // of all the wave's threads
+    __device__ __forceinline__ Run() {}
     __device__ __forceinline__ Run(const RecurArgs& a, int64_t s0, int64_t count) {
         const int64_t n = count - s0, m = a.steps - s0;
         left = n < 0 ? 0 : n > kRun ? kRun : (int)n;
         steps = m < 0 ? 0 : m > kRun ? kRun : (int)m;
         first = left > 0 ? s0 : count > 0 ? count - 1 : 0;
+        whole = __all(left == kRun);
     }
-    __device__ __forceinline__ bool whole() const { return __all(left == kRun); }
-    template <typename T, int V, bool WIDE>
-    __device__ __forceinline__ void load(const T* p, int64_t st, int64_t c, int64_t n, Part<T, V> (&v)[kRun]) const {
+    // Whether the wave takes the group that step i begins.
+    __device__ __forceinline__ bool takes(int i) const { return whole || __any(i < left); }
+    __device__ __forceinline__ bool stores(int i) const { return whole || __any(i < steps); }
+    template <typename T, bool WIDE>
+    __device__ __forceinline__ void load(const T* p, int64_t st, int64_t c, int64_t n, Part<T> (&v)[kRun]) const {
         p += first * st;
-        if (whole()) {
-#pragma unroll
-            for (int i = 0; i < kRun; ++i, p += st) v[i] = load_part<T, V, WIDE>(p, c, n);
-        } else {
+        if (whole) {
 #pragma unroll
             for (int i = 0; i < kRun; ++i) {
-                v[i] = load_part<T, V, WIDE>(p, c, n);
-                p += i + 1 < left ? st : 0;
+                v[i] = load_part<T, WIDE>(p, c, n);
+                move(p, st);
             }
+            return;
+        }
 #pragma unroll
-            for (int i = 0; i < kRun; ++i)
+        for (int k = 0; k < kRun; k += kGroup) {
+            if (__any(k < left)) {
 #pragma unroll
-                for (int j = 0; j < V; ++j) v[i].v[j] = i < left ? v[i].v[j] : (T)0.0f;
+                for (int i = k; i < k + kGroup; ++i) {
+                    v[i] = load_part<T, WIDE>(p, c, n);
+                    move(p, i + 1 < left ? st : 0);
+                }
+            } else {
+#pragma unroll
+                for (int i = k; i < k + kGroup; ++i) v[i] = Part<T>{};
+            }
         }
     }
+    // Zeros for the steps that the item has not.
+    template <typename T>
+    __device__ __forceinline__ void take_out(Part<T> (&v)[kRun]) const {
+        if (whole) return;
+#pragma unroll
+        for (int i = 0; i < kRun; ++i) v[i].clear_unless(i < left);
+    }
+    // Their gates leave a state as it is.
+    template <int V>
+    __device__ __forceinline__ void take_out(float (&q)[kRun][V]) const {
+        if (whole) return;
+#pragma unroll
+        for (int i = 0; i < kRun; ++i)
+#pragma unroll
+            for (int j = 0; j < V; ++j) q[i][j] = i < left ? q[i][j] : 0.0f;
+    }
 };
-
-// The gates of steps that the item has not: they leave a state as it is.
-template <int V>
-__device__ __forceinline__ void take_out(const Run& r, float (&q)[kRun][V]) {
-    if (r.whole()) return;
-#pragma unroll
-    for (int i = 0; i < kRun; ++i)
-#pragma unroll
-        for (int j = 0; j < V; ++j) q[i][j] = i < r.left ? q[i][j] : 0.0f;
-}
 
 // Where a thread works: its channels, and the runs it takes.
 template <int V, bool SCAN>
 struct Lane {
-    static constexpr int kLanes = kRecurBlock / V;                      // threads of a step (scan)
-    static constexpr int kSlots = SCAN ? kRecurThreads / kLanes : 1;    // runs of a tile
-    static constexpr int kInWave = 64 / kLanes;                         // of them in a wave
-    static constexpr int kWaves = kRecurThreads / 64;
+    static constexpr int kThreads = SCAN ? kScanBlock : kWalkBlock;
+    static constexpr int kLanes = kRecurBlock / V;              // threads of a step (scan)
+    static constexpr int kSlots = SCAN ? kThreads / kLanes : 1; // runs of a tile
+    static constexpr int kInWave = 64 / kLanes;                 // of them in a wave
+    static constexpr int kWaves = kThreads / 64;
     uint32_t b;
     int64_t c;       // first channel
     int slot, split;
@@ -199,15 +257,15 @@ struct Lane {
             t0 = (int)((int64_t)cut.tiles * split / cut.splits);
             t1 = split < cut.splits ? (int)((int64_t)cut.tiles * (split + 1) / cut.splits) : t0;
         } else {
-            const uint32_t id = group_index() * kRecurThreads + threadIdx.x;
+            const uint32_t id = group_index() * kThreads + threadIdx.x;
             live = id < cut.columns * a.batch;
-            b = cut.by_columns.quotient(live ? id : 0);
+            b = live ? cut.by_columns.quotient(id) : 0;
             c = (int64_t)((live ? id : 0) - b * cut.columns) * V;
             slot = split = 0;
             t0 = 0;
             t1 = live ? cut.tiles : 0;
         }
-        if (!live) b = 0, c = 0;
+        if (!live) c = 0;
         count = a.steps;
         if (a.lengths) {
             const int64_t n = a.lengths[b];
@@ -329,7 +387,7 @@ inline bool walks(const RecurArgs& a) {
     constexpr int v = kRecurChannels;
     return a.steps <= 2 * kRun || (uint64_t)a.batch * ((a.channels + v - 1) / v) >= kWalkThreads;
 }
-constexpr uint32_t kScanGroups = 1024;  // workgroups that fill the card
+constexpr uint32_t kScanGroups = 256;  // workgroups that fill the card: one a CU
 inline RecurCut recur_cut(const RecurArgs& a) {
     constexpr int v = kRecurChannels;
     RecurCut c{};
@@ -339,10 +397,10 @@ inline RecurCut recur_cut(const RecurArgs& a) {
     c.splits = 1;
     if (walks(a)) {
         c.tiles = (int32_t)runs;
-        c.groups = (uint32_t)(((uint64_t)c.columns * a.batch + kRecurThreads - 1) / kRecurThreads);
+        c.groups = (uint32_t)(((uint64_t)c.columns * a.batch + kWalkBlock - 1) / kWalkBlock);
         return c;
     }
-    const int slots = kRecurThreads * v / kRecurBlock;
+    const int slots = kScanBlock * v / kRecurBlock;
     c.tiles = (int32_t)((runs + slots - 1) / slots);
     c.blocks = (uint32_t)((a.channels + kRecurBlock - 1) / kRecurBlock);
     const uint64_t base = (uint64_t)c.blocks * a.batch;

@@ -23,67 +23,109 @@ namespace {
 
 constexpr int V = kRecurChannels;
 
+// What a thread reads for a run.
+template <typename T, bool Z>
+struct Inputs {
+    Part<T> g[kRun], x[kRun], z[Z ? kRun : 1];
+};
+
+// AHEAD: the next tile's loads are out while this one is worked on (fp32 has no
+// registers for that).
 template <typename T, bool WIDE, bool Z, int GAIN, bool SCAN>
-__global__ __launch_bounds__(kRecurThreads) void k_recur(RecurArgs a, RecurCut cut) {
+__global__ __launch_bounds__((Lane<V, SCAN>::kThreads)) void k_recur(RecurArgs a, RecurCut cut) {
     typedef Lane<V, SCAN> L;
+    constexpr bool AHEAD = SCAN && sizeof(T) == 2;
     __shared__ float maps[SCAN ? 2 : 1][L::kWaves][L::kLanes][2 * V];
     const L ln(a, cut);
     const int64_t C = a.channels, at = ln.state_at(a), runs = (a.steps + kRun - 1) / kRun;
     float h[V];
     load_state(cut.splits > 1 ? cut.entry : a.state, at, ln.c, C, ln.live, h);
     if constexpr (SCAN) through_splits<V, false>(a, cut, ln.split, at, ln.c, ln.live, h);
+    auto load = [&](int t) {
+        Inputs<T, Z> in;
+        const Run r(a, ((int64_t)t * L::kSlots + ln.slot) * kRun, ln.count);
+        r.template load<T, WIDE>(ln.template at<const T>(a.g), a.g.st, ln.c, C, in.g);
+        r.template load<T, WIDE>(ln.template at<const T>(a.x), a.x.st, ln.c, C, in.x);
+        if constexpr (Z) r.template load<T, WIDE>(ln.template at<const T>(a.z), a.z.st, ln.c, C, in.z);
+        return in;
+    };
+    Inputs<T, Z> next;
+    if constexpr (AHEAD)
+        if (ln.t0 < ln.t1) next = load(ln.t0);
     for (int t = ln.t0; t < ln.t1; ++t) {
         const int64_t run = (int64_t)t * L::kSlots + ln.slot, s0 = run * kRun;
         const Run r(a, s0, ln.count);
-        Part<T, V> x[kRun], z[kRun];
-        float q[kRun][V];
-        {
-            Part<T, V> g[kRun];
-            r.template load<T, V, WIDE>(ln.template at<const T>(a.g), a.g.st, ln.c, C, g);
-            r.template load<T, V, WIDE>(ln.template at<const T>(a.x), a.x.st, ln.c, C, x);
-            if constexpr (Z) r.template load<T, V, WIDE>(ln.template at<const T>(a.z), a.z.st, ln.c, C, z);
-#pragma unroll
-            for (int i = 0; i < kRun; ++i)
-#pragma unroll
-                for (int j = 0; j < V; ++j) q[i][j] = gate_of((float)g[i].v[j]);
-            take_out(r, q);
-        }
-        float mine[V];
-        if constexpr (SCAN) {
-            Product P[V];
-            float A[V], B[V];
-#pragma unroll
-            for (int j = 0; j < V; ++j) B[j] = 0.0f;
-#pragma unroll
-            for (int i = 0; i < kRun; ++i)
-#pragma unroll
-                for (int j = 0; j < V; ++j) {
-                    P[j].take(q[i][j]);
-                    B[j] = advance<GAIN>(B[j], q[i][j], (float)x[i].v[j]);
-                }
-#pragma unroll
-            for (int j = 0; j < V; ++j) A[j] = P[j].gate();
-            JoinMaps<V, SCAN, false>::run(A, B, h, mine, maps, t & 1);
+        Inputs<T, Z> in;
+        if constexpr (AHEAD) {
+            in = next;
+            if (t + 1 < ln.t1) next = load(t + 1);
         } else {
-#pragma unroll
-            for (int j = 0; j < V; ++j) mine[j] = h[j];
+            in = load(t);
         }
-        if (a.carries) store_state(a.carries, (ln.b * runs + run) * C + ln.c, ln.c, C, ln.live && run < runs, mine);
+        r.take_out(in.x);
+        float mine[V];
         T* y = ln.template at<T>(a.y) + s0 * a.y.st;
+        auto out = [&](int i, float state, int j) { return Z ? state * sigmoid(in.z[Z ? i : 0].at(j)) : state; };
+        // Writes step i of the run; e(j): its states.
+        auto finish = [&](auto&& e) {
+            if (r.whole) {
+                if (ln.live) {
 #pragma unroll
-        for (int i = 0; i < kRun; ++i, y += a.y.st) {
-            float e[V];
+                    for (int i = 0; i < kRun; ++i) {
+                        float v[V];
+#pragma unroll
+                        for (int j = 0; j < V; ++j) v[j] = out(i, e(i, j), j);
+                        store_part<T, V, WIDE>(y, ln.c, C, v);
+                        move(y, a.y.st);
+                    }
+                }
+                return;
+            }
+#pragma unroll
+            for (int k = 0; k < kRun; k += kGroup)
+                if (r.stores(k)) {
+#pragma unroll
+                    for (int i = k; i < k + kGroup; ++i) {
+                        float v[V];
+#pragma unroll
+                        for (int j = 0; j < V; ++j) {
+                            v[j] = out(i, e(i, j), j);
+                            v[j] = i < r.left ? v[j] : 0.0f;
+                        }
+                        if (ln.live && i < r.steps) store_part<T, V, WIDE>(y, ln.c, C, v);
+                        move(y, a.y.st);
+                    }
+                }
+        };
+        if constexpr (SCAN) {
+            // the run's map step by step; the states are one multiply-add from it
+            float A[kRun][V], B[kRun][V], qa[V], qb[V];
 #pragma unroll
             for (int j = 0; j < V; ++j) {
-                mine[j] = advance<GAIN>(mine[j], q[i][j], (float)x[i].v[j]);
-                e[j] = Z ? mine[j] * sigmoid((float)z[i].v[j]) : mine[j];
-                e[j] = i < r.left ? e[j] : 0.0f;
-            }
-            if (ln.live && i < r.steps) store_part<T, V, WIDE>(y, ln.c, C, e);
-        }
-        if constexpr (!SCAN) {
+                Product P;
+                float state = 0.0f;
 #pragma unroll
-            for (int j = 0; j < V; ++j) h[j] = mine[j];
+                for (int i = 0; i < kRun; ++i) {
+                    float q = gate_of(in.g[i].at(j));
+                    if (!r.whole) q = i < r.left ? q : 0.0f;
+                    P.take(q);
+                    state = advance<GAIN>(state, q, in.x[i].at(j));
+                    A[i][j] = P.a;
+                    B[i][j] = state;
+                }
+                qa[j] = P.gate();
+                qb[j] = state;
+            }
+            JoinMaps<V, SCAN, false>::run(qa, qb, h, mine, maps, t & 1);
+            if (a.carries) store_state(a.carries, (ln.b * runs + run) * C + ln.c, ln.c, C, ln.live && run < runs, mine);
+            finish([&](int i, int j) { return fmaf(A[i][j], mine[j], B[i][j]); });
+        } else {
+            if (a.carries) store_state(a.carries, (ln.b * runs + run) * C + ln.c, ln.c, C, ln.live, h);
+            finish([&](int i, int j) {
+                float q = gate_of(in.g[i].at(j));
+                if (!r.whole) q = i < r.left ? q : 0.0f;
+                return h[j] = advance<GAIN>(h[j], q, in.x[i].at(j));
+            });
         }
     }
     if (a.last && ln.slot == 0 && ln.split == cut.splits - 1) store_state(a.last, at, ln.c, C, ln.live, h);
@@ -92,7 +134,7 @@ __global__ __launch_bounds__(kRecurThreads) void k_recur(RecurArgs a, RecurCut c
 // The maps of all splits but the last: each slot takes a stretch of the split's
 // runs, and the slots' maps are joined in their order.
 template <typename T, bool WIDE, int GAIN>
-__global__ __launch_bounds__(kRecurThreads) void k_recur_maps(RecurArgs a, RecurCut cut) {
+__global__ __launch_bounds__(kScanBlock) void k_recur_maps(RecurArgs a, RecurCut cut) {
     typedef Lane<V, true> L;
     __shared__ float maps[L::kSlots][L::kLanes][2 * V];
     const L ln(a, cut);
@@ -105,21 +147,18 @@ __global__ __launch_bounds__(kRecurThreads) void k_recur_maps(RecurArgs a, Recur
     for (int t = 0; t < n; ++t) {
         const int64_t s0 = ((int64_t)ln.t0 * L::kSlots + (int64_t)ln.slot * n + t) * kRun;
         const Run r(a, s0, ln.count);
-        Part<T, V> x[kRun], g[kRun];
-        r.template load<T, V, WIDE>(ln.template at<const T>(a.g), a.g.st, ln.c, C, g);
-        r.template load<T, V, WIDE>(ln.template at<const T>(a.x), a.x.st, ln.c, C, x);
-        float q[kRun][V];
-#pragma unroll
-        for (int i = 0; i < kRun; ++i)
-#pragma unroll
-            for (int j = 0; j < V; ++j) q[i][j] = gate_of((float)g[i].v[j]);
-        take_out(r, q);
+        Part<T> x[kRun], g[kRun];
+        r.template load<T, WIDE>(ln.template at<const T>(a.g), a.g.st, ln.c, C, g);
+        r.template load<T, WIDE>(ln.template at<const T>(a.x), a.x.st, ln.c, C, x);
+        r.take_out(x);
 #pragma unroll
         for (int i = 0; i < kRun; ++i)
 #pragma unroll
             for (int j = 0; j < V; ++j) {
-                P[j].take(q[i][j]);
-                B[j] = advance<GAIN>(B[j], q[i][j], (float)x[i].v[j]);
+                float q = gate_of(g[i].at(j));
+                if (!r.whole) q = i < r.left ? q : 0.0f;
+                P[j].take(q);
+                B[j] = advance<GAIN>(B[j], q, x[i].at(j));
             }
     }
     const int col = threadIdx.x % L::kLanes;
@@ -158,7 +197,7 @@ hipError_t launch_recur(const RecurArgs& a, float* ws) {
         const hipError_t e = recur_dispatch(a, [&](auto t, auto wide, auto) {
             return by_gain(a.gain, [&](auto gain) {
                 hipLaunchKernelGGL((k_recur_maps<decltype(t), decltype(wide)::value, decltype(gain)::value>), grid_dim(groups),
-                                   dim3(kRecurThreads), 0, a.stream, a, cut);
+                                   dim3(kScanBlock), 0, a.stream, a, cut);
                 return hipGetLastError();
             });
         });
@@ -169,7 +208,7 @@ hipError_t launch_recur(const RecurArgs& a, float* ws) {
     const hipError_t e = recur_dispatch(a, [&](auto t, auto wide, auto z) {
         return by_gain(a.gain, [&](auto gain) {
             auto go = [&](auto kernel) {
-                hipLaunchKernelGGL(kernel, grid_dim(cut.groups), dim3(kRecurThreads), 0, a.stream, a, cut);
+                hipLaunchKernelGGL(kernel, grid_dim(cut.groups), dim3(cut.blocks ? kScanBlock : kWalkBlock), 0, a.stream, a, cut);
             };
             if (cut.blocks) go(k_recur<decltype(t), decltype(wide)::value, decltype(z)::value, decltype(gain)::value, true>);
             else go(k_recur<decltype(t), decltype(wide)::value, decltype(z)::value, decltype(gain)::value, false>);

@@ -21,6 +21,10 @@ namespace {
 
 constexpr int V = kRecurChannels;
 
+// Nothing is moved over it: the steps of a run have much to do ahead of the chain
+// that links them, which taken all at once does not fit the registers.
+__device__ __forceinline__ void apart() { __builtin_amdgcn_sched_barrier(0); }
+
 // dc/da times a (1 - a).
 template <int GAIN>
 __device__ __forceinline__ float gain_slope(float q) {
@@ -31,95 +35,166 @@ __device__ __forceinline__ float gain_slope(float q) {
     return -a * a * __builtin_amdgcn_sqrtf(rest * __builtin_amdgcn_rcpf(1.0f + a));
 }
 
+// What a thread reads for a run.
+template <typename T, bool Z>
+struct Inputs {
+    Part<T> g[kRun], x[kRun], dy[kRun], z[Z ? kRun : 1];
+    float before[V];
+};
+
+// AHEAD: the next tile's loads are out while this one is worked on.
 template <typename T, bool WIDE, bool Z, int GAIN, bool SCAN>
-__global__ __launch_bounds__(kRecurThreads) void k_recur_grad(RecurArgs a, RecurCut cut) {
+__global__ __launch_bounds__((Lane<V, SCAN>::kThreads)) void k_recur_grad(RecurArgs a, RecurCut cut) {
     typedef Lane<V, SCAN> L;
+    constexpr bool AHEAD = SCAN && sizeof(T) == 2;
     __shared__ float maps[SCAN ? 2 : 1][L::kWaves][L::kLanes][2 * V];
+    // The states before the steps of a thread's run (in registers they would leave no room for the
+    // next tile).
+    struct alignas(4 * V) Pair {
+        float v[V];
+    };
+    __shared__ Pair before[kRun][L::kThreads];
     const L ln(a, cut);
     const int64_t C = a.channels, at = ln.state_at(a), runs = (a.steps + kRun - 1) / kRun;
     float G[V];  // what the steps behind pass to the state
     load_state(cut.splits > 1 ? cut.entry : a.dlast, at, ln.c, C, ln.live, G);
     if constexpr (SCAN) through_splits<V, true>(a, cut, ln.split, at, ln.c, ln.live, G);
+    auto load = [&](int t) {
+        Inputs<T, Z> in;
+        const int64_t run = (int64_t)t * L::kSlots + ln.slot;
+        const Run r(a, run * kRun, ln.count);
+        load_state(a.carries, (ln.b * runs + run) * C + ln.c, ln.c, C, ln.live && run < runs, in.before);
+        r.template load<T, WIDE>(ln.template at<const T>(a.g), a.g.st, ln.c, C, in.g);
+        r.template load<T, WIDE>(ln.template at<const T>(a.dy), a.dy.st, ln.c, C, in.dy);
+        if constexpr (Z) r.template load<T, WIDE>(ln.template at<const T>(a.z), a.z.st, ln.c, C, in.z);
+        r.template load<T, WIDE>(ln.template at<const T>(a.x), a.x.st, ln.c, C, in.x);
+        return in;
+    };
+    Inputs<T, Z> next;
+    if constexpr (AHEAD)
+        if (ln.t0 < ln.t1) next = load(ln.t1 - 1);
     for (int t = ln.t1 - 1; t >= ln.t0; --t) {
         const int64_t run = (int64_t)t * L::kSlots + ln.slot, s0 = run * kRun;
         const Run r(a, s0, ln.count);
-        Part<T, V> x[kRun], dy[kRun];
-        float q[kRun][V], qz[Z ? kRun : 1][V], h[V];
-        load_state(a.carries, (ln.b * runs + run) * C + ln.c, ln.c, C, ln.live && run < runs, h);
-        {
-            Part<T, V> g[kRun], z[kRun];
-            r.template load<T, V, WIDE>(ln.template at<const T>(a.g), a.g.st, ln.c, C, g);
-            r.template load<T, V, WIDE>(ln.template at<const T>(a.x), a.x.st, ln.c, C, x);
-            r.template load<T, V, WIDE>(ln.template at<const T>(a.dy), a.dy.st, ln.c, C, dy);
-            if constexpr (Z) r.template load<T, V, WIDE>(ln.template at<const T>(a.z), a.z.st, ln.c, C, z);
-#pragma unroll
-            for (int i = 0; i < kRun; ++i)
-#pragma unroll
-                for (int j = 0; j < V; ++j) {
-                    q[i][j] = gate_of((float)g[i].v[j]);
-                    if constexpr (Z) qz[i][j] = gate_of((float)z[i].v[j]);
-                }
-            take_out(r, q);
+        Inputs<T, Z> in;
+        if constexpr (AHEAD) {
+            in = next;
+            if (t > ln.t0) next = load(t - 1);
+        } else {
+            in = load(t);
         }
+        r.take_out(in.x);
+        r.take_out(in.dy);
+        if constexpr (Z) r.take_out(in.z);
+        float q[kRun][V], qz[Z ? kRun : 1][V];
+#pragma unroll
+        for (int i = 0; i < kRun; ++i)
+#pragma unroll
+            for (int j = 0; j < V; ++j) {
+                q[i][j] = gate_of(in.g[i].at(j));
+                if constexpr (Z) qz[i][j] = gate_of(in.z[i].at(j));
+            }
+        r.take_out(q);
         // the gradient that the output of step i brings to its state
         auto brought = [&](int i, int j) {
-            const float d = (float)dy[i].v[j];
+            const float d = in.dy[i].at(j);
             if constexpr (!Z) return d;
             const float s = fabsf(qz[Z ? i : 0][j]);
             return d * (closed(qz[Z ? i : 0][j]) ? s : 1.0f - s);
         };
         float mine[V];
         if constexpr (SCAN) {
-            Product P[V];
-            float A[V], B[V];
+            float qa[V], qb[V];
 #pragma unroll
-            for (int j = 0; j < V; ++j) B[j] = 0.0f;
+            for (int j = 0; j < V; ++j) {
+                Product P;
+                float D = 0.0f;
 #pragma unroll
-            for (int i = kRun - 1; i >= 0; --i)
-#pragma unroll
-                for (int j = 0; j < V; ++j) {
-                    P[j].take(q[i][j]);
-                    B[j] = decay(B[j] + brought(i, j), q[i][j]);
+                for (int i = kRun - 1; i >= 0; --i) {
+                    P.take(q[i][j]);
+                    D = decay(D + brought(i, j), q[i][j]);
+                    if (i % kGroup == 0) apart();
                 }
-#pragma unroll
-            for (int j = 0; j < V; ++j) A[j] = P[j].gate();
-            JoinMaps<V, SCAN, true>::run(A, B, G, mine, maps, t & 1);
+                qa[j] = P.gate();
+                qb[j] = D;
+            }
+            JoinMaps<V, SCAN, true>::run(qa, qb, G, mine, maps, t & 1);
         } else {
 #pragma unroll
             for (int j = 0; j < V; ++j) mine[j] = G[j];
         }
-        float before[kRun + 1][V];
+        anew(q);
+        if constexpr (Z) anew(qz);
 #pragma unroll
-        for (int j = 0; j < V; ++j) before[0][j] = h[j];
+        for (int i = 0; i < kRun; ++i) in.dy[i].anew();
+        {
+            float h[V];
 #pragma unroll
-        for (int i = 0; i < kRun; ++i)
+            for (int j = 0; j < V; ++j) h[j] = in.before[j];
 #pragma unroll
-            for (int j = 0; j < V; ++j) before[i + 1][j] = advance<GAIN>(before[i][j], q[i][j], (float)x[i].v[j]);
-        T* to_x = ln.template at<T>(a.dx) + (s0 + kRun - 1) * a.dx.st;
-        T* to_g = ln.template at<T>(a.dg) + (s0 + kRun - 1) * a.dg.st;
-        T* to_z = ln.template at<T>(a.dz) + (s0 + kRun - 1) * a.dz.st;
+            for (int i = 0; i < kRun; ++i) {
+                Pair p;
 #pragma unroll
-        for (int i = kRun - 1; i >= 0; --i, to_x -= a.dx.st, to_g -= a.dg.st, to_z -= a.dz.st) {
+                for (int j = 0; j < V; ++j) {
+                    p.v[j] = h[j];
+                    h[j] = advance<GAIN>(h[j], q[i][j], in.x[i].at(j));
+                }
+                before[i][threadIdx.x] = p;
+                in.x[i].anew();
+                if (i % kGroup == kGroup - 1) apart();
+            }
+#pragma unroll
+            for (int j = 0; j < V; ++j) in.before[j] = h[j];  // the state behind the run
+        }
+        anew(q);
+        const int64_t last = s0 + kRun - 1;
+        T *to_x = ln.template at<T>(a.dx) + last * a.dx.st, *to_g = ln.template at<T>(a.dg) + last * a.dg.st,
+          *to_z = ln.template at<T>(a.dz) + last * a.dz.st;
+        auto step = [&](int i, bool inside, bool stored, auto every) {
             float dx[V], dg[V], dz[V];
-            const bool inside = i < r.left;
+            const Pair p = before[i][threadIdx.x];
 #pragma unroll
             for (int j = 0; j < V; ++j) {
                 const float D = mine[j] + brought(i, j), s = fabsf(q[i][j]), slope = fmaf(-s, s, s);
                 dx[j] = inside ? gain_of<GAIN>(q[i][j]) * D : 0.0f;
-                if (GAIN == kGainMean) dg[j] = D * slope * (before[i][j] - (float)x[i].v[j]);
-                else dg[j] = D * fmaf(gain_slope<GAIN>(q[i][j]), (float)x[i].v[j], slope * before[i][j]);
+                if (GAIN == kGainMean) dg[j] = D * slope * (p.v[j] - in.x[i].at(j));
+                else dg[j] = D * fmaf(gain_slope<GAIN>(q[i][j]), in.x[i].at(j), slope * p.v[j]);
                 dg[j] = inside ? dg[j] : 0.0f;
                 if constexpr (Z) {
                     const float u = fabsf(qz[Z ? i : 0][j]);
-                    dz[j] = inside ? (float)dy[i].v[j] * before[i + 1][j] * fmaf(-u, u, u) : 0.0f;
+                    dz[j] = inside ? in.dy[i].at(j) * in.before[j] * fmaf(-u, u, u) : 0.0f;
                 }
                 mine[j] = decay(D, q[i][j]);
+                in.before[j] = p.v[j];
             }
-            if (ln.live && i < r.steps) {
-                if (a.dx.p) store_part<T, V, WIDE>(to_x, ln.c, C, dx);
-                if (a.dg.p) store_part<T, V, WIDE>(to_g, ln.c, C, dg);
+            if (stored) {
+                if (every || a.dx.p) store_part<T, V, WIDE>(to_x, ln.c, C, dx);
+                if (every || a.dg.p) store_part<T, V, WIDE>(to_g, ln.c, C, dg);
                 if constexpr (Z)
-                    if (a.dz.p) store_part<T, V, WIDE>(to_z, ln.c, C, dz);
+                    if (every || a.dz.p) store_part<T, V, WIDE>(to_z, ln.c, C, dz);
+            }
+            move(to_x, -a.dx.st);
+            move(to_g, -a.dg.st);
+            if constexpr (Z) move(to_z, -a.dz.st);
+            if (i % kGroup == 0) apart();
+        };
+        // (every: all gradients are asked for)
+        if (r.whole && a.dx.p && a.dg.p && (!Z || a.dz.p)) {
+            if (ln.live) {
+#pragma unroll
+                for (int i = kRun - 1; i >= 0; --i) step(i, true, true, std::true_type{});
+            }
+        } else {
+#pragma unroll
+            for (int k = kRun - kGroup; k >= 0; k -= kGroup) {
+                if (r.stores(k)) {
+#pragma unroll
+                    for (int i = k + kGroup - 1; i >= k; --i) step(i, i < r.left, ln.live && i < r.steps, std::false_type{});
+                } else {
+                    to_x -= kGroup * a.dx.st;
+                    to_g -= kGroup * a.dg.st;
+                    to_z -= kGroup * a.dz.st;
+                }
             }
         }
         if constexpr (!SCAN) {
@@ -132,7 +207,7 @@ __global__ __launch_bounds__(kRecurThreads) void k_recur_grad(RecurArgs a, Recur
 
 // The maps of all splits but the first, from their ends.
 template <typename T, bool WIDE, bool Z>
-__global__ __launch_bounds__(kRecurThreads) void k_recur_grad_maps(RecurArgs a, RecurCut cut) {
+__global__ __launch_bounds__(kScanBlock) void k_recur_grad_maps(RecurArgs a, RecurCut cut) {
     typedef Lane<V, true> L;
     __shared__ float maps[L::kSlots][L::kLanes][2 * V];
     const L ln(a, cut, 1);
@@ -145,23 +220,21 @@ __global__ __launch_bounds__(kRecurThreads) void k_recur_grad_maps(RecurArgs a, 
     for (int t = n - 1; t >= 0; --t) {
         const int64_t s0 = ((int64_t)ln.t0 * L::kSlots + (int64_t)ln.slot * n + t) * kRun;
         const Run r(a, s0, ln.count);
-        Part<T, V> g[kRun], dy[kRun], z[kRun];
-        r.template load<T, V, WIDE>(ln.template at<const T>(a.g), a.g.st, ln.c, C, g);
-        r.template load<T, V, WIDE>(ln.template at<const T>(a.dy), a.dy.st, ln.c, C, dy);
-        if constexpr (Z) r.template load<T, V, WIDE>(ln.template at<const T>(a.z), a.z.st, ln.c, C, z);
-        float q[kRun][V];
-#pragma unroll
-        for (int i = 0; i < kRun; ++i)
-#pragma unroll
-            for (int j = 0; j < V; ++j) q[i][j] = gate_of((float)g[i].v[j]);
-        take_out(r, q);
+        Part<T> g[kRun], dy[kRun], z[kRun];
+        r.template load<T, WIDE>(ln.template at<const T>(a.g), a.g.st, ln.c, C, g);
+        r.template load<T, WIDE>(ln.template at<const T>(a.dy), a.dy.st, ln.c, C, dy);
+        if constexpr (Z) r.template load<T, WIDE>(ln.template at<const T>(a.z), a.z.st, ln.c, C, z);
+        r.take_out(dy);
+        if constexpr (Z) r.take_out(z);
 #pragma unroll
         for (int i = kRun - 1; i >= 0; --i)
 #pragma unroll
             for (int j = 0; j < V; ++j) {
-                const float d = (float)dy[i].v[j];
-                P[j].take(q[i][j]);
-                B[j] = decay(B[j] + (Z ? d * sigmoid((float)z[i].v[j]) : d), q[i][j]);
+                float q = gate_of(g[i].at(j));
+                if (!r.whole) q = i < r.left ? q : 0.0f;
+                const float d = dy[i].at(j);
+                P[j].take(q);
+                B[j] = decay(B[j] + (Z ? d * sigmoid(z[i].at(j)) : d), q);
             }
     }
     const int col = threadIdx.x % L::kLanes;
@@ -204,7 +277,7 @@ hipError_t launch_recur_grad(const RecurArgs& a, float* ws) {
         const uint32_t groups = cut.groups / cut.splits * (cut.splits - 1);
         const hipError_t e = recur_dispatch(a, [&](auto t, auto wide, auto z) {
             hipLaunchKernelGGL((k_recur_grad_maps<decltype(t), decltype(wide)::value, decltype(z)::value>), grid_dim(groups),
-                               dim3(kRecurThreads), 0, a.stream, a, cut);
+                               dim3(kScanBlock), 0, a.stream, a, cut);
             return hipGetLastError();
         });
         timing_end(tk, a.stream);
@@ -214,7 +287,7 @@ hipError_t launch_recur_grad(const RecurArgs& a, float* ws) {
     const hipError_t e = recur_dispatch(a, [&](auto t, auto wide, auto z) {
         return by_gain(a.gain, [&](auto gain) {
             auto go = [&](auto kernel) {
-                hipLaunchKernelGGL(kernel, grid_dim(cut.groups), dim3(kRecurThreads), 0, a.stream, a, cut);
+                hipLaunchKernelGGL(kernel, grid_dim(cut.groups), dim3(cut.blocks ? kScanBlock : kWalkBlock), 0, a.stream, a, cut);
             };
             if (cut.blocks) go(k_recur_grad<decltype(t), decltype(wide)::value, decltype(z)::value, decltype(gain)::value, true>);
             else go(k_recur_grad<decltype(t), decltype(wide)::value, decltype(z)::value, decltype(gain)::value, false>);

@@ -114,10 +114,8 @@ struct Cursor {
 template <typename T, int W>
 __device__ __forceinline__ Raw<T> load_weight(const void* w, int64_t sb, uint32_t item, int c, int left) {
     Raw<T> r;
-    if (w) return load_raw<T, W>((const T*)w + item * sb + c, left);
-#pragma unroll
-    for (int i = 0; i < kChunk; ++i) r.v[i] = (T)1.0f;
-    return r;
+    r.fill(1.0f);
+    return w ? load_raw<T, W>((const T*)w + item * sb + c, left) : r;
 }
 
 // Host: the widest pieces that rows are read and written in.

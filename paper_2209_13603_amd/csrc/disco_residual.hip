@@ -57,9 +57,7 @@ __global__ __launch_bounds__(512) void k_residual(ResidualArgs a, NormShape s) {
             for (int j = 0; j < NV; ++j) {
                 r.f[j] = load_raw<T, W>(f + j * step, n - j * step);
                 if (has(s, kHasX)) r.x[j] = load_raw<T, W>(x + j * step, n - j * step);
-                else
-#pragma unroll
-                    for (int i = 0; i < kChunk; ++i) r.x[j].v[i] = (T)0.0f;
+                else r.x[j].fill(0.0f);
             }
             return r;
         };
@@ -76,11 +74,11 @@ __global__ __launch_bounds__(512) void k_residual(ResidualArgs a, NormShape s) {
             const int n = at < stop ? C - c : 0;
             const Row now = next;
 #pragma unroll
-            for (int j = 0; j < NV; ++j) stay_raw(w[j]), stay_raw(g[j]), stay_raw(w2[j]);
+            for (int j = 0; j < NV; ++j) w[j].anew(), g[j].anew(), w2[j].anew();
             if (base + s.slots < stop) next = load(at + s.slots);
             float e[NV * kChunk];
 #pragma unroll
-            for (int i = 0; i < NV * kChunk; ++i) e[i] = (float)now.f[i / kChunk].v[i % kChunk];
+            for (int i = 0; i < NV * kChunk; ++i) e[i] = now.f[i / kChunk].at(i % kChunk);
             float r = 1.0f, up;
             if (has(s, kHasPost)) r = norm_factor(e, a, rs.one(squares(e)), rs, &up, &again);
             r *= a.drop.factor;  // (1 where nothing is dropped)
@@ -93,9 +91,9 @@ __global__ __launch_bounds__(512) void k_residual(ResidualArgs a, NormShape s) {
                 if constexpr (DROP) bits = drop_words(a.drop, offset, item * s.row_item + at * s.row_at, lane + s.lanes * j);
 #pragma unroll
                 for (int i = 0; i < kChunk; ++i) {
-                    float d = u[i] * r * (float)w[j].v[i];
+                    float d = u[i] * r * w[j].at(i);
                     if constexpr (DROP) d = stays(bits, i, a.drop.out) ? d : 0.0f;
-                    v[i] = u[i] = fmaf(a.scale, (float)now.x[j].v[i], d * (float)g[j].v[i]);
+                    v[i] = u[i] = fmaf(a.scale, now.x[j].at(i), d * g[j].at(i));
                 }
                 if (has(s, kHasH)) store_raw<T, W>(h + j * step, n - j * step, v);
             }
@@ -105,7 +103,7 @@ __global__ __launch_bounds__(512) void k_residual(ResidualArgs a, NormShape s) {
             for (int j = 0; j < NV; ++j) {
                 float v[kChunk];
 #pragma unroll
-                for (int i = 0; i < kChunk; ++i) v[i] = e[j * kChunk + i] * r * (float)w2[j].v[i];
+                for (int i = 0; i < kChunk; ++i) v[i] = e[j * kChunk + i] * r * w2[j].at(i);
                 store_raw<T, W>(y + j * step, n - j * step, v);
             }
         }

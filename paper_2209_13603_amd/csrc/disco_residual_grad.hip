@@ -112,7 +112,7 @@ __global__ __launch_bounds__(THREADS) void k_residual_grad(ResidualArgs a, NormS
         };
         auto raw = [&](Raw<T>(&r)[NV]) {
 #pragma unroll
-            for (int j = 0; j < NV; ++j) stay_raw(r[j]);
+            for (int j = 0; j < NV; ++j) r[j].anew();
         };
         load_weights();
         Row next = load(first + slot);
@@ -123,7 +123,7 @@ __global__ __launch_bounds__(THREADS) void k_residual_grad(ResidualArgs a, NormS
             Row now = next;
             raw(w), raw(g), raw(w2);
             if (base + s.slots < stop) next = load(at + s.slots);
-            auto at_entry = [](const Raw<T>(&r)[NV], int i) { return (float)r[i / kChunk].v[i % kChunk]; };
+            auto at_entry = [](const Raw<T>(&r)[NV], int i) { return r[i / kChunk].at(i % kChunk); };
             float n1[N], d[N], h[N], D[N];
 #pragma unroll
             for (int i = 0; i < N; ++i) n1[i] = at_entry(now.f, i);
