@@ -56,6 +56,10 @@ __device__ __forceinline__ float decay(float h, float q) {
 // A product A of a's step by step, and 1 - A as a sum of what each step takes.
 struct Product {
     float a = 1.0f, rest = 0.0f;
+    __device__ __forceinline__ void take_rest(float r) {  // 1 - a of the step
+        rest = fmaf(r, a, rest);
+        a = fmaf(-r, a, a);
+    }
     __device__ __forceinline__ void take(float q) {
         const float s = fabsf(q), u = s * a, v = fmaf(-s, a, a);
         a = closed(q) ? u : v;
@@ -90,9 +94,35 @@ __device__ __forceinline__ float advance(float h, float q, float x) {
     return decay(h, q) + x;
 }
 __device__ __forceinline__ float sigmoid(float z) {
-    const float q = gate_of(z), s = fabsf(q);
-    return closed(q) ? s : 1.0f - s;
+    return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(-1.44269504f * z));
 }
+
+// A step of the forward call.  fp32 takes a gate as above; bf16, where the vector
+// unit is what bounds the call, as 1 - a alone, which keeps an a near 0 to 2^-24 of the state before it
+// instead of its own size, at two thirds of the instructions (one series of 131072 x 768: FILL).
+template <typename T>
+struct Step;
+template <>
+struct Step<float> {
+    float q;
+    __device__ __forceinline__ Step(float g, bool in) : q(in ? gate_of(g) : 0.0f) {}
+    __device__ __forceinline__ void onto(Product& p) const { p.take(q); }
+    template <int GAIN>
+    __device__ __forceinline__ float advance(float h, float x) const { return disco::advance<GAIN>(h, q, x); }
+};
+template <>
+struct Step<__bf16> {
+    float rest;
+    __device__ __forceinline__ Step(float g, bool in) : rest(in ? sigmoid(-g) : 0.0f) {}
+    __device__ __forceinline__ void onto(Product& p) const { p.take_rest(rest); }
+    template <int GAIN>
+    __device__ __forceinline__ float advance(float h, float x) const {
+        const float left = fmaf(-rest, h, h);
+        if (GAIN == kGainMean) return fmaf(rest, x, left);
+        if (GAIN == kGainPower) return fmaf(__builtin_amdgcn_sqrtf(fmaf(-rest, rest, rest + rest)), x, left);
+        return left + x;
+    }
+};
 
 // Two neighbouring channels as they lie: bf16 in one register (as single values, once
 // branches meet, they take one each).
@@ -165,6 +195,13 @@ __device__ __forceinline__ void move(T*& p, int64_t by) {
     asm("" : "+v"(p));
 }
 
+// The same for a place that all threads share, in bytes.
+template <typename P>
+__device__ __forceinline__ void move_all(P& p, int64_t by) {
+    p += by;
+    asm("" : "+s"(p));
+}
+
 // The run of a thread: 16 steps from s0 on, of which the item has `left` and the
 // tensors `steps`.  Whole runs go without conditions; of the others a wave takes
 // the groups of four steps in which one of its threads has any.  Their loads stop at the item's last
@@ -183,20 +220,30 @@ struct Run {
         first = left > 0 ? s0 : count > 0 ? count - 1 : 0;
         whole = __all(left == kRun);
     }
-    // Whether the wave takes the group that step i begins.
-    __device__ __forceinline__ bool takes(int i) const { return whole || __any(i < left); }
     __device__ __forceinline__ bool stores(int i) const { return whole || __any(i < steps); }
-    template <typename T, bool WIDE>
-    __device__ __forceinline__ void load(const T* p, int64_t st, int64_t c, int64_t n, Part<T> (&v)[kRun]) const {
-        p += first * st;
+    // Of whole runs `from`, a workgroup's first step, goes on through scalar registers, `off` (bytes) is
+    // the thread's place from there (scan); otherwise p is its own.
+    template <typename T, bool WIDE, bool SCAN>
+    __device__ __forceinline__ void load(const T* p, const char* from, uint32_t off, int64_t st, int64_t c, int64_t n,
+                                         Part<T> (&v)[kRun]) const {
         if (whole) {
+            if constexpr (SCAN) {
 #pragma unroll
-            for (int i = 0; i < kRun; ++i) {
-                v[i] = load_part<T, WIDE>(p, c, n);
-                move(p, st);
+                for (int i = 0; i < kRun; ++i) {
+                    v[i] = load_part<T, WIDE>((const T*)(from + off), c, n);
+                    move_all(from, st * (int64_t)sizeof(T));
+                }
+            } else {
+                p += first * st;
+#pragma unroll
+                for (int i = 0; i < kRun; ++i) {
+                    v[i] = load_part<T, WIDE>(p, c, n);
+                    move(p, st);
+                }
             }
             return;
         }
+        p += first * st;
 #pragma unroll
         for (int k = 0; k < kRun; k += kGroup) {
             if (__any(k < left)) {
@@ -276,6 +323,20 @@ struct Lane {
     __device__ __forceinline__ T* at(const Rows& r) const {
         return (T*)r.p + b * r.sb + c;
     }
+    // The first step of tile t in a tensor, and the thread's place from there in bytes (scan).
+    template <typename T>
+    __device__ __forceinline__ char* tile(const Rows& r, int t) const {
+        return (char*)((T*)r.p + (int64_t)b * r.sb + (int64_t)t * kSlots * kRun * r.st);
+    }
+    template <typename T>
+    __device__ __forceinline__ uint32_t offset(const Rows& r) const {
+        return (uint32_t)((slot * kRun * (uint32_t)r.st + (uint32_t)c) * (uint32_t)sizeof(T));
+    }
+    template <typename T, bool WIDE>
+    __device__ __forceinline__ void load(const Rows& r, const Run& run, int t, int64_t channels, Part<T> (&v)[kRun]) const {
+        run.template load<T, WIDE, SCAN>(at<const T>(r), SCAN ? tile<T>(r, t) : nullptr, SCAN ? offset<T>(r) : 0, r.st, c,
+                                         channels, v);
+    }
     // The place of this thread's channels in a [batch][channels] array.
     __device__ __forceinline__ int64_t state_at(const RecurArgs& a) const { return (int64_t)b * a.channels + c; }
 };
@@ -301,6 +362,50 @@ struct JoinMaps {
     typedef Lane<V, SCAN> L;
     __device__ __forceinline__ static void run(float (&A)[V], float (&B)[V], float (&h)[V], float (&mine)[V],
                                                float (*maps)[L::kWaves][L::kLanes][2 * V], int turn) {
+        in_wave(A, B, maps, turn);
+        const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, col = threadIdx.x % L::kLanes;
+        const int order = BACK ? L::kInWave - 1 - lane / L::kLanes : lane / L::kLanes;
+        // of the runs before this one in the wave
+        float ea[V], eb[V];
+#pragma unroll
+        for (int j = 0; j < V; ++j) {
+            const int from = BACK ? lane + L::kLanes : lane - L::kLanes;
+            const float a = __shfl(A[j], from), b = __shfl(B[j], from);
+            ea[j] = order ? a : 0.0f;
+            eb[j] = order ? b : 0.0f;
+        }
+        __syncthreads();
+#pragma unroll
+        for (int k = 0; k < L::kWaves; ++k) {
+            const int w = BACK ? L::kWaves - 1 - k : k;
+#pragma unroll
+            for (int j = 0; j < V; ++j) {
+                if (w == wave) mine[j] = decay(h[j], ea[j]) + eb[j];
+                h[j] = decay(h[j], maps[turn][w][col][j]) + maps[turn][w][col][V + j];
+            }
+        }
+    }
+    // The tile's own map, in the first wave's threads.
+    __device__ __forceinline__ static void all(float (&A)[V], float (&B)[V], float (*maps)[L::kWaves][L::kLanes][2 * V], int turn) {
+        in_wave(A, B, maps, turn);
+        __syncthreads();
+        if (threadIdx.x >= 64) return;
+        const int col = threadIdx.x % L::kLanes;
+#pragma unroll
+        for (int k = 0; k < L::kWaves; ++k) {
+            const int w = BACK ? L::kWaves - 1 - k : k;
+#pragma unroll
+            for (int j = 0; j < V; ++j) {
+                const float a = maps[turn][w][col][j], b = maps[turn][w][col][V + j];
+                B[j] = k ? decay(B[j], a) + b : b;
+                A[j] = k ? joined(A[j], a) : a;
+            }
+        }
+    }
+
+private:
+    // Joins the maps of a wave's runs with those before them in it, and leaves the wave's.
+    __device__ __forceinline__ static void in_wave(float (&A)[V], float (&B)[V], float (*maps)[L::kWaves][L::kLanes][2 * V], int turn) {
         const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, col = threadIdx.x % L::kLanes;
         const int at = lane / L::kLanes;  // place in the wave
         const int order = BACK ? L::kInWave - 1 - at : at;
@@ -323,35 +428,41 @@ struct JoinMaps {
                 maps[turn][wave][col][V + j] = B[j];
             }
         }
-        // of the runs before this one in the wave
-        float ea[V], eb[V];
-#pragma unroll
-        for (int j = 0; j < V; ++j) {
-            const int from = BACK ? lane + L::kLanes : lane - L::kLanes;
-            const float a = __shfl(A[j], from), b = __shfl(B[j], from);
-            ea[j] = order ? a : 0.0f;
-            eb[j] = order ? b : 0.0f;
-        }
-        __syncthreads();
-#pragma unroll
-        for (int k = 0; k < L::kWaves; ++k) {
-            const int w = BACK ? L::kWaves - 1 - k : k;
-#pragma unroll
-            for (int j = 0; j < V; ++j) {
-                if (w == wave) mine[j] = decay(h[j], ea[j]) + eb[j];
-                h[j] = decay(h[j], maps[turn][w][col][j]) + maps[turn][w][col][V + j];
-            }
-        }
     }
 };
 
 // Where a call has splits, the first kernel keeps the given state for the second.
-template <int V, bool SCAN>
-__device__ __forceinline__ void keep_entry(const Lane<V, SCAN>& ln, const RecurArgs& a, const RecurCut& cut, const float* given) {
-    float h[V];
+template <typename L>
+__device__ __forceinline__ void keep_entry(const L& ln, const RecurArgs& a, const RecurCut& cut, const float* given) {
+    float h[kRecurChannels];
     load_state(given, ln.state_at(a), ln.c, a.channels, ln.live, h);
     store_state(cut.entry, ln.state_at(a), ln.c, a.channels, ln.live, h);
 }
+
+// A split's map from those of its tiles, taken in the order opposite to that in which the
+// call then goes through them, so that it finds the last read ones in the caches.
+template <int V>
+struct SplitMap {
+    float A[V] = {0.0f}, B[V] = {0.0f};
+    // The map of a tile that comes before those taken so far.
+    __device__ __forceinline__ void before(const float (&a)[V], const float (&b)[V]) {
+#pragma unroll
+        for (int j = 0; j < V; ++j) {
+            B[j] += decay(b[j], A[j]);
+            A[j] = joined(A[j], a[j]);
+        }
+    }
+    template <typename L>
+    __device__ __forceinline__ void store(const L& ln, const RecurArgs& a, const RecurCut& cut) const {
+        float* out = cut.maps + 2 * ((int64_t)ln.split * a.batch * a.channels + ln.state_at(a));
+#pragma unroll
+        for (int j = 0; j < V; ++j)
+            if (ln.c + j < a.channels) {
+                out[2 * j] = A[j];
+                out[2 * j + 1] = B[j];
+            }
+    }
+};
 
 // The state before split `split` (behind it, looking backwards) from that at the
 // ends of the series.
@@ -381,13 +492,17 @@ inline bool recur_wide(const RecurArgs& a) {
     return true;
 }
 
-// Whether threads walk alone: where there are enough of them, or few steps.
+// Whether threads walk alone: where there are enough of them, few steps, or steps so
+// far apart that a tile has no 32-bit offsets.
 constexpr uint32_t kWalkThreads = 65536;
 inline bool walks(const RecurArgs& a) {
     constexpr int v = kRecurChannels;
+    const int64_t e = a.bf16 ? 2 : 4, tile = kScanBlock * v / kRecurBlock * kRun;
+    for (const Rows* t : {&a.x, &a.g, &a.z, &a.y, &a.dy, &a.dx, &a.dg, &a.dz})
+        if (t->p && (t->st >= ((int64_t)1 << 31) / (e * tile) - a.channels)) return true;
     return a.steps <= 2 * kRun || (uint64_t)a.batch * ((a.channels + v - 1) / v) >= kWalkThreads;
 }
-constexpr uint32_t kScanGroups = 256;  // workgroups that fill the card: one a CU
+constexpr uint32_t kScanGroups = 512;
 inline RecurCut recur_cut(const RecurArgs& a) {
     constexpr int v = kRecurChannels;
     RecurCut c{};
@@ -404,7 +519,7 @@ inline RecurCut recur_cut(const RecurArgs& a) {
     c.tiles = (int32_t)((runs + slots - 1) / slots);
     c.blocks = (uint32_t)((a.channels + kRecurBlock - 1) / kRecurBlock);
     const uint64_t base = (uint64_t)c.blocks * a.batch;
-    c.splits = (int32_t)std::max<uint64_t>(1, std::min<uint64_t>({kScanGroups / base, (uint64_t)c.tiles / 2, kMaxSplits}));
+    c.splits = base >= 192 ? 1 : (int32_t)std::max<uint64_t>(1, std::min<uint64_t>({kScanGroups / base, (uint64_t)c.tiles, kMaxSplits}));
     c.groups = (uint32_t)(base * c.splits);
     return c;
 }

@@ -34,7 +34,7 @@ struct Inputs {
 template <typename T, bool WIDE, bool Z, int GAIN, bool SCAN>
 __global__ __launch_bounds__((Lane<V, SCAN>::kThreads)) void k_recur(RecurArgs a, RecurCut cut) {
     typedef Lane<V, SCAN> L;
-    constexpr bool AHEAD = SCAN && sizeof(T) == 2;
+    constexpr bool AHEAD = SCAN && sizeof(T) == 2 && Z;
     __shared__ float maps[SCAN ? 2 : 1][L::kWaves][L::kLanes][2 * V];
     const L ln(a, cut);
     const int64_t C = a.channels, at = ln.state_at(a), runs = (a.steps + kRun - 1) / kRun;
@@ -44,9 +44,9 @@ __global__ __launch_bounds__((Lane<V, SCAN>::kThreads)) void k_recur(RecurArgs a
     auto load = [&](int t) {
         Inputs<T, Z> in;
         const Run r(a, ((int64_t)t * L::kSlots + ln.slot) * kRun, ln.count);
-        r.template load<T, WIDE>(ln.template at<const T>(a.g), a.g.st, ln.c, C, in.g);
-        r.template load<T, WIDE>(ln.template at<const T>(a.x), a.x.st, ln.c, C, in.x);
-        if constexpr (Z) r.template load<T, WIDE>(ln.template at<const T>(a.z), a.z.st, ln.c, C, in.z);
+        ln.template load<T, WIDE>(a.g, r, t, C, in.g);
+        ln.template load<T, WIDE>(a.x, r, t, C, in.x);
+        if constexpr (Z) ln.template load<T, WIDE>(a.z, r, t, C, in.z);
         return in;
     };
     Inputs<T, Z> next;
@@ -70,13 +70,20 @@ __global__ __launch_bounds__((Lane<V, SCAN>::kThreads)) void k_recur(RecurArgs a
         auto finish = [&](auto&& e) {
             if (r.whole) {
                 if (ln.live) {
+                    char* to = SCAN ? ln.template tile<T>(a.y, t) : nullptr;
+                    const uint32_t off = SCAN ? ln.template offset<T>(a.y) : 0;
 #pragma unroll
                     for (int i = 0; i < kRun; ++i) {
                         float v[V];
 #pragma unroll
                         for (int j = 0; j < V; ++j) v[j] = out(i, e(i, j), j);
-                        store_part<T, V, WIDE>(y, ln.c, C, v);
-                        move(y, a.y.st);
+                        if constexpr (SCAN) {
+                            store_part<T, V, WIDE>((T*)(to + off), ln.c, C, v);
+                            move_all(to, a.y.st * (int64_t)sizeof(T));
+                        } else {
+                            store_part<T, V, WIDE>(y, ln.c, C, v);
+                            move(y, a.y.st);
+                        }
                     }
                 }
                 return;
@@ -106,10 +113,9 @@ __global__ __launch_bounds__((Lane<V, SCAN>::kThreads)) void k_recur(RecurArgs a
                 float state = 0.0f;
 #pragma unroll
                 for (int i = 0; i < kRun; ++i) {
-                    float q = gate_of(in.g[i].at(j));
-                    if (!r.whole) q = i < r.left ? q : 0.0f;
-                    P.take(q);
-                    state = advance<GAIN>(state, q, in.x[i].at(j));
+                    const Step<T> step(in.g[i].at(j), r.whole || i < r.left);
+                    step.onto(P);
+                    state = step.template advance<GAIN>(state, in.x[i].at(j));
                     A[i][j] = P.a;
                     B[i][j] = state;
                 }
@@ -122,68 +128,56 @@ __global__ __launch_bounds__((Lane<V, SCAN>::kThreads)) void k_recur(RecurArgs a
         } else {
             if (a.carries) store_state(a.carries, (ln.b * runs + run) * C + ln.c, ln.c, C, ln.live, h);
             finish([&](int i, int j) {
-                float q = gate_of(in.g[i].at(j));
-                if (!r.whole) q = i < r.left ? q : 0.0f;
-                return h[j] = advance<GAIN>(h[j], q, in.x[i].at(j));
+                const Step<T> step(in.g[i].at(j), r.whole || i < r.left);
+                return h[j] = step.template advance<GAIN>(h[j], in.x[i].at(j));
             });
         }
     }
     if (a.last && ln.slot == 0 && ln.split == cut.splits - 1) store_state(a.last, at, ln.c, C, ln.live, h);
 }
 
-// The maps of all splits but the last: each slot takes a stretch of the split's
-// runs, and the slots' maps are joined in their order.
+// The maps of all splits but the last.
 template <typename T, bool WIDE, int GAIN>
 __global__ __launch_bounds__(kScanBlock) void k_recur_maps(RecurArgs a, RecurCut cut) {
     typedef Lane<V, true> L;
-    __shared__ float maps[L::kSlots][L::kLanes][2 * V];
+    __shared__ float maps[2][L::kWaves][L::kLanes][2 * V];
     const L ln(a, cut);
     const int64_t C = a.channels;
-    const int n = ln.t1 - ln.t0;
-    Product P[V];
-    float A[V], B[V];
-#pragma unroll
-    for (int j = 0; j < V; ++j) B[j] = 0.0f;
-    for (int t = 0; t < n; ++t) {
-        const int64_t s0 = ((int64_t)ln.t0 * L::kSlots + (int64_t)ln.slot * n + t) * kRun;
-        const Run r(a, s0, ln.count);
-        Part<T> x[kRun], g[kRun];
-        r.template load<T, WIDE>(ln.template at<const T>(a.g), a.g.st, ln.c, C, g);
-        r.template load<T, WIDE>(ln.template at<const T>(a.x), a.x.st, ln.c, C, x);
-        r.take_out(x);
-#pragma unroll
-        for (int i = 0; i < kRun; ++i)
-#pragma unroll
-            for (int j = 0; j < V; ++j) {
-                float q = gate_of(g[i].at(j));
-                if (!r.whole) q = i < r.left ? q : 0.0f;
-                P[j].take(q);
-                B[j] = advance<GAIN>(B[j], q, x[i].at(j));
-            }
-    }
-    const int col = threadIdx.x % L::kLanes;
-#pragma unroll
-    for (int j = 0; j < V; ++j) {
-        A[j] = P[j].gate();
-        maps[ln.slot][col][j] = A[j];
-        maps[ln.slot][col][V + j] = B[j];
-    }
-    __syncthreads();
-    if (ln.slot != 0 || !ln.live) return;
-    if (ln.split == 0) keep_entry(ln, a, cut, a.state);
-    for (int s = 1; s < L::kSlots; ++s)
+    SplitMap<V> all;
+    struct Pair {
+        Part<T> g[kRun], x[kRun];
+    };
+    auto load = [&](int t) {
+        Pair in;
+        const Run r(a, ((int64_t)t * L::kSlots + ln.slot) * kRun, ln.count);
+        ln.template load<T, WIDE>(a.g, r, t, C, in.g);
+        ln.template load<T, WIDE>(a.x, r, t, C, in.x);
+        return in;
+    };
+    for (int t = ln.t1 - 1; t >= ln.t0; --t) {
+        const Run r(a, ((int64_t)t * L::kSlots + ln.slot) * kRun, ln.count);
+        Pair in = load(t);
+        r.take_out(in.x);
+        float qa[V], qb[V];
 #pragma unroll
         for (int j = 0; j < V; ++j) {
-            B[j] = decay(B[j], maps[s][col][j]) + maps[s][col][V + j];
-            A[j] = joined(A[j], maps[s][col][j]);
-        }
-    float* out = cut.maps + 2 * ((int64_t)ln.split * a.batch * C + ln.state_at(a));
+            Product P;
+            float state = 0.0f;
 #pragma unroll
-    for (int j = 0; j < V; ++j)
-        if (ln.c + j < C) {
-            out[2 * j] = A[j];
-            out[2 * j + 1] = B[j];
+            for (int i = 0; i < kRun; ++i) {
+                const Step<T> step(in.g[i].at(j), r.whole || i < r.left);
+                step.onto(P);
+                state = step.template advance<GAIN>(state, in.x[i].at(j));
+            }
+            qa[j] = P.gate();
+            qb[j] = state;
         }
+        JoinMaps<V, true, false>::all(qa, qb, maps, t & 1);
+        if (ln.slot == 0) all.before(qa, qb);
+    }
+    if (ln.slot != 0 || !ln.live) return;
+    if (ln.split == 0) keep_entry(ln, a, cut, a.state);
+    all.store(ln, a, cut);
 }
 
 }  // namespace

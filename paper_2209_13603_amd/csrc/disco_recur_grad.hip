@@ -64,10 +64,10 @@ __global__ __launch_bounds__((Lane<V, SCAN>::kThreads)) void k_recur_grad(RecurA
         const int64_t run = (int64_t)t * L::kSlots + ln.slot;
         const Run r(a, run * kRun, ln.count);
         load_state(a.carries, (ln.b * runs + run) * C + ln.c, ln.c, C, ln.live && run < runs, in.before);
-        r.template load<T, WIDE>(ln.template at<const T>(a.g), a.g.st, ln.c, C, in.g);
-        r.template load<T, WIDE>(ln.template at<const T>(a.dy), a.dy.st, ln.c, C, in.dy);
-        if constexpr (Z) r.template load<T, WIDE>(ln.template at<const T>(a.z), a.z.st, ln.c, C, in.z);
-        r.template load<T, WIDE>(ln.template at<const T>(a.x), a.x.st, ln.c, C, in.x);
+        ln.template load<T, WIDE>(a.g, r, t, C, in.g);
+        ln.template load<T, WIDE>(a.dy, r, t, C, in.dy);
+        if constexpr (Z) ln.template load<T, WIDE>(a.z, r, t, C, in.z);
+        ln.template load<T, WIDE>(a.x, r, t, C, in.x);
         return in;
     };
     Inputs<T, Z> next;
@@ -150,6 +150,16 @@ __global__ __launch_bounds__((Lane<V, SCAN>::kThreads)) void k_recur_grad(RecurA
         const int64_t last = s0 + kRun - 1;
         T *to_x = ln.template at<T>(a.dx) + last * a.dx.st, *to_g = ln.template at<T>(a.dg) + last * a.dg.st,
           *to_z = ln.template at<T>(a.dz) + last * a.dz.st;
+        // (as the loads: a place that the workgroup shares, and the thread's from there)
+        const int64_t behind = (int64_t)(kRun - 1) * (int64_t)sizeof(T);
+        char *tile_x = nullptr, *tile_g = nullptr, *tile_z = nullptr;
+        uint32_t off_x = 0, off_g = 0, off_z = 0;
+        if constexpr (SCAN) {
+            tile_x = ln.template tile<T>(a.dx, t) + behind * a.dx.st;
+            tile_g = ln.template tile<T>(a.dg, t) + behind * a.dg.st;
+            tile_z = ln.template tile<T>(a.dz, t) + behind * a.dz.st;
+            off_x = ln.template offset<T>(a.dx), off_g = ln.template offset<T>(a.dg), off_z = ln.template offset<T>(a.dz);
+        }
         auto step = [&](int i, bool inside, bool stored, auto every) {
             float dx[V], dg[V], dz[V];
             const Pair p = before[i][threadIdx.x];
@@ -167,15 +177,24 @@ __global__ __launch_bounds__((Lane<V, SCAN>::kThreads)) void k_recur_grad(RecurA
                 mine[j] = decay(D, q[i][j]);
                 in.before[j] = p.v[j];
             }
-            if (stored) {
-                if (every || a.dx.p) store_part<T, V, WIDE>(to_x, ln.c, C, dx);
-                if (every || a.dg.p) store_part<T, V, WIDE>(to_g, ln.c, C, dg);
-                if constexpr (Z)
-                    if (every || a.dz.p) store_part<T, V, WIDE>(to_z, ln.c, C, dz);
+            if constexpr (SCAN && every) {
+                store_part<T, V, WIDE>((T*)(tile_x + off_x), ln.c, C, dx);
+                store_part<T, V, WIDE>((T*)(tile_g + off_g), ln.c, C, dg);
+                if constexpr (Z) store_part<T, V, WIDE>((T*)(tile_z + off_z), ln.c, C, dz);
+                move_all(tile_x, -a.dx.st * (int64_t)sizeof(T));
+                move_all(tile_g, -a.dg.st * (int64_t)sizeof(T));
+                if constexpr (Z) move_all(tile_z, -a.dz.st * (int64_t)sizeof(T));
+            } else {
+                if (stored) {
+                    if (every || a.dx.p) store_part<T, V, WIDE>(to_x, ln.c, C, dx);
+                    if (every || a.dg.p) store_part<T, V, WIDE>(to_g, ln.c, C, dg);
+                    if constexpr (Z)
+                        if (every || a.dz.p) store_part<T, V, WIDE>(to_z, ln.c, C, dz);
+                }
+                move(to_x, -a.dx.st);
+                move(to_g, -a.dg.st);
+                if constexpr (Z) move(to_z, -a.dz.st);
             }
-            move(to_x, -a.dx.st);
-            move(to_g, -a.dg.st);
-            if constexpr (Z) move(to_z, -a.dz.st);
             if (i % kGroup == 0) apart();
         };
         // (every: all gradients are asked for)
@@ -209,57 +228,40 @@ __global__ __launch_bounds__((Lane<V, SCAN>::kThreads)) void k_recur_grad(RecurA
 template <typename T, bool WIDE, bool Z>
 __global__ __launch_bounds__(kScanBlock) void k_recur_grad_maps(RecurArgs a, RecurCut cut) {
     typedef Lane<V, true> L;
-    __shared__ float maps[L::kSlots][L::kLanes][2 * V];
+    __shared__ float maps[2][L::kWaves][L::kLanes][2 * V];
     const L ln(a, cut, 1);
     const int64_t C = a.channels;
-    const int n = ln.t1 - ln.t0;
-    Product P[V];
-    float A[V], B[V];
-#pragma unroll
-    for (int j = 0; j < V; ++j) B[j] = 0.0f;
-    for (int t = n - 1; t >= 0; --t) {
-        const int64_t s0 = ((int64_t)ln.t0 * L::kSlots + (int64_t)ln.slot * n + t) * kRun;
-        const Run r(a, s0, ln.count);
+    SplitMap<V> all;
+    for (int t = ln.t0; t < ln.t1; ++t) {
+        const Run r(a, ((int64_t)t * L::kSlots + ln.slot) * kRun, ln.count);
         Part<T> g[kRun], dy[kRun], z[kRun];
-        r.template load<T, WIDE>(ln.template at<const T>(a.g), a.g.st, ln.c, C, g);
-        r.template load<T, WIDE>(ln.template at<const T>(a.dy), a.dy.st, ln.c, C, dy);
-        if constexpr (Z) r.template load<T, WIDE>(ln.template at<const T>(a.z), a.z.st, ln.c, C, z);
+        ln.template load<T, WIDE>(a.g, r, t, C, g);
+        ln.template load<T, WIDE>(a.dy, r, t, C, dy);
+        if constexpr (Z) ln.template load<T, WIDE>(a.z, r, t, C, z);
         r.take_out(dy);
         if constexpr (Z) r.take_out(z);
+        float qa[V], qb[V];
 #pragma unroll
-        for (int i = kRun - 1; i >= 0; --i)
+        for (int j = 0; j < V; ++j) {
+            Product P;
+            float D = 0.0f;
 #pragma unroll
-            for (int j = 0; j < V; ++j) {
+            for (int i = kRun - 1; i >= 0; --i) {
                 float q = gate_of(g[i].at(j));
                 if (!r.whole) q = i < r.left ? q : 0.0f;
                 const float d = dy[i].at(j);
-                P[j].take(q);
-                B[j] = decay(B[j] + (Z ? d * sigmoid(z[i].at(j)) : d), q);
+                P.take(q);
+                D = decay(D + (Z ? d * sigmoid(z[i].at(j)) : d), q);
             }
+            qa[j] = P.gate();
+            qb[j] = D;
+        }
+        JoinMaps<V, true, true>::all(qa, qb, maps, t & 1);
+        if (ln.slot == 0) all.before(qa, qb);
     }
-    const int col = threadIdx.x % L::kLanes;
-#pragma unroll
-    for (int j = 0; j < V; ++j) {
-        A[j] = P[j].gate();
-        maps[ln.slot][col][j] = A[j];
-        maps[ln.slot][col][V + j] = B[j];
-    }
-    __syncthreads();
-    if (ln.slot != L::kSlots - 1 || !ln.live) return;
+    if (ln.slot != 0 || !ln.live) return;
     if (ln.split == 1) keep_entry(ln, a, cut, a.dlast);
-    for (int s = L::kSlots - 2; s >= 0; --s)
-#pragma unroll
-        for (int j = 0; j < V; ++j) {
-            B[j] = decay(B[j], maps[s][col][j]) + maps[s][col][V + j];
-            A[j] = joined(A[j], maps[s][col][j]);
-        }
-    float* out = cut.maps + 2 * ((int64_t)ln.split * a.batch * C + ln.state_at(a));
-#pragma unroll
-    for (int j = 0; j < V; ++j)
-        if (ln.c + j < C) {
-            out[2 * j] = A[j];
-            out[2 * j + 1] = B[j];
-        }
+    all.store(ln, a, cut);
 }
 
 }  // namespace
