@@ -15,10 +15,15 @@ memory come from torch's allocator, on the stream that the call runs on.
 from __future__ import annotations
 
 import ctypes
+import struct
 from typing import NamedTuple
 
-from .attention import _Call, _dtype, _ref, _same_device
-from .disco import DropoutArgs, ResidualArgs, Rows, _check, _tensor, library
+from .attention import _Call, _dtype, _same_device
+from .disco import _check, library
+
+# disco_rows_t, disco_tensor_t, disco_dropout_t and disco_residual_t (all of whole 8-byte pieces).
+_ROWS, _TENSOR = struct.Struct("=Qii5q"), struct.Struct("=Qii4q")
+_DROPOUT, _RESIDUAL = struct.Struct("=d3Q"), struct.Struct("=ddii4Q")
 
 
 class Dropout(NamedTuple):
@@ -40,27 +45,64 @@ class ResidualGrads(NamedTuple):
     dnext_weight: object
 
 
-def _rows(t, name) -> Rows:
-    if t.dim() != 3:
-        raise ValueError("%s must be [batch, tokens, channels]" % name)
-    B, S, C = t.shape
-    sb, st, sc = t.stride()
-    if sc != 1 and C > 1:
-        raise ValueError("the last axis of %s must be contiguous" % name)
-    return Rows(t.data_ptr() or None, _dtype(t), 0, B, S, C, sb, st)
+class _Pack:
+    """The structures of one call, in one buffer (a ctypes object for each takes several times as long).  The
+    methods return the address of what they add, None for None."""
+    __slots__ = ("buffer", "base", "at")
 
+    def __init__(self):
+        self.buffer = ctypes.create_string_buffer(1024)
+        self.base = ctypes.addressof(self.buffer)
+        self.at = 0
 
-def _dropout(d, first):
-    import torch
-    if d is None:
-        return None
-    address = None
-    if d.counter is not None:
-        if d.counter.dtype != torch.int64 or d.counter.numel() != 1:
-            raise ValueError("counter must be one torch.int64")
-        _same_device(first, d.counter)
-        address = d.counter.data_ptr()
-    return DropoutArgs(d.p, d.seed & 0xFFFFFFFFFFFFFFFF, d.offset & 0xFFFFFFFFFFFFFFFF, address)
+    def _add(self, form, *values):
+        at = self.at
+        form.pack_into(self.buffer, at, *values)
+        self.at = at + form.size
+        return self.base + at
+
+    def rows(self, t, name):
+        if t is None:
+            return None
+        shape = t.shape
+        if len(shape) != 3:
+            raise ValueError("%s must be [batch, tokens, channels]" % name)
+        B, S, C = shape
+        sb, st, sc = t.stride()
+        if sc != 1 and C > 1:
+            raise ValueError("the last axis of %s must be contiguous" % name)
+        at = self.at
+        _ROWS.pack_into(self.buffer, at, t.data_ptr(), _dtype(t), 0, B, S, C, sb, st)
+        self.at = at + 56
+        return self.base + at
+
+    def weight(self, t, name):
+        if t is None:
+            return None
+        shape = t.shape
+        if not 1 <= len(shape) <= 2 or not t.is_contiguous():
+            raise ValueError("%s must be [channels] or [batch, channels], contiguous" % name)
+        at = self.at
+        _TENSOR.pack_into(self.buffer, at, t.data_ptr(), _dtype(t), len(shape), shape[0], shape[-1], 0, 0)
+        self.at = at + 48
+        return self.base + at
+
+    def dropout(self, d, first):
+        import torch
+        if d is None:
+            return None
+        counter = 0
+        if d.counter is not None:
+            if d.counter.dtype != torch.int64 or d.counter.numel() != 1:
+                raise ValueError("counter must be one torch.int64")
+            _same_device(first, d.counter)
+            counter = d.counter.data_ptr()
+        return self._add(_DROPOUT, d.p, d.seed & 0xFFFFFFFFFFFFFFFF, d.offset & 0xFFFFFFFFFFFFFFFF, counter)
+
+    def residual(self, first, post_norm, post_weight, gate, next_weight, scale, eps, dropout):
+        at = [self.weight(w, name) or 0
+              for w, name in ((post_weight, "post_weight"), (gate, "gate"), (next_weight, "next_weight"))]
+        return self._add(_RESIDUAL, scale, eps, 1 if post_norm else 0, 0, *at, self.dropout(dropout, first) or 0)
 
 
 def dropout(x, how, y=None, stream=None):
@@ -73,7 +115,8 @@ def dropout(x, how, y=None, stream=None):
     _same_device(x, y)
     if y.shape != x.shape:
         raise ValueError("x and y must have the same shape")
-    args = _dropout(how, x)
+    pack = _Pack()
+    args = pack.dropout(how, x)
     if x.dim() == 3:
         tx, ty = x, y
     else:
@@ -82,20 +125,8 @@ def dropout(x, how, y=None, stream=None):
         last = x.shape[-1] if x.dim() else 1
         tx, ty = (t.view(1, x.numel() // last if last else 0, last) for t in (x, y))
     if x.numel():
-        _check(library().disco_dropout(_rows(tx, "x"), args, _rows(ty, "y"), call.handle))
+        _check(library().disco_dropout(pack.rows(tx, "x"), args, pack.rows(ty, "y"), call.handle))
     return y
-
-
-def _residual(first, post_norm, post_weight, gate, next_weight, scale, eps, dropout):
-    """(disco_residual_t, the tensors of the weights): what it points to lives as long as it does."""
-    _same_device(first, post_weight, gate, next_weight)
-    tensors = [_tensor(w) if w is not None else None for w in (post_weight, gate, next_weight)]
-    for w in (post_weight, gate, next_weight):
-        if w is not None and not w.is_contiguous():
-            raise ValueError("weights must be contiguous")
-    drop = _dropout(dropout, first)
-    ptr = [ctypes.pointer(t) if t is not None else None for t in (*tensors, drop)]
-    return ResidualArgs(scale, eps, int(post_norm), 0, *ptr), tensors
 
 
 def residual_norm(x, f, post_norm=False, post_weight=None, gate=None, next_weight=None, scale=1.0, eps=1e-6, dropout=None,
@@ -114,10 +145,11 @@ def residual_norm(x, f, post_norm=False, post_weight=None, gate=None, next_weigh
     if want_y and y is None:
         y = call.like(f)
     h, y = h if want_h else None, y if want_y else None
-    _same_device(f, x, h, y)
-    args, keep = _residual(f, post_norm, post_weight, gate, next_weight, scale, eps, dropout)
-    rows = [_rows(t, name) if t is not None else None for t, name in ((x, "x"), (f, "f"), (h, "h"), (y, "y"))]
-    _check(library().disco_residual_norm(rows[0], rows[1], args, rows[2], rows[3], call.handle))
+    _same_device(f, x, h, y, post_weight, gate, next_weight)
+    pack = _Pack()
+    args = pack.residual(f, post_norm, post_weight, gate, next_weight, scale, eps, dropout)
+    _check(library().disco_residual_norm(pack.rows(x, "x"), pack.rows(f, "f"), args, pack.rows(h, "h"), pack.rows(y, "y"),
+                                         call.handle))
     return h, y
 
 
@@ -135,15 +167,15 @@ def residual_norm_backward(x, f, dh, dy, post_norm=False, post_weight=None, gate
         df = None
     elif df is None:
         df = call.like(f)
-    _same_device(f, x, dh, dy, dx, df)
-    args, keep = _residual(f, post_norm, post_weight, gate, next_weight, scale, eps, dropout)
+    _same_device(f, x, dh, dy, dx, df, post_weight, gate, next_weight)
+    pack = _Pack()
+    args = pack.residual(f, post_norm, post_weight, gate, next_weight, scale, eps, dropout)
+    at_f = pack.rows(f, "f")
     dw = [call.like(w) if w is not None and want_weights else None for w in (post_weight, gate, next_weight)]
-    rows = [_rows(t, name) if t is not None else None
-            for t, name in ((x, "x"), (f, "f"), (dh, "dh"), (dy, "dy"), (dx, "dx"), (df, "df"))]
-    sums = [_tensor(t) if t is not None else None for t in dw]
-    ws = (None, None, 0)
+    keep, ws, n = (None, None, 0)
     if any(t is not None for t in dw):
-        ws = call.workspace("disco_residual_norm_workspace", rows[1], args)
-    _check(library().disco_residual_norm_backward(rows[0], rows[1], args, rows[2], rows[3], rows[4], rows[5], *map(_ref, sums),
-                                                  ws[1], ws[2], call.handle))
+        keep, ws, n = call.workspace("disco_residual_norm_workspace", at_f, args)
+    _check(library().disco_residual_norm_backward(
+        pack.rows(x, "x"), at_f, args, pack.rows(dh, "dh"), pack.rows(dy, "dy"), pack.rows(dx, "dx"), pack.rows(df, "df"),
+        pack.weight(dw[0], "dpost_weight"), pack.weight(dw[1], "dgate"), pack.weight(dw[2], "dnext_weight"), ws, n, call.handle))
     return ResidualGrads(dx, df, *dw)

@@ -224,7 +224,7 @@ def library(path: str = None) -> ctypes.CDLL:
     lib.disco_last_error.argtypes = []
     lib.disco_last_error.restype = ctypes.c_char_p
     V, Z, I32, S = ctypes.c_void_p, ctypes.c_size_t, ctypes.c_int32, P(ctypes.c_size_t)
-    H, T, R, A, W = P(Heads), P(Tensor), P(RotationArgs), P(AttentionArgs), P(Rows)
+    H, T, R, A = P(Heads), P(Tensor), P(RotationArgs), P(AttentionArgs)
     token_calls = {
         "disco_norm_rotate": [H, I32, T, ctypes.c_double, R, H, V],
         "disco_norm_rotate_backward": [H, I32, T, ctypes.c_double, R, H, H, T, V, Z, V],
@@ -235,13 +235,14 @@ def library(path: str = None) -> ctypes.CDLL:
         # the tensor arrays of many gradients come as addresses
         "disco_gradient_clip": [I32, V, V, ctypes.c_double, ctypes.c_double, V, V, Z, V],
         "disco_gradient_clip_workspace": [I32, V, S],
-        "disco_dropout": [W, P(DropoutArgs), W, V],
-        "disco_residual_norm": [W, W, P(ResidualArgs), W, W, V],
-        "disco_residual_norm_backward": [W, W, P(ResidualArgs), W, W, W, W, T, T, T, V, Z, V],
-        "disco_residual_norm_workspace": [W, P(ResidualArgs), S],
-        "disco_gated_recurrence": [W, W, W, P(RecurrenceArgs), V, W, V, V, V, Z, V],
-        "disco_gated_recurrence_backward": [W, W, W, P(RecurrenceArgs), V, W, V, W, W, W, V, V, Z, V],
-        "disco_gated_recurrence_workspace": [W, S],
+        # (these take their structures as addresses: blocks.py packs those of a call into one buffer)
+        "disco_dropout": [V] * 4,
+        "disco_residual_norm": [V] * 6,
+        "disco_residual_norm_backward": [V] * 11 + [Z, V],
+        "disco_residual_norm_workspace": [V, V, S],
+        "disco_gated_recurrence": [V] * 9 + [Z, V],
+        "disco_gated_recurrence_backward": [V] * 12 + [Z, V],
+        "disco_gated_recurrence_workspace": [V, S],
     }
     for name, args in token_calls.items():
         getattr(lib, name).argtypes = args

@@ -12,11 +12,14 @@ the stream that the call runs on.
 """
 from __future__ import annotations
 
+import struct
 from typing import NamedTuple
 
-from .attention import _Call, _ref, _same_device
-from .blocks import _rows
-from .disco import RecurrenceArgs, _check, library
+from .attention import _Call, _same_device
+from .blocks import _Pack
+from .disco import _check, library
+
+_RECURRENCE = struct.Struct("=iiQ")  # disco_recurrence_t
 
 GAINS = {"mean": 0, "power": 1, "one": 2}
 RUN = 16  # tokens between two states that are kept for the gradients
@@ -29,17 +32,17 @@ class RecurrenceGrads(NamedTuple):
     dstate: object
 
 
-def _options(x, lengths, gain):
+def _options(pack, x, lengths, gain):
     import torch
-    address = None
+    address = 0
     if lengths is not None:
         if lengths.dtype != torch.int32 or tuple(lengths.shape) != (x.shape[0],) or not lengths.is_contiguous():
             raise ValueError("lengths must be torch.int32 [batch], contiguous")
         _same_device(x, lengths)
-        address = lengths.data_ptr() or None
+        address = lengths.data_ptr()
     if gain not in GAINS:
         raise ValueError("gain must be one of %s" % ", ".join(GAINS))
-    return RecurrenceArgs(GAINS[gain], 0, address)
+    return pack._add(_RECURRENCE, GAINS[gain], 0, address)
 
 
 def _floats(x, t, name, shape):
@@ -72,12 +75,12 @@ def gated_recurrence(x, gate, out_gate=None, state=None, lengths=None, gain="mea
     if state_out is None:
         state_out = call.empty((B, C), torch.float32)
     carries = call.empty((B, -(-T // RUN), C), torch.float32) if return_carries else None
-    options = _options(x, lengths, gain)
-    rx = _rows(x, "x")
-    keep, ws, n = call.workspace("disco_gated_recurrence_workspace", rx)
+    pack = _Pack()
+    options, at_x = _options(pack, x, lengths, gain), pack.rows(x, "x")
+    keep, ws, n = call.workspace("disco_gated_recurrence_workspace", at_x)
     _check(library().disco_gated_recurrence(
-        rx, _rows(gate, "gate"), _ref(_rows(out_gate, "out_gate") if out_gate is not None else None), options,
-        _floats(x, state, "state", (B, C)), _rows(y, "y"), _floats(x, state_out, "state_out", (B, C)),
+        at_x, pack.rows(gate, "gate"), pack.rows(out_gate, "out_gate"), options, _floats(x, state, "state", (B, C)),
+        pack.rows(y, "y"), _floats(x, state_out, "state_out", (B, C)),
         carries.data_ptr() or None if carries is not None else None, ws, n, call.handle))
     return (y, state_out, carries) if return_carries else (y, state_out)
 
@@ -101,13 +104,12 @@ def gated_recurrence_backward(x, gate, carries, dy, out_gate=None, lengths=None,
     if want_dstate and dstate_out is None:
         dstate_out = call.empty((B, C), torch.float32)
     _same_device(x, gate, out_gate, carries, dy, dx, dgate, dout_gate)
-    options = _options(x, lengths, gain)
-    rows = [_rows(t, name) if t is not None else None
-            for t, name in ((x, "x"), (gate, "gate"), (out_gate, "out_gate"), (dy, "dy"), (dx, "dx"), (dgate, "dgate"),
-                            (dout_gate, "dout_gate"))]
-    keep, ws, n = call.workspace("disco_gated_recurrence_workspace", rows[0])
+    pack = _Pack()
+    options, at_x = _options(pack, x, lengths, gain), pack.rows(x, "x")
+    keep, ws, n = call.workspace("disco_gated_recurrence_workspace", at_x)
     _check(library().disco_gated_recurrence_backward(
-        *rows[:3], options, _floats(x, carries, "carries", (B, -(-T // RUN), C)), rows[3],
-        _floats(x, dstate, "dstate", (B, C)), *rows[4:],
+        at_x, pack.rows(gate, "gate"), pack.rows(out_gate, "out_gate"), options,
+        _floats(x, carries, "carries", (B, -(-T // RUN), C)), pack.rows(dy, "dy"), _floats(x, dstate, "dstate", (B, C)),
+        pack.rows(dx, "dx"), pack.rows(dgate, "dgate"), pack.rows(dout_gate, "dout_gate"),
         _floats(x, dstate_out, "dstate_out", (B, C)) if want_dstate else None, ws, n, call.handle))
     return RecurrenceGrads(dx, dgate, dout_gate, dstate_out if want_dstate else None)

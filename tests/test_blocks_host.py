@@ -184,16 +184,16 @@ def test_gated_recurrence_backward_refuses():
 
 def test_workspace_sizes_are_host_arithmetic():
     lib, n = disco.library(), ctypes.c_size_t()
-    assert lib.disco_gated_recurrence_workspace(rows(1), n) == 0 and n.value == 0
-    assert lib.disco_gated_recurrence_workspace(rows(1, tokens=100000), n) == 0 and n.value > 0  # one long series: splits
-    assert lib.disco_gated_recurrence_workspace(rows(1, tokens=24, batch=100000), n) == 0 and n.value == 0
-    assert lib.disco_gated_recurrence_workspace(rows(1), None) == INVALID
-    assert lib.disco_residual_norm_workspace(rows(1), None, n) == 0 and n.value == 0
+    assert lib.disco_gated_recurrence_workspace(ref(rows(1)), n) == 0 and n.value == 0
+    assert lib.disco_gated_recurrence_workspace(ref(rows(1, tokens=100000)), n) == 0 and n.value > 0  # one long series: splits
+    assert lib.disco_gated_recurrence_workspace(ref(rows(1, tokens=24, batch=100000)), n) == 0 and n.value == 0
+    assert lib.disco_gated_recurrence_workspace(ref(rows(1)), None) == INVALID
+    assert lib.disco_residual_norm_workspace(ref(rows(1)), None, n) == 0 and n.value == 0
     opt = options(gate=tensor(8))
-    assert lib.disco_residual_norm_workspace(rows(1), opt, n) == 0 and n.value > 0
+    assert lib.disco_residual_norm_workspace(ref(rows(1)), ref(opt), n) == 0 and n.value > 0
     shared = n.value
     opt = options(gate=tensor(2, 8))
-    assert lib.disco_residual_norm_workspace(rows(1), opt, n) == 0 and n.value > shared
+    assert lib.disco_residual_norm_workspace(ref(rows(1)), ref(opt), n) == 0 and n.value > shared
 
 
 def test_generator_gives_its_published_values():
