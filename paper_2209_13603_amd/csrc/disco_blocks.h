@@ -107,6 +107,20 @@ __device__ __forceinline__ bool stays(const Words& r, int i, uint32_t out) {
     return (i % 2 ? r.w[i / 2] >> 16 : r.w[i / 2] & 0xffffu) >= out;
 }
 
+// Pieces of rows at any address of their entries' alignment: the memory takes these
+// loads and stores whole (entry by entry, rows of 167 in bf16 took three times as long).
+typedef uint32_t Any4 __attribute__((ext_vector_type(4), aligned(2)));
+typedef uint32_t Any2 __attribute__((ext_vector_type(2), aligned(2)));
+typedef uint32_t Any1 __attribute__((aligned(2)));
+typedef float Any4f __attribute__((ext_vector_type(4), aligned(4)));
+typedef float Any2f __attribute__((ext_vector_type(2), aligned(4)));
+
+// One of two values (of the values, not of their places).
+template <typename X>
+__device__ __forceinline__ X pick(bool first, X a, X b) {
+    return first ? a : b;
+}
+
 // Eight entries of a row as they lie in memory: bf16 two in a register (as single
 // values, once branches meet, they take one each).
 template <typename T>
@@ -127,18 +141,41 @@ struct Raw<__bf16> {
 #pragma unroll
         for (int i = 0; i < kChunk / 2; ++i) asm("" : "+v"(w[i]));
     }
-    // Entries i .. i + W - 1
-    template <int W>
-    __device__ __forceinline__ void load(int i, const __bf16* p) {
-        if constexpr (W == 1) {
-            const uint32_t v = *(const uint16_t*)p;
-            w[i / 2] = i % 2 ? (w[i / 2] & 0xffffu) | v << 16 : (w[i / 2] & 0xffff0000u) | v;
-        } else {
-            typedef uint32_t U __attribute__((ext_vector_type(W / 2)));
-            const U v = *(const U*)p;
+    __device__ __forceinline__ void load(const __bf16* p) {
+        const Any4 v = *(const Any4*)p;
 #pragma unroll
-            for (int j = 0; j < W / 2; ++j) w[i / 2 + j] = v[j];
+        for (int i = 0; i < 4; ++i) w[i] = v[i];
+    }
+    // The first `left` < 8 entries: pieces of four, two and one.
+    __device__ __forceinline__ void load(const __bf16* p, int left) {
+        uint32_t four[2] = {0u, 0u}, two = 0u, one = 0u;
+        if (left & 4) {
+            const Any2 v = *(const Any2*)p;
+            four[0] = v[0], four[1] = v[1];
         }
+        if (left & 2) two = *(const Any1*)(p + (left & 4));
+        if (left & 1) one = *(const uint16_t*)(p + (left & 6));
+        const bool q = left & 4, h = left & 2;
+        const uint32_t a = pick(h, two, one), b = pick(h, one, 0u);
+        w[0] = pick(q, four[0], a);
+        w[1] = pick(q, four[1], b);
+        w[2] = pick(q, a, 0u);
+        w[3] = pick(q, b, 0u);
+    }
+    __device__ __forceinline__ void pack(const float (&e)[kChunk]) {
+#pragma unroll
+        for (int i = 0; i < kChunk / 2; ++i) {
+            typedef float F __attribute__((ext_vector_type(2)));
+            typedef __bf16 B __attribute__((ext_vector_type(2)));
+            w[i] = __builtin_bit_cast(uint32_t, __builtin_convertvector((F{e[2 * i], e[2 * i + 1]}), B));
+        }
+    }
+    __device__ __forceinline__ void store(__bf16* p) const { *(Any4*)p = Any4{w[0], w[1], w[2], w[3]}; }
+    __device__ __forceinline__ void store(__bf16* p, int left) const {
+        if (left & 4) *(Any2*)p = Any2{w[0], w[1]};
+        const uint32_t a = pick<uint32_t>(left & 4, w[2], w[0]), b = pick<uint32_t>(left & 4, w[3], w[1]);
+        if (left & 2) *(Any1*)(p + (left & 4)) = a;
+        if (left & 1) *(uint16_t*)(p + (left & 6)) = (uint16_t)pick<uint32_t>(left & 2, b, a);
     }
 };
 template <>
@@ -150,36 +187,61 @@ struct Raw<float> {
         for (int i = 0; i < kChunk; ++i) w[i] = v;
     }
     __device__ __forceinline__ void anew() {}
-    template <int W>
-    __device__ __forceinline__ void load(int i, const float* p) {
-        typedef float U __attribute__((ext_vector_type(W)));
-        const U v = *(const U*)p;
+    __device__ __forceinline__ void load(const float* p) {
+        const Any4f u = *(const Any4f*)p, v = *(const Any4f*)(p + 4);
 #pragma unroll
-        for (int j = 0; j < W; ++j) w[i + j] = v[j];
+        for (int i = 0; i < 4; ++i) w[i] = u[i], w[4 + i] = v[i];
+    }
+    __device__ __forceinline__ void load(const float* p, int left) {
+        float four[4] = {0.0f}, two[2] = {0.0f}, one = 0.0f;
+        if (left & 4) {
+            const Any4f v = *(const Any4f*)p;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) four[i] = v[i];
+        }
+        if (left & 2) two[0] = p[left & 4], two[1] = p[(left & 4) + 1];
+        if (left & 1) one = p[left & 6];
+        const bool q = left & 4, h = left & 2;
+        const float r[4] = {pick(h, two[0], one), pick(h, two[1], 0.0f), pick(h, one, 0.0f), 0.0f};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            w[i] = pick(q, four[i], r[i]);
+            w[4 + i] = pick(q, r[i], 0.0f);
+        }
+    }
+    __device__ __forceinline__ void pack(const float (&e)[kChunk]) {
+#pragma unroll
+        for (int i = 0; i < kChunk; ++i) w[i] = e[i];
+    }
+    __device__ __forceinline__ void store(float* p) const {
+        *(Any4f*)p = Any4f{w[0], w[1], w[2], w[3]};
+        *(Any4f*)(p + 4) = Any4f{w[4], w[5], w[6], w[7]};
+    }
+    __device__ __forceinline__ void store(float* p, int left) const {
+        if (left & 4) *(Any4f*)p = Any4f{w[0], w[1], w[2], w[3]};
+        float r[3];
+#pragma unroll
+        for (int i = 0; i < 3; ++i) r[i] = pick<float>(left & 4, w[4 + i], w[i]);
+        if (left & 2) p[left & 4] = r[0], p[(left & 4) + 1] = r[1];
+        if (left & 1) p[left & 6] = pick<float>(left & 2, r[2], r[0]);
     }
 };
-// The first eight entries at p, of which `left` are there (perhaps none), W at a time: left and
-// the address are multiples of W entries.  Zeros beyond.
-template <typename T, int W>
+// The first eight entries at p, of which `left` are there (perhaps none): zeros beyond.  EIGHTS:
+// rows are of whole chunks.
+template <typename T, bool EIGHTS>
 __device__ __forceinline__ Raw<T> load_raw(const T* p, int left) {
     Raw<T> r;
     r.fill(0.0f);
-#pragma unroll
-    for (int i = 0; i < kChunk; i += W)
-        if (i < left) r.template load<W>(i, p + i);
+    if (left >= kChunk) r.load(p);
+    else if (!EIGHTS && left > 0) r.load(p, left);
     return r;
 }
-template <typename T, int W>
+template <typename T, bool EIGHTS>
 __device__ __forceinline__ void store_raw(T* p, int left, const float (&e)[kChunk]) {
-    typedef float F __attribute__((ext_vector_type(W)));
-    typedef T V __attribute__((ext_vector_type(W)));
-#pragma unroll
-    for (int i = 0; i < kChunk; i += W) {
-        F f;
-#pragma unroll
-        for (int j = 0; j < W; ++j) f[j] = e[i + j];
-        if (i < left) *(V*)(p + i) = __builtin_convertvector(f, V);
-    }
+    Raw<T> r;
+    r.pack(e);
+    if (left >= kChunk) r.store(p);
+    else if (!EIGHTS && left > 0) r.store(p, left);
 }
 
 // Sum over the 2^k neighbouring lanes of a row, in each of them: exchanges within
@@ -204,11 +266,6 @@ __device__ __forceinline__ float lanes_sum(float v, int lanes) {
         v = __uint_as_float(r[0]) + __uint_as_float(r[1]);
     }
     return v;
-}
-
-// Host: whether rows of a tensor are read or written w entries at a time.
-inline bool rows_fit(const Rows& t, int w, size_t elem) {
-    return !t.p || ((uintptr_t)t.p % (w * elem) == 0 && t.sb % w == 0 && t.st % w == 0);
 }
 
 }  // namespace disco

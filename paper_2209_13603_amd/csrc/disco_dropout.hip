@@ -27,7 +27,7 @@ struct Shape {
     uint32_t all;            // chunks of all rows
 };
 
-template <typename T, int W>
+template <typename T, bool EIGHTS>
 __global__ __launch_bounds__(kThreads) void k_dropout(DropoutArgs a, Shape s) {
     const uint32_t i = group_index() * kThreads + threadIdx.x;
     if (i >= s.all) return;
@@ -35,17 +35,17 @@ __global__ __launch_bounds__(kThreads) void k_dropout(DropoutArgs a, Shape s) {
     const uint32_t b = s.tokens.quotient(row), tok = row - b * s.tokens.d;
     const int64_t c = (int64_t)chunk * kChunk;
     const int left = (int)min((int64_t)kChunk, a.channels - c);
-    const Raw<T> x = load_raw<T, W>((const T*)a.x.p + b * a.x.sb + tok * a.x.st + c, left);
+    const Raw<T> x = load_raw<T, EIGHTS>((const T*)a.x.p + b * a.x.sb + tok * a.x.st + c, left);
     const Words r = drop_words(a.drop, drop_offset(a.drop), row, chunk);
     float e[kChunk];
 #pragma unroll
     for (int j = 0; j < kChunk; ++j) e[j] = stays(r, j, a.drop.out) ? x.at(j) * a.drop.factor : 0.0f;
-    store_raw<T, W>((T*)a.y.p + b * a.y.sb + tok * a.y.st + c, left, e);
+    store_raw<T, EIGHTS>((T*)a.y.p + b * a.y.sb + tok * a.y.st + c, left, e);
 }
 
-template <typename T, int W>
+template <typename T, bool EIGHTS>
 hipError_t launch(const DropoutArgs& a, const Shape& s) {
-    hipLaunchKernelGGL((k_dropout<T, W>), grid_dim((s.all + kThreads - 1) / kThreads), dim3(kThreads), 0, a.stream, a, s);
+    hipLaunchKernelGGL((k_dropout<T, EIGHTS>), grid_dim((s.all + kThreads - 1) / kThreads), dim3(kThreads), 0, a.stream, a, s);
     return hipGetLastError();
 }
 
@@ -57,15 +57,11 @@ hipError_t launch_dropout(const DropoutArgs& a) {
     s.chunks = divisor((uint32_t)chunks);
     s.tokens = divisor((uint32_t)a.tokens);
     s.all = (uint32_t)(chunks * a.batch * a.tokens);
-    const size_t e = a.bf16 ? 2 : 4;
-    int w = a.bf16 ? 8 : 4;
-    while (w > 1 && (a.channels % w || !rows_fit(a.x, w, e) || !rows_fit(a.y, w, e))) w /= 2;
     const int tk = timing_begin("dropout", a.stream);
+    const bool eights = a.channels % kChunk == 0;
     hipError_t err;
-    if (a.bf16)
-        err = w == 8 ? launch<__bf16, 8>(a, s) : w == 4 ? launch<__bf16, 4>(a, s) : w == 2 ? launch<__bf16, 2>(a, s) : launch<__bf16, 1>(a, s);
-    else
-        err = w == 4 ? launch<float, 4>(a, s) : w == 2 ? launch<float, 2>(a, s) : launch<float, 1>(a, s);
+    if (a.bf16) err = eights ? launch<__bf16, true>(a, s) : launch<__bf16, false>(a, s);
+    else err = eights ? launch<float, true>(a, s) : launch<float, false>(a, s);
     timing_end(tk, a.stream);
     return err;
 }

@@ -35,7 +35,7 @@ constexpr int kRecurChannels = 2;  // of a thread: see Part
 // otherwise a thread walks all runs of its V channels by itself.
 struct RecurCut {
     uint32_t columns;   // groups of V channels
-    uint32_t blocks;    // of 64 channels (scan)
+    uint32_t blocks;    // of 32 groups, over all items (scan)
     uint32_t groups;    // workgroups
     int32_t splits, tiles;  // tiles of all runs; a split takes every tiles / splits
     Divisor by_columns;
@@ -143,37 +143,38 @@ struct Part<float> {
     __device__ __forceinline__ void clear_unless(bool in) { v[0] = in ? v[0] : 0.0f, v[1] = in ? v[1] : 0.0f; }
     __device__ __forceinline__ void anew() {}
 };
-// Channels c, c + 1 of a row of n, in one load where WIDE.
-template <typename T, bool WIDE>
-__device__ __forceinline__ Part<T> load_part(const T* p, int64_t c, int64_t n) {
+// A thread's two channels of a row.  EVEN: rows have an even number of channels, and the
+// two go together; otherwise one by one, the second `next` entries from the first: 1, or 0
+// in the thread of the last channel, which is alone.
+template <typename T, bool EVEN>
+__device__ __forceinline__ Part<T> load_part(const T* p, int next) {
     Part<T> r;
-    if constexpr (WIDE && sizeof(T) == 2) {
-        r.u = *(const uint32_t*)p;
-    } else if constexpr (WIDE) {
-        const float2 v = *(const float2*)p;
-        r.v[0] = v.x, r.v[1] = v.y;
-    } else if constexpr (sizeof(T) == 2) {
-        const uint16_t* q = (const uint16_t*)p;
-        r.u = c < n ? q[0] : 0u;
-        if (c + 1 < n) r.u |= (uint32_t)q[1] << 16;
+    if constexpr (sizeof(T) == 2) {
+        if constexpr (EVEN) {
+            r.u = *(const Any1*)p;
+        } else {
+            const uint32_t lo = *(const uint16_t*)p, hi = *(const uint16_t*)(p + next);
+            r.u = lo | hi << 16;
+        }
+    } else if constexpr (EVEN) {
+        const Any2f v = *(const Any2f*)p;
+        r.v[0] = v[0], r.v[1] = v[1];
     } else {
-        r.v[0] = c < n ? p[0] : 0.0f;
-        r.v[1] = c + 1 < n ? p[1] : 0.0f;
+        r.v[0] = p[0], r.v[1] = p[next];
     }
     return r;
 }
-template <typename T, int V, bool WIDE>
-__device__ __forceinline__ void store_part(T* p, int64_t c, int64_t n, const float (&e)[V]) {
-    typedef T Vec __attribute__((ext_vector_type(V)));
-    if constexpr (WIDE) {
-        Vec v;
-#pragma unroll
-        for (int j = 0; j < V; ++j) v[j] = (T)e[j];
-        *(Vec*)p = v;
+template <typename T, bool EVEN>
+__device__ __forceinline__ void store_part(T* p, int next, const float (&v)[2]) {
+    if constexpr (!EVEN) {
+        p[0] = (T)v[0];
+        p[next] = (T)(next ? v[1] : v[0]);
+    } else if constexpr (sizeof(T) == 2) {
+        typedef float F __attribute__((ext_vector_type(2)));
+        typedef __bf16 B __attribute__((ext_vector_type(2)));
+        *(Any1*)p = __builtin_bit_cast(uint32_t, __builtin_convertvector((F{v[0], v[1]}), B));
     } else {
-#pragma unroll
-        for (int j = 0; j < V; ++j)
-            if (c + j < n) p[j] = (T)e[j];
+        *(Any2f*)p = Any2f{v[0], v[1]};
     }
 }
 
@@ -223,21 +224,21 @@ struct Run {
     __device__ __forceinline__ bool stores(int i) const { return whole || __any(i < steps); }
     // Of whole runs `from`, a workgroup's first step, goes on through scalar registers, `off` (bytes) is
     // the thread's place from there (scan); otherwise p is its own.
-    template <typename T, bool WIDE, bool SCAN>
-    __device__ __forceinline__ void load(const T* p, const char* from, uint32_t off, int64_t st, int64_t c, int64_t n,
+    template <typename T, bool EVEN, bool SCAN>
+    __device__ __forceinline__ void load(const T* p, const char* from, uint32_t off, int64_t st, int next,
                                          Part<T> (&v)[kRun]) const {
         if (whole) {
             if constexpr (SCAN) {
 #pragma unroll
                 for (int i = 0; i < kRun; ++i) {
-                    v[i] = load_part<T, WIDE>((const T*)(from + off), c, n);
+                    v[i] = load_part<T, EVEN>((const T*)(from + off), next);
                     move_all(from, st * (int64_t)sizeof(T));
                 }
             } else {
                 p += first * st;
 #pragma unroll
                 for (int i = 0; i < kRun; ++i) {
-                    v[i] = load_part<T, WIDE>(p, c, n);
+                    v[i] = load_part<T, EVEN>(p, next);
                     move(p, st);
                 }
             }
@@ -249,7 +250,7 @@ struct Run {
             if (__any(k < left)) {
 #pragma unroll
                 for (int i = k; i < k + kGroup; ++i) {
-                    v[i] = load_part<T, WIDE>(p, c, n);
+                    v[i] = load_part<T, EVEN>(p, next);
                     move(p, i + 1 < left ? st : 0);
                 }
             } else {
@@ -284,35 +285,37 @@ struct Lane {
     static constexpr int kSlots = SCAN ? kThreads / kLanes : 1; // runs of a tile
     static constexpr int kInWave = 64 / kLanes;                 // of them in a wave
     static constexpr int kWaves = kThreads / 64;
-    uint32_t b;
+    uint32_t b, b0;  // batch item; of the workgroup's first thread (scan)
     int64_t c;       // first channel
+    int next;        // see load_part
     int slot, split;
     bool live;       // has channels
     int64_t count;   // steps of this item
     int t0, t1;      // tiles
     __device__ __forceinline__ Lane(const RecurArgs& a, const RecurCut& cut, int first_split = 0) {
+        const uint32_t all = cut.columns * a.batch;
+        uint32_t column;
         if constexpr (SCAN) {
-            uint32_t id = group_index();
-            const uint32_t block = id % cut.blocks;
-            id /= cut.blocks;
-            b = id % a.batch;
-            split = first_split + (int)(id / a.batch);
+            const uint32_t id = group_index(), block = id % cut.blocks;
+            split = first_split + (int)(id / cut.blocks);
             slot = threadIdx.x / kLanes;
-            const uint32_t column = block * kLanes + threadIdx.x % kLanes;
-            live = column < cut.columns && split < cut.splits;
-            c = (int64_t)column * V;
+            b0 = cut.by_columns.quotient(block * kLanes);
+            column = block * kLanes + threadIdx.x % kLanes;
+            live = column < all && split < cut.splits;
             t0 = (int)((int64_t)cut.tiles * split / cut.splits);
             t1 = split < cut.splits ? (int)((int64_t)cut.tiles * (split + 1) / cut.splits) : t0;
         } else {
-            const uint32_t id = group_index() * kThreads + threadIdx.x;
-            live = id < cut.columns * a.batch;
-            b = live ? cut.by_columns.quotient(id) : 0;
-            c = (int64_t)((live ? id : 0) - b * cut.columns) * V;
+            column = group_index() * kThreads + threadIdx.x;
+            live = column < all;
             slot = split = 0;
             t0 = 0;
             t1 = live ? cut.tiles : 0;
         }
-        if (!live) c = 0;
+        column = min(column, all - 1);  // threads without channels read the last ones and write nothing
+        b = cut.by_columns.quotient(column);
+        if constexpr (!SCAN) b0 = b;
+        c = (int64_t)(column - b * cut.columns) * V;
+        next = c + 1 < a.channels ? 1 : 0;
         count = a.steps;
         if (a.lengths) {
             const int64_t n = a.lengths[b];
@@ -323,25 +326,25 @@ struct Lane {
     __device__ __forceinline__ T* at(const Rows& r) const {
         return (T*)r.p + b * r.sb + c;
     }
-    // The first step of tile t in a tensor, and the thread's place from there in bytes (scan).
+    // The first step of tile t in a tensor, of the workgroup's first item, and the thread's place from there
+    // in bytes (scan).
     template <typename T>
     __device__ __forceinline__ char* tile(const Rows& r, int t) const {
-        return (char*)((T*)r.p + (int64_t)b * r.sb + (int64_t)t * kSlots * kRun * r.st);
+        return (char*)((T*)r.p + (int64_t)b0 * r.sb + (int64_t)t * kSlots * kRun * r.st);
     }
     template <typename T>
     __device__ __forceinline__ uint32_t offset(const Rows& r) const {
-        return (uint32_t)((slot * kRun * (uint32_t)r.st + (uint32_t)c) * (uint32_t)sizeof(T));
+        return ((b - b0) * (uint32_t)r.sb + slot * kRun * (uint32_t)r.st + (uint32_t)c) * (uint32_t)sizeof(T);
     }
-    template <typename T, bool WIDE>
-    __device__ __forceinline__ void load(const Rows& r, const Run& run, int t, int64_t channels, Part<T> (&v)[kRun]) const {
-        run.template load<T, WIDE, SCAN>(at<const T>(r), SCAN ? tile<T>(r, t) : nullptr, SCAN ? offset<T>(r) : 0, r.st, c,
-                                         channels, v);
+    template <typename T, bool EVEN>
+    __device__ __forceinline__ void load(const Rows& r, const Run& run, int t, Part<T> (&v)[kRun]) const {
+        run.template load<T, EVEN, SCAN>(at<const T>(r), SCAN ? tile<T>(r, t) : nullptr, SCAN ? offset<T>(r) : 0, r.st, next, v);
     }
     // The place of this thread's channels in a [batch][channels] array.
     __device__ __forceinline__ int64_t state_at(const RecurArgs& a) const { return (int64_t)b * a.channels + c; }
 };
 
-// fp32 values of a thread's channels (never wide: channels may be odd).
+// fp32 values of a thread's channels (one by one: channels may be odd).
 template <int V>
 __device__ __forceinline__ void load_state(const float* p, int64_t at, int64_t c, int64_t n, bool live, float (&h)[V]) {
 #pragma unroll
@@ -483,55 +486,49 @@ __device__ __forceinline__ void through_splits(const RecurArgs& a, const RecurCu
     }
 }
 
-inline bool recur_wide(const RecurArgs& a) {
-    constexpr int v = kRecurChannels;
-    const size_t e = a.bf16 ? 2 : 4;
-    if (a.channels % v) return false;
-    for (const Rows* t : {&a.x, &a.g, &a.z, &a.y, &a.dy, &a.dx, &a.dg, &a.dz})
-        if (!rows_fit(*t, v, e)) return false;
-    return true;
-}
-
-// Whether threads walk alone: where there are enough of them, few steps, or steps so
+// Whether threads walk alone: where there are enough of them, few steps, or steps or items so
 // far apart that a tile has no 32-bit offsets.
 constexpr uint32_t kWalkThreads = 65536;
 inline bool walks(const RecurArgs& a) {
-    constexpr int v = kRecurChannels;
-    const int64_t e = a.bf16 ? 2 : 4, tile = kScanBlock * v / kRecurBlock * kRun;
-    for (const Rows* t : {&a.x, &a.g, &a.z, &a.y, &a.dy, &a.dx, &a.dg, &a.dz})
-        if (t->p && (t->st >= ((int64_t)1 << 31) / (e * tile) - a.channels)) return true;
-    return a.steps <= 2 * kRun || (uint64_t)a.batch * ((a.channels + v - 1) / v) >= kWalkThreads;
+    constexpr int64_t v = kRecurChannels, lanes = kRecurBlock / v, tile = (int64_t)kScanBlock / lanes * kRun;
+    const int64_t e = a.bf16 ? 2 : 4, most = ((int64_t)1 << 31) / e, columns = (a.channels + v - 1) / v;
+    const int64_t items = std::min<int64_t>(a.batch - 1, lanes / columns + 1);  // from the first thread's to the last one's
+    for (const Rows* t : {&a.x, &a.g, &a.z, &a.y, &a.dy, &a.dx, &a.dg, &a.dz}) {
+        if (!t->p) continue;
+        if (t->st > most / tile || (items > 0 && t->sb > most / items) || t->st * tile + t->sb * items + a.channels > most) return true;
+    }
+    return a.steps <= 2 * kRun || a.batch * columns >= kWalkThreads;
 }
 constexpr uint32_t kScanGroups = 512;
 inline RecurCut recur_cut(const RecurArgs& a) {
-    constexpr int v = kRecurChannels;
+    constexpr uint32_t v = kRecurChannels, lanes = kRecurBlock / v, slots = kScanBlock / lanes;
     RecurCut c{};
     c.columns = (uint32_t)((a.channels + v - 1) / v);
     c.by_columns = divisor(c.columns);
-    const int64_t runs = (a.steps + kRun - 1) / kRun;
+    const int64_t runs = (a.steps + kRun - 1) / kRun, all = (int64_t)c.columns * a.batch;
     c.splits = 1;
     if (walks(a)) {
         c.tiles = (int32_t)runs;
-        c.groups = (uint32_t)(((uint64_t)c.columns * a.batch + kWalkBlock - 1) / kWalkBlock);
+        c.groups = (uint32_t)((all + kWalkBlock - 1) / kWalkBlock);
         return c;
     }
-    const int slots = kScanBlock * v / kRecurBlock;
     c.tiles = (int32_t)((runs + slots - 1) / slots);
-    c.blocks = (uint32_t)((a.channels + kRecurBlock - 1) / kRecurBlock);
-    const uint64_t base = (uint64_t)c.blocks * a.batch;
-    c.splits = base >= 192 ? 1 : (int32_t)std::max<uint64_t>(1, std::min<uint64_t>({kScanGroups / base, (uint64_t)c.tiles, kMaxSplits}));
-    c.groups = (uint32_t)(base * c.splits);
+    c.blocks = (uint32_t)((all + lanes - 1) / lanes);
+    // Two workgroups a CU; split only where that leaves a CU with none.
+    if (c.blocks < 192)
+        c.splits = (int32_t)std::max<int64_t>(1, std::min<int64_t>({(int64_t)(kScanGroups / c.blocks), (int64_t)c.tiles, (int64_t)kMaxSplits}));
+    c.groups = c.blocks * (uint32_t)c.splits;
     return c;
 }
 
-// Calls f with the storage type, whether loads are wide, and whether there is an
-// output gate.
+// Calls f with the storage type, whether rows have an even number of channels, and
+// whether there is an output gate.
 template <typename F>
 hipError_t recur_dispatch(const RecurArgs& a, F&& f) {
-    auto gated = [&](auto t, auto wide) {
-        return a.z.p ? f(t, wide, std::true_type{}) : f(t, wide, std::false_type{});
+    auto gated = [&](auto t, auto even) {
+        return a.z.p ? f(t, even, std::true_type{}) : f(t, even, std::false_type{});
     };
-    auto type = [&](auto t) { return recur_wide(a) ? gated(t, std::true_type{}) : gated(t, std::false_type{}); };
+    auto type = [&](auto t) { return a.channels % 2 == 0 ? gated(t, std::true_type{}) : gated(t, std::false_type{}); };
     return a.bf16 ? type(__bf16{}) : type(float{});
 }
 

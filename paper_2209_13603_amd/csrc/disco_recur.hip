@@ -31,7 +31,7 @@ struct Inputs {
 
 // AHEAD: the next tile's loads are out while this one is worked on (fp32 has no
 // registers for that).
-template <typename T, bool WIDE, bool Z, int GAIN, bool SCAN>
+template <typename T, bool EVEN, bool Z, int GAIN, bool SCAN>
 __global__ __launch_bounds__((Lane<V, SCAN>::kThreads)) void k_recur(RecurArgs a, RecurCut cut) {
     typedef Lane<V, SCAN> L;
     constexpr bool AHEAD = SCAN && sizeof(T) == 2 && Z;
@@ -44,9 +44,9 @@ __global__ __launch_bounds__((Lane<V, SCAN>::kThreads)) void k_recur(RecurArgs a
     auto load = [&](int t) {
         Inputs<T, Z> in;
         const Run r(a, ((int64_t)t * L::kSlots + ln.slot) * kRun, ln.count);
-        ln.template load<T, WIDE>(a.g, r, t, C, in.g);
-        ln.template load<T, WIDE>(a.x, r, t, C, in.x);
-        if constexpr (Z) ln.template load<T, WIDE>(a.z, r, t, C, in.z);
+        ln.template load<T, EVEN>(a.g, r, t, in.g);
+        ln.template load<T, EVEN>(a.x, r, t, in.x);
+        if constexpr (Z) ln.template load<T, EVEN>(a.z, r, t, in.z);
         return in;
     };
     Inputs<T, Z> next;
@@ -78,10 +78,10 @@ __global__ __launch_bounds__((Lane<V, SCAN>::kThreads)) void k_recur(RecurArgs a
 #pragma unroll
                         for (int j = 0; j < V; ++j) v[j] = out(i, e(i, j), j);
                         if constexpr (SCAN) {
-                            store_part<T, V, WIDE>((T*)(to + off), ln.c, C, v);
+                            store_part<T, EVEN>((T*)(to + off), ln.next, v);
                             move_all(to, a.y.st * (int64_t)sizeof(T));
                         } else {
-                            store_part<T, V, WIDE>(y, ln.c, C, v);
+                            store_part<T, EVEN>(y, ln.next, v);
                             move(y, a.y.st);
                         }
                     }
@@ -99,7 +99,7 @@ __global__ __launch_bounds__((Lane<V, SCAN>::kThreads)) void k_recur(RecurArgs a
                             v[j] = out(i, e(i, j), j);
                             v[j] = i < r.left ? v[j] : 0.0f;
                         }
-                        if (ln.live && i < r.steps) store_part<T, V, WIDE>(y, ln.c, C, v);
+                        if (ln.live && i < r.steps) store_part<T, EVEN>(y, ln.next, v);
                         move(y, a.y.st);
                     }
                 }
@@ -137,12 +137,11 @@ __global__ __launch_bounds__((Lane<V, SCAN>::kThreads)) void k_recur(RecurArgs a
 }
 
 // The maps of all splits but the last.
-template <typename T, bool WIDE, int GAIN>
+template <typename T, bool EVEN, int GAIN>
 __global__ __launch_bounds__(kScanBlock) void k_recur_maps(RecurArgs a, RecurCut cut) {
     typedef Lane<V, true> L;
     __shared__ float maps[2][L::kWaves][L::kLanes][2 * V];
     const L ln(a, cut);
-    const int64_t C = a.channels;
     SplitMap<V> all;
     struct Pair {
         Part<T> g[kRun], x[kRun];
@@ -150,8 +149,8 @@ __global__ __launch_bounds__(kScanBlock) void k_recur_maps(RecurArgs a, RecurCut
     auto load = [&](int t) {
         Pair in;
         const Run r(a, ((int64_t)t * L::kSlots + ln.slot) * kRun, ln.count);
-        ln.template load<T, WIDE>(a.g, r, t, C, in.g);
-        ln.template load<T, WIDE>(a.x, r, t, C, in.x);
+        ln.template load<T, EVEN>(a.g, r, t, in.g);
+        ln.template load<T, EVEN>(a.x, r, t, in.x);
         return in;
     };
     for (int t = ln.t1 - 1; t >= ln.t0; --t) {
@@ -188,9 +187,9 @@ hipError_t launch_recur(const RecurArgs& a, float* ws) {
     if (cut.splits > 1) {
         const int tk = timing_begin("recurrence_maps", a.stream);
         const uint32_t groups = cut.groups / cut.splits * (cut.splits - 1);
-        const hipError_t e = recur_dispatch(a, [&](auto t, auto wide, auto) {
+        const hipError_t e = recur_dispatch(a, [&](auto t, auto even, auto) {
             return by_gain(a.gain, [&](auto gain) {
-                hipLaunchKernelGGL((k_recur_maps<decltype(t), decltype(wide)::value, decltype(gain)::value>), grid_dim(groups),
+                hipLaunchKernelGGL((k_recur_maps<decltype(t), decltype(even)::value, decltype(gain)::value>), grid_dim(groups),
                                    dim3(kScanBlock), 0, a.stream, a, cut);
                 return hipGetLastError();
             });
@@ -199,13 +198,13 @@ hipError_t launch_recur(const RecurArgs& a, float* ws) {
         if (e != hipSuccess) return e;
     }
     const int tk = timing_begin("recurrence", a.stream);
-    const hipError_t e = recur_dispatch(a, [&](auto t, auto wide, auto z) {
+    const hipError_t e = recur_dispatch(a, [&](auto t, auto even, auto z) {
         return by_gain(a.gain, [&](auto gain) {
             auto go = [&](auto kernel) {
                 hipLaunchKernelGGL(kernel, grid_dim(cut.groups), dim3(cut.blocks ? kScanBlock : kWalkBlock), 0, a.stream, a, cut);
             };
-            if (cut.blocks) go(k_recur<decltype(t), decltype(wide)::value, decltype(z)::value, decltype(gain)::value, true>);
-            else go(k_recur<decltype(t), decltype(wide)::value, decltype(z)::value, decltype(gain)::value, false>);
+            if (cut.blocks) go(k_recur<decltype(t), decltype(even)::value, decltype(z)::value, decltype(gain)::value, true>);
+            else go(k_recur<decltype(t), decltype(even)::value, decltype(z)::value, decltype(gain)::value, false>);
             return hipGetLastError();
         });
     });

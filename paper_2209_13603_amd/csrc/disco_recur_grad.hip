@@ -43,7 +43,7 @@ struct Inputs {
 };
 
 // AHEAD: the next tile's loads are out while this one is worked on.
-template <typename T, bool WIDE, bool Z, int GAIN, bool SCAN>
+template <typename T, bool EVEN, bool Z, int GAIN, bool SCAN>
 __global__ __launch_bounds__((Lane<V, SCAN>::kThreads)) void k_recur_grad(RecurArgs a, RecurCut cut) {
     typedef Lane<V, SCAN> L;
     constexpr bool AHEAD = SCAN && sizeof(T) == 2;
@@ -64,10 +64,10 @@ __global__ __launch_bounds__((Lane<V, SCAN>::kThreads)) void k_recur_grad(RecurA
         const int64_t run = (int64_t)t * L::kSlots + ln.slot;
         const Run r(a, run * kRun, ln.count);
         load_state(a.carries, (ln.b * runs + run) * C + ln.c, ln.c, C, ln.live && run < runs, in.before);
-        ln.template load<T, WIDE>(a.g, r, t, C, in.g);
-        ln.template load<T, WIDE>(a.dy, r, t, C, in.dy);
-        if constexpr (Z) ln.template load<T, WIDE>(a.z, r, t, C, in.z);
-        ln.template load<T, WIDE>(a.x, r, t, C, in.x);
+        ln.template load<T, EVEN>(a.g, r, t, in.g);
+        ln.template load<T, EVEN>(a.dy, r, t, in.dy);
+        if constexpr (Z) ln.template load<T, EVEN>(a.z, r, t, in.z);
+        ln.template load<T, EVEN>(a.x, r, t, in.x);
         return in;
     };
     Inputs<T, Z> next;
@@ -178,18 +178,18 @@ __global__ __launch_bounds__((Lane<V, SCAN>::kThreads)) void k_recur_grad(RecurA
                 in.before[j] = p.v[j];
             }
             if constexpr (SCAN && every) {
-                store_part<T, V, WIDE>((T*)(tile_x + off_x), ln.c, C, dx);
-                store_part<T, V, WIDE>((T*)(tile_g + off_g), ln.c, C, dg);
-                if constexpr (Z) store_part<T, V, WIDE>((T*)(tile_z + off_z), ln.c, C, dz);
+                store_part<T, EVEN>((T*)(tile_x + off_x), ln.next, dx);
+                store_part<T, EVEN>((T*)(tile_g + off_g), ln.next, dg);
+                if constexpr (Z) store_part<T, EVEN>((T*)(tile_z + off_z), ln.next, dz);
                 move_all(tile_x, -a.dx.st * (int64_t)sizeof(T));
                 move_all(tile_g, -a.dg.st * (int64_t)sizeof(T));
                 if constexpr (Z) move_all(tile_z, -a.dz.st * (int64_t)sizeof(T));
             } else {
                 if (stored) {
-                    if (every || a.dx.p) store_part<T, V, WIDE>(to_x, ln.c, C, dx);
-                    if (every || a.dg.p) store_part<T, V, WIDE>(to_g, ln.c, C, dg);
+                    if (every || a.dx.p) store_part<T, EVEN>(to_x, ln.next, dx);
+                    if (every || a.dg.p) store_part<T, EVEN>(to_g, ln.next, dg);
                     if constexpr (Z)
-                        if (every || a.dz.p) store_part<T, V, WIDE>(to_z, ln.c, C, dz);
+                        if (every || a.dz.p) store_part<T, EVEN>(to_z, ln.next, dz);
                 }
                 move(to_x, -a.dx.st);
                 move(to_g, -a.dg.st);
@@ -225,19 +225,18 @@ __global__ __launch_bounds__((Lane<V, SCAN>::kThreads)) void k_recur_grad(RecurA
 }
 
 // The maps of all splits but the first, from their ends.
-template <typename T, bool WIDE, bool Z>
+template <typename T, bool EVEN, bool Z>
 __global__ __launch_bounds__(kScanBlock) void k_recur_grad_maps(RecurArgs a, RecurCut cut) {
     typedef Lane<V, true> L;
     __shared__ float maps[2][L::kWaves][L::kLanes][2 * V];
     const L ln(a, cut, 1);
-    const int64_t C = a.channels;
     SplitMap<V> all;
     for (int t = ln.t0; t < ln.t1; ++t) {
         const Run r(a, ((int64_t)t * L::kSlots + ln.slot) * kRun, ln.count);
         Part<T> g[kRun], dy[kRun], z[kRun];
-        ln.template load<T, WIDE>(a.g, r, t, C, g);
-        ln.template load<T, WIDE>(a.dy, r, t, C, dy);
-        if constexpr (Z) ln.template load<T, WIDE>(a.z, r, t, C, z);
+        ln.template load<T, EVEN>(a.g, r, t, g);
+        ln.template load<T, EVEN>(a.dy, r, t, dy);
+        if constexpr (Z) ln.template load<T, EVEN>(a.z, r, t, z);
         r.take_out(dy);
         if constexpr (Z) r.take_out(z);
         float qa[V], qb[V];
@@ -277,8 +276,8 @@ hipError_t launch_recur_grad(const RecurArgs& a, float* ws) {
     if (cut.splits > 1) {
         const int tk = timing_begin("recurrence_grad_maps", a.stream);
         const uint32_t groups = cut.groups / cut.splits * (cut.splits - 1);
-        const hipError_t e = recur_dispatch(a, [&](auto t, auto wide, auto z) {
-            hipLaunchKernelGGL((k_recur_grad_maps<decltype(t), decltype(wide)::value, decltype(z)::value>), grid_dim(groups),
+        const hipError_t e = recur_dispatch(a, [&](auto t, auto even, auto z) {
+            hipLaunchKernelGGL((k_recur_grad_maps<decltype(t), decltype(even)::value, decltype(z)::value>), grid_dim(groups),
                                dim3(kScanBlock), 0, a.stream, a, cut);
             return hipGetLastError();
         });
@@ -286,13 +285,13 @@ hipError_t launch_recur_grad(const RecurArgs& a, float* ws) {
         if (e != hipSuccess) return e;
     }
     const int tk = timing_begin("recurrence_grad", a.stream);
-    const hipError_t e = recur_dispatch(a, [&](auto t, auto wide, auto z) {
+    const hipError_t e = recur_dispatch(a, [&](auto t, auto even, auto z) {
         return by_gain(a.gain, [&](auto gain) {
             auto go = [&](auto kernel) {
                 hipLaunchKernelGGL(kernel, grid_dim(cut.groups), dim3(cut.blocks ? kScanBlock : kWalkBlock), 0, a.stream, a, cut);
             };
-            if (cut.blocks) go(k_recur_grad<decltype(t), decltype(wide)::value, decltype(z)::value, decltype(gain)::value, true>);
-            else go(k_recur_grad<decltype(t), decltype(wide)::value, decltype(z)::value, decltype(gain)::value, false>);
+            if (cut.blocks) go(k_recur_grad<decltype(t), decltype(even)::value, decltype(z)::value, decltype(gain)::value, true>);
+            else go(k_recur_grad<decltype(t), decltype(even)::value, decltype(z)::value, decltype(gain)::value, false>);
             return hipGetLastError();
         });
     });

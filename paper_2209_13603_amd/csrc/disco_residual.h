@@ -111,26 +111,11 @@ struct Cursor {
     }
 };
 // A chunk of a weight, or of ones.
-template <typename T, int W>
+template <typename T, bool EIGHTS>
 __device__ __forceinline__ Raw<T> load_weight(const void* w, int64_t sb, uint32_t item, int c, int left) {
     Raw<T> r;
     r.fill(1.0f);
-    return w ? load_raw<T, W>((const T*)w + item * sb + c, left) : r;
-}
-
-// Host: the widest pieces that rows are read and written in.
-inline int norm_width(const ResidualArgs& a) {
-    const size_t e = a.bf16 ? 2 : 4;
-    auto fits = [&](int v) {
-        if (a.channels % v) return false;
-        for (const void* p : {a.post_w, a.gate, a.next_w})
-            if ((uintptr_t)p % (v * e)) return false;
-        for (const Rows* t : {&a.x, &a.f, &a.h, &a.y, &a.dh, &a.dy, &a.dx, &a.df})
-            if (!rows_fit(*t, v, e)) return false;
-        return true;
-    };
-    const int most = a.bf16 ? 8 : 4;
-    return fits(most) ? most : fits(2) ? 2 : 1;
+    return w ? load_raw<T, EIGHTS>((const T*)w + item * sb + c, left) : r;
 }
 
 // The items and positions of a call's rows, in a; most: chunks that a thread holds at
@@ -189,16 +174,12 @@ inline void norm_runs(NormShape* s, uint32_t most) {
     s->groups = std::max(1u, (s->rows + s->per_group - 1) / s->per_group);
 }
 
-// Calls f with the storage type, the width of a piece and whether entries are dropped.
+// Calls f with the storage type, whether rows are of whole chunks and whether entries are dropped.
 template <typename F>
 hipError_t norm_dispatch(const ResidualArgs& a, F&& f) {
     auto dropped = [&](auto t, auto w) { return a.dropped ? f(t, w, std::true_type{}) : f(t, w, std::false_type{}); };
     auto width = [&](auto t) {
-        switch (norm_width(a)) {
-            case 1: return dropped(t, std::integral_constant<int, 1>{});
-            case 2: return dropped(t, std::integral_constant<int, 2>{});
-            default: return dropped(t, std::integral_constant<int, (sizeof(t) == 2 ? 8 : 4)>{});
-        }
+        return a.channels % kChunk == 0 ? dropped(t, std::true_type{}) : dropped(t, std::false_type{});
     };
     return a.bf16 ? width(__bf16{}) : width(float{});
 }

@@ -30,7 +30,7 @@ namespace disco {
 
 namespace {
 
-template <typename T, int NV, int W, bool DROP>
+template <typename T, int NV, bool EIGHTS, bool DROP>
 __global__ __launch_bounds__(512) void k_residual(ResidualArgs a, NormShape s) {
     __shared__ float red[2][1024 / kNormWave][2];
     const int lane = threadIdx.x & (s.lanes - 1), c = lane * kChunk, C = a.channels;
@@ -55,8 +55,8 @@ __global__ __launch_bounds__(512) void k_residual(ResidualArgs a, NormShape s) {
             const T *f = to_f.next(), *x = to_x.next();
 #pragma unroll
             for (int j = 0; j < NV; ++j) {
-                r.f[j] = load_raw<T, W>(f + j * step, n - j * step);
-                if (has(s, kHasX)) r.x[j] = load_raw<T, W>(x + j * step, n - j * step);
+                r.f[j] = load_raw<T, EIGHTS>(f + j * step, n - j * step);
+                if (has(s, kHasX)) r.x[j] = load_raw<T, EIGHTS>(x + j * step, n - j * step);
                 else r.x[j].fill(0.0f);
             }
             return r;
@@ -64,9 +64,9 @@ __global__ __launch_bounds__(512) void k_residual(ResidualArgs a, NormShape s) {
         Raw<T> w[NV], g[NV], w2[NV];
 #pragma unroll
         for (int j = 0; j < NV; ++j) {
-            w[j] = load_weight<T, W>(a.post_w, a.post_sb, item, c + j * step, C - c - j * step);
-            g[j] = load_weight<T, W>(a.gate, a.gate_sb, item, c + j * step, C - c - j * step);
-            w2[j] = load_weight<T, W>(a.next_w, a.next_sb, item, c + j * step, C - c - j * step);
+            w[j] = load_weight<T, EIGHTS>(a.post_w, a.post_sb, item, c + j * step, C - c - j * step);
+            g[j] = load_weight<T, EIGHTS>(a.gate, a.gate_sb, item, c + j * step, C - c - j * step);
+            w2[j] = load_weight<T, EIGHTS>(a.next_w, a.next_sb, item, c + j * step, C - c - j * step);
         }
         Row next = load(first + slot);
         for (uint32_t base = first; base < stop; base += s.slots) {
@@ -95,7 +95,7 @@ __global__ __launch_bounds__(512) void k_residual(ResidualArgs a, NormShape s) {
                     if constexpr (DROP) d = stays(bits, i, a.drop.out) ? d : 0.0f;
                     v[i] = u[i] = fmaf(a.scale, now.x[j].at(i), d * g[j].at(i));
                 }
-                if (has(s, kHasH)) store_raw<T, W>(h + j * step, n - j * step, v);
+                if (has(s, kHasH)) store_raw<T, EIGHTS>(h + j * step, n - j * step, v);
             }
             if (!has(s, kHasY)) continue;
             r = norm_factor(e, a, rs.one(squares(e)), rs, &up, &again);
@@ -104,7 +104,7 @@ __global__ __launch_bounds__(512) void k_residual(ResidualArgs a, NormShape s) {
                 float v[kChunk];
 #pragma unroll
                 for (int i = 0; i < kChunk; ++i) v[i] = e[j * kChunk + i] * r * w2[j].at(i);
-                store_raw<T, W>(y + j * step, n - j * step, v);
+                store_raw<T, EIGHTS>(y + j * step, n - j * step, v);
             }
         }
         seg += stop - first;

@@ -33,7 +33,7 @@ struct Partials {
 
 // The next row's loads go out before this one's arithmetic, a run's weights stay in
 // registers.
-template <typename T, int NV, int W, bool DROP, int THREADS>
+template <typename T, int NV, bool EIGHTS, bool DROP, int THREADS>
 __global__ __launch_bounds__(THREADS) void k_residual_grad(ResidualArgs a, NormShape s, Partials ps) {
     constexpr int N = NV * kChunk;
     __shared__ float red[2][1024 / kNormWave][2];
@@ -94,10 +94,10 @@ __global__ __launch_bounds__(THREADS) void k_residual_grad(ResidualArgs a, NormS
             const T *x = to_x.next(), *f = to_f.next(), *dh = to_dh.next(), *dy = to_dy.next();
 #pragma unroll
             for (int j = 0; j < NV; ++j) {
-                r.f[j] = load_raw<T, W>(f + j * step, n - j * step);
-                r.x[j] = load_raw<T, W>(x + j * step, has(s, kHasX) ? n - j * step : 0);
-                r.dh[j] = load_raw<T, W>(dh + j * step, has(s, kHasDh) ? n - j * step : 0);
-                r.dy[j] = load_raw<T, W>(dy + j * step, has(s, kHasDy) ? n - j * step : 0);
+                r.f[j] = load_raw<T, EIGHTS>(f + j * step, n - j * step);
+                r.x[j] = load_raw<T, EIGHTS>(x + j * step, has(s, kHasX) ? n - j * step : 0);
+                r.dh[j] = load_raw<T, EIGHTS>(dh + j * step, has(s, kHasDh) ? n - j * step : 0);
+                r.dy[j] = load_raw<T, EIGHTS>(dy + j * step, has(s, kHasDy) ? n - j * step : 0);
             }
             return r;
         };
@@ -105,9 +105,9 @@ __global__ __launch_bounds__(THREADS) void k_residual_grad(ResidualArgs a, NormS
         auto load_weights = [&] {
 #pragma unroll
             for (int j = 0; j < NV; ++j) {
-                w[j] = load_weight<T, W>(a.post_w, a.post_sb, item, c + j * step, C - c - j * step);
-                g[j] = load_weight<T, W>(a.gate, a.gate_sb, item, c + j * step, C - c - j * step);
-                w2[j] = load_weight<T, W>(a.next_w, a.next_sb, item, c + j * step, C - c - j * step);
+                w[j] = load_weight<T, EIGHTS>(a.post_w, a.post_sb, item, c + j * step, C - c - j * step);
+                g[j] = load_weight<T, EIGHTS>(a.gate, a.gate_sb, item, c + j * step, C - c - j * step);
+                w2[j] = load_weight<T, EIGHTS>(a.next_w, a.next_sb, item, c + j * step, C - c - j * step);
             }
         };
         auto raw = [&](Raw<T>(&r)[NV]) {
@@ -199,7 +199,7 @@ __global__ __launch_bounds__(THREADS) void k_residual_grad(ResidualArgs a, NormS
                     float e[kChunk];
 #pragma unroll
                     for (int i = 0; i < kChunk; ++i) e[i] = v[j * kChunk + i];
-                    store_raw<T, W>(to + j * step, n - j * step, e);
+                    store_raw<T, EIGHTS>(to + j * step, n - j * step, e);
                 }
             };
             if (has(s, kHasDx)) store(dx, h);
@@ -325,7 +325,7 @@ hipError_t launch_residual_grad(const ResidualArgs& args, float* ws) {
             hipLaunchKernelGGL(kernel, dim3(s.groups), dim3((unsigned)s.threads), 0, a.stream, a, s, ps);
             return hipGetLastError();
         };
-        constexpr int W = decltype(w)::value;
+        constexpr bool W = decltype(w)::value;
         constexpr bool DROP = decltype(drop)::value;
         if constexpr (sizeof(t) == 2) {
             if (s.nv == 1) return go(k_residual_grad<__bf16, 1, W, DROP, 256>);
