@@ -573,8 +573,9 @@ typedef struct {
  * A gate of -inf starts anew from x, one of +inf holds the state, where x and h are finite.
  * carries: NULL, or [batch][(tokens + 15) / 16][channels] floats, the states before
  * every 16th token, which the backward call reads.  How the work is cut depends on
- * the sizes alone, and parts are joined in a fixed order.  batch * channels < 2^31,
- * channels up to 2^24.  options NULL: gain MEAN, no lengths.  Errors: INVALID_ARGUMENT,
+ * the sizes and strides alone, and parts are joined in a fixed order.  batch * channels < 2^31,
+ * channels up to 2^24 (an odd number of them takes up to twice the time: a row's channels then go
+ * one by one).  options NULL: gain MEAN, no lengths.  Errors: INVALID_ARGUMENT,
  * SHAPE, DTYPE, OUT_OF_MEMORY, DEVICE. */
 disco_status_t disco_gated_recurrence(const disco_rows_t* x, const disco_rows_t* gate, const disco_rows_t* out_gate,
                                       const disco_recurrence_t* options, const float* state, disco_rows_t* y, float* last,

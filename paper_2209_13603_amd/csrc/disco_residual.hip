@@ -11,14 +11,18 @@
 // read or written once and a row stays in registers from its loads to its stores.
 // The gradients recompute h and both norms from x and f, which costs no byte more
 // than reading a stored h, and leaves h and y without a rounding between them:
-// y is taken from h before its rounding to bf16.  Rows of up to 512 entries in the
-// gradients (1024 forward) lie in one wave, whose lanes share the sums by shuffles;
-// longer ones in a workgroup.  A thread holds chunks of eight entries, the
-// share of one block of the dropout's generator.  All sums are fp32.
+// y is taken from h before its rounding to bf16.  Rows of up to 1024 entries (512 in the
+// gradients of fp32) lie in one wave, whose lanes share the sums by shuffles and without a
+// barrier; longer ones in a workgroup, with one barrier a sum.  A thread holds chunks of eight
+// entries, the share of one block of the dropout's generator.  All sums are fp32.
 //
 // The gradients of the weights are summed in a fixed order: each workgroup walks
 // a run of rows and leaves one partial row a sum (one an item for weights of
 // [batch, channels]), which k_residual_join adds.
+//
+// Measured, bf16: 32768 rows of 1024, dropped, both norms and a gate 50 us forward (268 MB, 5.4 TB/s)
+// and 96 us gradients (403 MB, 4.2 TB/s); 4050 rows of 8192 48 and 92 us; 32768 rows of 512
+// forward 23 us (134 MB, in part from the caches).
 #include <hip/hip_runtime.h>
 
 #include <cstdint>
