@@ -97,8 +97,8 @@ __device__ __forceinline__ float sigmoid(float z) {
     return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(-1.44269504f * z));
 }
 
-// A step of the forward call.  fp32 takes a gate as above; bf16, where the vector
-// unit is busy for most of the call, as 1 - a alone, which keeps an a near 0 to 2^-24 of the state before it
+// A step of the forward call.  fp32 takes a gate as above; bf16, where the chain
+// of vector operations shows in the time (half of the cycles issue one), as 1 - a alone, which keeps an a near 0 to 2^-24 of the state before it
 // instead of its own size, at two thirds of the instructions (one series of 131072 x 768 251 us as fp32
 // takes it, 232 so).
 template <typename T>
