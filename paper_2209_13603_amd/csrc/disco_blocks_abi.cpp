@@ -356,10 +356,8 @@ disco_status_t disco_gated_recurrence(const disco_rows_t* x, const disco_rows_t*
         take(&d, y, "y");
         d.take(state, "state");
         d.take(last, "last");
-        if (a.steps > 0) {
-            d.take(carries, "carries");
-            d.take(a.lengths, "lengths");
-        }
+        if (a.steps > 0) d.take(carries, "carries");
+        d.take(a.lengths, "lengths");  // (read without steps too)
         if (need && workspace) d.take(workspace, "workspace");
         d.enter();
         Workspace ws(workspace, workspace_bytes, need, stream);
@@ -410,10 +408,8 @@ disco_status_t disco_gated_recurrence_backward(const disco_rows_t* x, const disc
         for (const auto& o : outs) take(&d, o.first, o.second);
         d.take(dlast, "dlast");
         d.take(dstate, "dstate");
-        if (a.steps > 0) {
-            d.take(carries, "carries");
-            d.take(a.lengths, "lengths");
-        }
+        if (a.steps > 0) d.take(carries, "carries");
+        d.take(a.lengths, "lengths");  // (read without steps too)
         if (need && workspace) d.take(workspace, "workspace");
         d.enter();
         Workspace ws(workspace, workspace_bytes, need, stream);

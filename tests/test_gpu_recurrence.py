@@ -229,3 +229,23 @@ def test_gradients_against_differences():
             diff = (total({**base, name: base[name] + 1e-2 * d}) - total({**base, name: base[name] - 1e-2 * d})) / 2e-2
             want, size = float((grad.double() * d.double()).sum()), float(grad.double().norm() * d.double().norm())
             assert abs(diff - want) <= 2e-3 * size, (gain, name)
+
+
+def test_lengths_on_the_host_are_refused_without_steps_too():
+    """A call of no steps reads the lengths as well, to give the state: they have to be the device's."""
+    import ctypes
+    import torch
+    from paper_2209_13603_amd import blocks, disco
+    x, _, _, _, state, _ = _inputs(2, 5, 6, "fp32")
+    host = (ctypes.c_int32 * 2)(1, 2)
+    opt = disco.RecurrenceArgs(0, 0, ctypes.addressof(host))
+    last = torch.full_like(state, 7.0)
+    p = blocks._Pack()
+    r = p.rows(x[:, :0], "x")
+    lib, to = disco.library(), ctypes.addressof(opt)
+    assert lib.disco_gated_recurrence(r, r, None, to, state.data_ptr(), r, last.data_ptr(), None, None, 0, None) == \
+        disco.DISCO_ERR_DEVICE
+    assert lib.disco_gated_recurrence_backward(r, r, None, to, None, r, state.data_ptr(), None, None, None, last.data_ptr(), None, 0,
+                                               None) == disco.DISCO_ERR_DEVICE
+    torch.cuda.synchronize()
+    assert bool((last == 7).all())
