@@ -16,6 +16,7 @@
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
+#include <cmath>
 #include <cstdint>
 #include <type_traits>
 
@@ -49,21 +50,15 @@ __device__ __forceinline__ float gate_of(float g) {
     return __uint_as_float(__float_as_uint(q) | (__float_as_uint(g) & 0x80000000u));
 }
 __device__ __forceinline__ bool closed(float q) { return __float_as_int(q) < 0; }  // a is the smaller
-__device__ __forceinline__ float decay(float h, float q) {
-    const float s = fabsf(q);
-    return closed(q) ? s * h : fmaf(-s, h, h);
-}
-// A product A of a's step by step, and 1 - A as a sum of what each step takes.
+__device__ __forceinline__ float decay(float h, float q) { return fmaf(-q, h, closed(q) ? 0.0f : h); }
+// A product A of a's step by step, and 1 - A as the sum of what each step takes.  The sum is
+// asked for only where A is not below 1/2, that is where no a was: a step with an a below 1/2 need not
+// be right in it.
 struct Product {
     float a = 1.0f, rest = 0.0f;
-    __device__ __forceinline__ void take_rest(float r) {  // 1 - a of the step
-        rest = fmaf(r, a, rest);
-        a = fmaf(-r, a, a);
-    }
     __device__ __forceinline__ void take(float q) {
-        const float s = fabsf(q), u = s * a, v = fmaf(-s, a, a);
-        a = closed(q) ? u : v;
-        rest += closed(q) ? v : u;
+        rest = fmaf(fabsf(q), a, rest);
+        a = decay(a, q);
     }
     // As a gate.
     __device__ __forceinline__ float gate() const { return a < 0.5f ? -a : rest; }
@@ -97,31 +92,38 @@ __device__ __forceinline__ float sigmoid(float z) {
     return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(-1.44269504f * z));
 }
 
-// A step of the forward call.  fp32 takes a gate as above; bf16, where the chain
-// of vector operations shows in the time (half of the cycles issue one), as 1 - a alone, which keeps an a near 0 to 2^-24 of the state before it
-// instead of its own size, at two thirds of the instructions (one series of 131072 x 768 251 us as fp32
-// takes it, 232 so).
+// A step of a run that is scanned.  fp32 takes a gate as above; bf16, where the vector operations
+// show in the time (half of the cycles issue one), as a and 1 - a, each with a relative error of fp32 however small
+// it is: over the 16 steps of a run the roundings of an a near 1 come to 16 x 2^-25 of a state at most, and from run to run the
+// map has 1 - A as a sum.  One series of 131072 x 768 takes 250 us as fp32 takes it and 238 so.
 template <typename T>
 struct Step;
 template <>
 struct Step<float> {
     float q;
-    __device__ __forceinline__ Step(float g, bool in) : q(in ? gate_of(g) : 0.0f) {}
+    __device__ __forceinline__ explicit Step(float g) : q(gate_of(g)) {}
     __device__ __forceinline__ void onto(Product& p) const { p.take(q); }
     template <int GAIN>
     __device__ __forceinline__ float advance(float h, float x) const { return disco::advance<GAIN>(h, q, x); }
 };
 template <>
 struct Step<__bf16> {
-    float rest;
-    __device__ __forceinline__ Step(float g, bool in) : rest(in ? sigmoid(-g) : 0.0f) {}
-    __device__ __forceinline__ void onto(Product& p) const { p.take_rest(rest); }
+    float a, rest;
+    __device__ __forceinline__ explicit Step(float g) {
+        const float e = __builtin_amdgcn_exp2f(-1.44269504f * fabsf(g));
+        const float most = __builtin_amdgcn_rcpf(1.0f + e), least = e * most;
+        a = g < 0.0f ? least : most;
+        rest = g < 0.0f ? most : least;
+    }
+    __device__ __forceinline__ void onto(Product& p) const {
+        p.rest = fmaf(rest, p.a, p.rest);
+        p.a *= a;
+    }
     template <int GAIN>
     __device__ __forceinline__ float advance(float h, float x) const {
-        const float left = fmaf(-rest, h, h);
-        if (GAIN == kGainMean) return fmaf(rest, x, left);
-        if (GAIN == kGainPower) return fmaf(__builtin_amdgcn_sqrtf(fmaf(-rest, rest, rest + rest)), x, left);
-        return left + x;
+        if (GAIN == kGainMean) return fmaf(a, h, rest * x);
+        if (GAIN == kGainPower) return fmaf(a, h, __builtin_amdgcn_sqrtf(fmaf(-rest, rest, rest + rest)) * x);
+        return fmaf(a, h, x);
     }
 };
 
@@ -134,6 +136,7 @@ struct Part<__bf16> {
     uint32_t u;
     __device__ __forceinline__ float at(int j) const { return __uint_as_float(j ? u & 0xffff0000u : u << 16); }
     __device__ __forceinline__ void clear_unless(bool in) { u = in ? u : 0u; }
+    __device__ __forceinline__ void hold_unless(bool in) { u = in ? u : 0x7f807f80u; }
     // A new value to the compiler: what is converted is then converted again, instead of kept.
     __device__ __forceinline__ void anew() { asm("" : "+v"(u)); }
 };
@@ -142,6 +145,7 @@ struct Part<float> {
     float v[2];
     __device__ __forceinline__ float at(int j) const { return v[j]; }
     __device__ __forceinline__ void clear_unless(bool in) { v[0] = in ? v[0] : 0.0f, v[1] = in ? v[1] : 0.0f; }
+    __device__ __forceinline__ void hold_unless(bool in) { v[0] = in ? v[0] : HUGE_VALF, v[1] = in ? v[1] : HUGE_VALF; }
     __device__ __forceinline__ void anew() {}
 };
 // A thread's two channels of a row.  EVEN: rows have an even number of channels, and the
@@ -267,7 +271,13 @@ struct Run {
 #pragma unroll
         for (int i = 0; i < kRun; ++i) v[i].clear_unless(i < left);
     }
-    // Their gates leave a state as it is.
+    // Their gates leave a state as it is: +inf before the sigmoid, q = 0 behind it.
+    template <typename T>
+    __device__ __forceinline__ void hold(Part<T> (&g)[kRun]) const {
+        if (whole) return;
+#pragma unroll
+        for (int i = 0; i < kRun; ++i) g[i].hold_unless(i < left);
+    }
     template <int V>
     __device__ __forceinline__ void take_out(float (&q)[kRun][V]) const {
         if (whole) return;

@@ -36,9 +36,10 @@ struct Inputs {
 
 // AHEAD: the next tile's loads are out while this one is worked on (fp32 has no
 // registers for that; without an output gate the smaller tiles of two workgroups a CU cover each other,
-// and it gained nothing).
+// and it gained nothing; their 128 registers are asked for: left to itself the compiler takes up to 150 in bf16,
+// and one series of 131072 x 768 takes 165 us instead of 133).
 template <typename T, bool EVEN, bool Z, int GAIN, bool SCAN>
-__global__ __launch_bounds__((Lane<V, SCAN>::kThreads)) void k_recur(RecurArgs a, RecurCut cut) {
+__global__ __launch_bounds__((Lane<V, SCAN>::kThreads), (SCAN && !Z && sizeof(T) == 2 ? 4 : 1)) void k_recur(RecurArgs a, RecurCut cut) {
     typedef Lane<V, SCAN> L;
     constexpr bool AHEAD = SCAN && sizeof(T) == 2 && Z;
     __shared__ float maps[SCAN ? 2 : 1][L::kWaves][L::kLanes][2 * V];
@@ -69,6 +70,7 @@ __global__ __launch_bounds__((Lane<V, SCAN>::kThreads)) void k_recur(RecurArgs a
             in = load(t);
         }
         r.take_out(in.x);
+        r.hold(in.g);
         float mine[V];
         T* y = ln.template at<T>(a.y) + s0 * a.y.st;
         auto out = [&](int i, float state, int j) { return Z ? state * sigmoid(in.z[Z ? i : 0].at(j)) : state; };
@@ -113,20 +115,23 @@ __global__ __launch_bounds__((Lane<V, SCAN>::kThreads)) void k_recur(RecurArgs a
         if constexpr (SCAN) {
             // the run's map step by step; the states are one multiply-add from it
             float A[kRun][V], B[kRun][V], qa[V], qb[V];
+            Product P[V];
+            float state[V] = {0.0f};
+#pragma unroll
+            for (int i = 0; i < kRun; ++i) {
+#pragma unroll
+                for (int j = 0; j < V; ++j) {
+                    const Step<T> step(in.g[i].at(j));
+                    step.onto(P[j]);
+                    state[j] = step.template advance<GAIN>(state[j], in.x[i].at(j));
+                    A[i][j] = P[j].a;
+                    B[i][j] = state[j];
+                }
+            }
 #pragma unroll
             for (int j = 0; j < V; ++j) {
-                Product P;
-                float state = 0.0f;
-#pragma unroll
-                for (int i = 0; i < kRun; ++i) {
-                    const Step<T> step(in.g[i].at(j), r.whole || i < r.left);
-                    step.onto(P);
-                    state = step.template advance<GAIN>(state, in.x[i].at(j));
-                    A[i][j] = P.a;
-                    B[i][j] = state;
-                }
-                qa[j] = P.gate();
-                qb[j] = state;
+                qa[j] = P[j].gate();
+                qb[j] = state[j];
             }
             JoinMaps<V, SCAN, false>::run(qa, qb, h, mine, maps, t & 1);
             if (a.carries) store_state(a.carries, (ln.b * runs + run) * C + ln.c, ln.c, C, ln.live && run < runs, mine);
@@ -134,8 +139,8 @@ __global__ __launch_bounds__((Lane<V, SCAN>::kThreads)) void k_recur(RecurArgs a
         } else {
             if (a.carries) store_state(a.carries, (ln.b * runs + run) * C + ln.c, ln.c, C, ln.live, h);
             finish([&](int i, int j) {
-                const Step<T> step(in.g[i].at(j), r.whole || i < r.left);
-                return h[j] = step.template advance<GAIN>(h[j], in.x[i].at(j));
+                const float q = gate_of(in.g[i].at(j));
+                return h[j] = advance<GAIN>(h[j], q, in.x[i].at(j));
             });
         }
     }
@@ -163,6 +168,7 @@ __global__ __launch_bounds__(kScanBlock) void k_recur_maps(RecurArgs a, RecurCut
         const Run r(a, ((int64_t)t * L::kSlots + ln.slot) * kRun, ln.count);
         Pair in = load(t);
         r.take_out(in.x);
+        r.hold(in.g);
         float qa[V], qb[V];
 #pragma unroll
         for (int j = 0; j < V; ++j) {
@@ -170,7 +176,7 @@ __global__ __launch_bounds__(kScanBlock) void k_recur_maps(RecurArgs a, RecurCut
             float state = 0.0f;
 #pragma unroll
             for (int i = 0; i < kRun; ++i) {
-                const Step<T> step(in.g[i].at(j), r.whole || i < r.left);
+                const Step<T> step(in.g[i].at(j));
                 step.onto(P);
                 state = step.template advance<GAIN>(state, in.x[i].at(j));
             }
