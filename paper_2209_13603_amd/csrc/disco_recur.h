@@ -18,6 +18,7 @@
 #include <algorithm>
 #include <cmath>
 #include <cstdint>
+#include <numeric>
 #include <type_traits>
 
 #include "disco_blocks.h"
@@ -35,7 +36,7 @@ constexpr int kRecurChannels = 2;  // of a thread: see Part
 // consecutive runs and join their maps, `splits` of them share the time axis;
 // otherwise a thread walks all runs of its V channels by itself.
 struct RecurCut {
-    uint32_t columns;   // groups of V channels
+    uint32_t columns;   // groups of V channels; of items too far apart (scan) with the empty ones that fill up the last block
     uint32_t blocks;    // of 32 groups, over all items (scan)
     uint32_t groups;    // workgroups
     int32_t splits, tiles;  // tiles of all runs; a split takes every tiles / splits
@@ -326,6 +327,10 @@ struct Lane {
         b = cut.by_columns.quotient(column);
         if constexpr (!SCAN) b0 = b;
         c = (int64_t)(column - b * cut.columns) * V;
+        if (SCAN && c >= a.channels) {  // reads the last ones and writes nothing
+            live = false;
+            c = (a.channels - 1) / V * V;
+        }
         next = c + 1 < a.channels ? 1 : 0;
         count = a.steps;
         if (a.lengths) {
@@ -497,32 +502,44 @@ __device__ __forceinline__ void through_splits(const RecurArgs& a, const RecurCu
     }
 }
 
-// Whether threads walk alone: where there are enough of them, few steps, or steps or items so
-// far apart that a tile has no 32-bit offsets.  A tile of 256 steps is half idle on 80 steps, but a
+// Whether a workgroup's threads reach all that they scan with 32-bit offsets from its first item's channels: `steps`
+// steps and `items` items on.
+inline bool within_reach(const RecurArgs& a, int64_t steps, int64_t items) {
+    const int64_t most = ((int64_t)1 << 31) / (a.bf16 ? 2 : 4);
+    for (const Rows* t : {&a.x, &a.g, &a.z, &a.y, &a.dy, &a.dx, &a.dg, &a.dz}) {
+        if (!t->p) continue;
+        if (t->st > most / steps || (items > 0 && t->sb > most / items) || t->st * steps + t->sb * items + a.channels > most) return false;
+    }
+    return true;
+}
+
+// Whether threads walk alone: where there are enough of them, few steps, or steps so far
+// apart that a tile has no 32-bit offsets.  A tile of 256 steps is half idle on 80 steps, but a
 // walk's runs wait for each other.  Forward and gradients, walking and scanning: 3221 x 76 x 16 18 + 27 and
 // 20 + 39 us; 64 x 48 x 512 11 + 16 and 12 + 25; 1024 x 64 x 16 13 + 19 and 9 + 14; 100 x 128 x 512 24 + 37
 // and 18 + 36; 32 x 128 x 512 20 + 34 and 9 + 15.
 constexpr uint32_t kWalkThreads = 65536;
+constexpr int64_t kTileSteps = (int64_t)kScanBlock / (kRecurBlock / kRecurChannels) * kRun;
 inline bool walks(const RecurArgs& a) {
-    constexpr int64_t v = kRecurChannels, lanes = kRecurBlock / v, tile = (int64_t)kScanBlock / lanes * kRun;
-    const int64_t e = a.bf16 ? 2 : 4, most = ((int64_t)1 << 31) / e, columns = (a.channels + v - 1) / v;
-    const int64_t items = std::min<int64_t>(a.batch - 1, lanes / columns + 1);  // from the first thread's to the last one's
-    for (const Rows* t : {&a.x, &a.g, &a.z, &a.y, &a.dy, &a.dx, &a.dg, &a.dz}) {
-        if (!t->p) continue;
-        if (t->st > most / tile || (items > 0 && t->sb > most / items) || t->st * tile + t->sb * items + a.channels > most) return true;
-    }
-    const int64_t all = a.batch * columns;
-    return a.steps <= 2 * kRun || all >= kWalkThreads || (a.steps <= 5 * kRun && all >= kWalkThreads / 4);
+    const int64_t all = a.batch * ((a.channels + kRecurChannels - 1) / kRecurChannels);
+    return a.steps <= 2 * kRun || all >= kWalkThreads || (a.steps <= 5 * kRun && all >= kWalkThreads / 4) ||
+           !within_reach(a, kTileSteps, 0);
 }
 constexpr uint32_t kScanGroups = 512;
 inline RecurCut recur_cut(const RecurArgs& a) {
     constexpr uint32_t v = kRecurChannels, lanes = kRecurBlock / v, slots = kScanBlock / lanes;
     RecurCut c{};
     c.columns = (uint32_t)((a.channels + v - 1) / v);
+    const int64_t runs = (a.steps + kRun - 1) / kRun;
+    const bool walk = walks(a);
+    // Blocks begin at multiples of gcd(columns, lanes) within an item.  Of items that a block would span beyond its reach each
+    // takes blocks of its own.
+    const int64_t spans = (c.columns - std::gcd(c.columns, lanes) + lanes - 1) / c.columns;
+    if (!walk && !within_reach(a, kTileSteps, std::min<int64_t>(a.batch - 1, spans))) c.columns = (c.columns + lanes - 1) / lanes * lanes;
     c.by_columns = divisor(c.columns);
-    const int64_t runs = (a.steps + kRun - 1) / kRun, all = (int64_t)c.columns * a.batch;
+    const int64_t all = (int64_t)c.columns * a.batch;
     c.splits = 1;
-    if (walks(a)) {
+    if (walk) {
         c.tiles = (int32_t)runs;
         c.groups = (uint32_t)((all + kWalkBlock - 1) / kWalkBlock);
         return c;
