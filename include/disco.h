@@ -411,7 +411,7 @@ typedef struct {
 
 /* Norm of every head with the rotation in the same pass:
  *   y = rotate(w * x / sqrt(mean(x^2) + eps)) for each row (batch, token, head),
- * the mean over the head's dim entries.  norm = 0: rotation alone (weight
+ * the mean over the head's dim entries; eps finite in fp32.  norm = 0: rotation alone (weight
  * NULL).  weight: NULL (ones), [dim] for all heads, or [heads, dim]; x's type.
  * rotation: NULL for the norm alone.  y has x's sizes and may be x itself (same
  * data and strides), otherwise must not overlap it.  batch * tokens * heads < 2^31.
@@ -524,8 +524,8 @@ typedef struct {
 disco_status_t disco_dropout(const disco_rows_t* x, const disco_dropout_t* dropout, disco_rows_t* y, hipStream_t stream);
 
 typedef struct {
-    double scale;                      /* of the residual x */
-    double eps;
+    double scale;                      /* of the residual x; finite in fp32 */
+    double eps;                        /* >= 0, finite in fp32 */
     int32_t post_norm;                 /* 1: the block's output f is normed */
     int32_t reserved;                  /* 0 */
     const disco_tensor_t* post_weight; /* NULL (ones), [channels] or [batch, channels]; x's type; so are the others */

@@ -121,7 +121,7 @@ void check_residual(const disco_rows_t* x, const disco_rows_t* f, const disco_re
         if (o->post_norm != 0 && o->post_norm != 1) refuse(DISCO_ERR_INVALID_ARGUMENT, "post_norm must be 0 or 1");
         if (o->post_weight && !o->post_norm) refuse(DISCO_ERR_INVALID_ARGUMENT, "a post_weight needs the post norm");
         if (!(std::fabs(o->scale) <= FLT_MAX)) refuse(DISCO_ERR_INVALID_ARGUMENT, "scale must be finite in fp32");
-        if (!(eps >= 0.0) || !std::isfinite(eps)) refuse(DISCO_ERR_INVALID_ARGUMENT, "eps must be >= 0 and finite");
+        if (!(eps >= 0.0 && eps <= FLT_MAX)) refuse(DISCO_ERR_INVALID_ARGUMENT, "eps must be >= 0 and finite in fp32");
         a->post = o->post_norm != 0;
         a->scale = (float)o->scale;
         check_weight(o->post_weight, "post_weight", f, &a->post_w, &a->post_sb);

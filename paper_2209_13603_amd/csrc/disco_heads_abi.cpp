@@ -21,7 +21,7 @@ void check_rotate(const disco_heads_t* x, int32_t norm, const disco_tensor_t* w,
                   const disco_rotation_t* r, RotateArgs* a) {
     if (norm != 0 && norm != 1) refuse(DISCO_ERR_INVALID_ARGUMENT, "norm must be 0 or 1");
     if (!norm && w) refuse(DISCO_ERR_INVALID_ARGUMENT, "a weight needs the norm");
-    if (norm && (!(eps >= 0.0) || !std::isfinite(eps))) refuse(DISCO_ERR_INVALID_ARGUMENT, "eps must be >= 0 and finite");
+    if (norm && !(eps >= 0.0 && eps <= FLT_MAX)) refuse(DISCO_ERR_INVALID_ARGUMENT, "eps must be >= 0 and finite in fp32");
     if (w) {
         if (w->dtype != x->dtype) refuse(DISCO_ERR_DTYPE, "weight and x have different dtypes");
         const bool shared = w->ndim == 1 && w->shape[0] == x->dim;
