@@ -517,7 +517,10 @@ inline bool within_reach(const RecurArgs& a, int64_t steps, int64_t items) {
 // apart that a tile has no 32-bit offsets.  A tile of 256 steps is half idle on 80 steps, but a
 // walk's runs wait for each other.  Forward and gradients, walking and scanning: 3221 x 76 x 16 18 + 27 and
 // 20 + 39 us; 64 x 48 x 512 11 + 16 and 12 + 25; 1024 x 64 x 16 13 + 19 and 9 + 14; 100 x 128 x 512 24 + 37
-// and 18 + 36; 32 x 128 x 512 20 + 34 and 9 + 15.
+// and 18 + 36; 32 x 128 x 512 20 + 34 and 9 + 15.  At the border of 65536 threads, whole steps of 256 x T x 512 in bf16:
+// T = 100 65 and 94 us, 128 80 and 95, 512 308 and 284 (412 and 412 with an output gate, 427 and 445 in fp32), 2048 1231 and 992:
+// from some hundred steps on the scan is ahead there; with four times the threads the walk still is (1024 x 512 x 512 870
+// and 1032).
 constexpr uint32_t kWalkThreads = 65536;
 constexpr int64_t kTileSteps = (int64_t)kScanBlock / (kRecurBlock / kRecurChannels) * kRun;
 inline bool walks(const RecurArgs& a) {
@@ -546,8 +549,11 @@ inline RecurCut recur_cut(const RecurArgs& a) {
     }
     c.tiles = (int32_t)((runs + slots - 1) / slots);
     c.blocks = (uint32_t)((all + lanes - 1) / lanes);
-    // Two workgroups a CU, as many as their registers allow (768 gained nothing); split, at the price of the
-    // second read, only where a quarter of the CUs would have none.
+    // Split, at the price of the second read, into as many workgroups as the forward call without an output gate holds: two a
+    // CU by its registers (768 gained nothing).  The gated forward call and all gradients hold one a CU, so that between 129 and 191
+    // blocks their parts go in two rounds.  Whole steps of B x 2048 x 960, in bf16 without and with an output gate and in fp32, as it is and
+    // unsplit: 105 blocks 95 and 107, 129 and 142, 148 and 150 us; 135 123 and 113; 150 127 and 116, 172 and 153; 180 153 and
+    // 123, 212 and 159, 228 and 181: from some 130 blocks on a call would be better left whole.
     if (c.blocks < 192)
         c.splits = (int32_t)std::max<int64_t>(1, std::min<int64_t>({(int64_t)(kScanGroups / c.blocks), (int64_t)c.tiles, (int64_t)kMaxSplits}));
     c.groups = c.blocks * (uint32_t)c.splits;

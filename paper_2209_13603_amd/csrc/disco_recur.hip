@@ -11,9 +11,9 @@
 // leaves CUs idle the time axis is split: k_recur_maps finds the splits' maps
 // first, at the price of a second read.  States and maps are fp32 throughout.
 //
-// Measured, bf16: 16384 channels of 2048 steps with an output gate 78 us (scan, 268 MB, 3.4 TB/s: the
-// loads of a tile wait for its one barrier); 1048576 of 24 steps 38 us (walk, 151 MB, 4.0 TB/s); one series of 131072 x
-// 768 without an output gate 108 us the maps (403 MB) and 132 us the states (604 MB, of which the
+// Measured (kernel traces), bf16: 16384 channels of 2048 steps with an output gate 70 us (scan, 268 MB, 3.8 TB/s: the
+// loads of a tile wait for its one barrier); 1048576 of 24 steps 33 us (walk, 151 MB, 4.5 TB/s); one series of 131072 x
+// 768 without an output gate 96 us the maps (403 MB, 4.2 TB/s) and 134 us the states (604 MB, 4.5 TB/s, of which the
 // first third is still in the caches).
 #include <hip/hip_runtime.h>
 

@@ -20,9 +20,11 @@
 // a run of rows and leaves one partial row a sum (one an item for weights of
 // [batch, channels]), which k_residual_join adds.
 //
-// Measured, bf16: 32768 rows of 1024, dropped, both norms and a gate 50 us forward (268 MB, 5.4 TB/s)
-// and 96 us gradients (403 MB, 4.2 TB/s); 4050 rows of 8192 48 and 92 us; 32768 rows of 512
-// forward 23 us (134 MB, in part from the caches).
+// Measured (kernel traces), bf16: 32768 rows of 1024, dropped, both norms and a gate 45.5 us forward (268 MB, 5.9 TB/s)
+// and 95 us gradients (403 MB, 4.2 TB/s); 4050 rows of 8192 42 and 93 us; 32768 rows of 512
+// forward 23 us (134 MB, in part from the caches).  Rows of weights by item go item by item: of few tokens an item most
+// of a workgroup's slots are idle (bf16 kernels by events, one token each of 8192 items of 64 channels 42 us forward, 137 + 80
+// gradients and join, with shared weights 7, 11 + 6; of 256 items of 1024 11, 29 + 42 and 6, 15 + 6).
 #include <hip/hip_runtime.h>
 
 #include <cstdint>
@@ -116,7 +118,9 @@ __global__ __launch_bounds__(512) void k_residual(ResidualArgs a, NormShape s) {
 }
 
 constexpr int kForwardChunks = 2;
-// Workgroups of a launch: as many as the CUs hold at a time by their registers.
+// Workgroups of a launch: as many as the CUs hold at a time by bf16's registers (of one chunk a thread they would hold
+// one to three waves a SIMD more).  fp32 of two chunks holds three waves a SIMD, 768 workgroups of these 1024, and the rest go in a
+// second round: 32768 rows of 1024 106 us by events (537 MB, 5.1 TB/s).
 uint32_t forward_groups(const NormShape& s) {
     return 256 * (uint32_t)std::max(1, 4 * (s.nv == 1 ? 5 : 4) / (s.threads / kNormWave));
 }

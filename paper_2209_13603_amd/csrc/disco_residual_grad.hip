@@ -5,7 +5,10 @@
 // (of f^2; of h^2 with t n2; of t n1) are taken within a wave or a workgroup, and
 // the products that make the weights' gradients add up in LDS over a
 // workgroup's run of rows.  With dropout and all three sums it reaches 4.2 TB/s (32768 x 1024
-// bf16, 96 us): eight waves a CU are all that a row and the next one's loads leave room for.
+// bf16, 95 us): with two chunks a thread eight waves a CU are all that a row and the next one's loads leave
+// room for.  One chunk a thread (up to 512 channels) holds sixteen; such rows over 128 lanes, with barriers for their
+// sums, were not measured.  fp32 rows of more than 4096 channels, a workgroup of 1024 threads with 128 registers each, spill 16 to
+// 97 of them (2000 x 8192 113 us by events, 3.5 TB/s).
 #include <hip/hip_runtime.h>
 
 #include <cstdint>
@@ -269,8 +272,7 @@ __global__ __launch_bounds__(1024) void k_residual_join(Joins js, NormShape s, i
 }
 
 // Workgroups: as many as the CUs hold at a time by their registers (a part of a
-// second round leaves most CUs idle: 4 x 8192 rows of 1024, 2048 workgroups of which 1536 are
-// held 126 us, 1536 108 us).
+// second round leaves most CUs idle).
 NormShape grad_shape(ResidualArgs* a) {
     NormShape s = norm_shape(a, a->bf16 ? 2 : 1);
     const int waves = s.threads / kNormWave, held = s.threads > 512 ? 16 : a->bf16 ? s.nv == 1 ? 16 : 8 : 12;
